@@ -8,6 +8,10 @@ the C ABI (include/spconv.h); all computation runs in the HIP kernels.
 
 A rule book is reusable for every layer with the same site set (Section 4 of
 the paper).  Everything runs on torch's current stream.
+
+What a block between two convolutions does with the rows they leave (layer norm,
+dropout, routing to experts, grouped products) is in rows.py, whose functions are
+exported here too.
 """
 from __future__ import annotations
 
@@ -441,3 +445,10 @@ def backward_weight(rb, op, x, dy, C_in, C_out, bias=True, stream=None):
         _stream_ptr(stream))
     _lib.check(st, "spconv_backward_weight")
     return dw, db
+
+
+# Operators on feature rows (they use the helpers above).
+from . import rows  # noqa: E402
+from .rows import *  # noqa: E402,F401,F403
+
+__all__ += rows.__all__

@@ -1,4 +1,5 @@
-"""ctypes binding of libspconv.so (the C ABI declared in include/spconv.h).
+"""ctypes binding of libspconv.so (the C ABI declared in include/spconv.h and
+include/spconv_rows.h).
 
 Argument marshalling only: every step of the rule-book build and of the
 forward runs in the library's HIP kernels.  PyTorch provides device memory
@@ -19,8 +20,9 @@ OP_VSC, OP_SC, OP_DC = 0, 1, 2
 POOL_MAX, POOL_AVG = 0, 1
 F32, BF16 = 0, 1
 BUILD_ASYNC, BUILD_TRANSPOSE = 1, 2
+ROUTE_MAX_EXPERTS, ROUTE_MAX_SLOTS = 1024, 16
 
-# Every symbol the header declares, with its ctypes signature.
+# Every symbol spconv.h declares, with its ctypes signature.
 _P, _I, _I64, _U = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint
 ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
 RELEASE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p)
@@ -49,6 +51,28 @@ SIGNATURES = {
     "spconv_status_string": (ctypes.c_char_p, [_I]),
 }
 
+# The same for spconv_rows.h.
+_U64, _D, _F, _SZ = ctypes.c_uint64, ctypes.c_double, ctypes.c_float, ctypes.c_size_t
+ROWS_SIGNATURES = {
+    "spconv_layer_norm_forward": (_I, [_I, _P, _P, _P, _F, _P, _P, _P, _I64, _I, _P]),
+    "spconv_layer_norm_backward_workspace": (_I, [_I64, _I, ctypes.POINTER(_SZ)]),
+    "spconv_layer_norm_backward": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I, _P, _SZ,
+                                        _P]),
+    "spconv_dropout_forward": (_I, [_I, _P, _P, _D, _U64, _U64, _P, _P, _I64, _P]),
+    "spconv_dropout_backward": (_I, [_I, _P, _D, _U64, _U64, _P, _P, _I64, _P]),
+    "spconv_route_workspace": (_I, [_I64, _I, _I, ctypes.POINTER(_SZ)]),
+    "spconv_route_forward": (_I, [_I, _P, _I64, _I, _I, _I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "spconv_route_backward": (_I, [_I, _P, _P, _P, _P, _I64, _I, _I, _I, _P, _P]),
+    "spconv_grouped_forward": (_I, [_I, _P, _I64, _P, _P, _P, _P, _I, _I, _P, _I64, _I, _I, _I,
+                                    _P]),
+    "spconv_grouped_backward_data": (_I, [_I, _P, _P, _P, _P, _I, _P, _I64, _I, _I, _I, _P]),
+    "spconv_grouped_backward_weight_workspace": (_I, [_I, _I64, _I, _I, _I, ctypes.POINTER(_SZ)]),
+    "spconv_grouped_backward_weight": (_I, [_I, _P, _I64, _P, _P, _P, _P, _P, _I64, _I, _I, _I, _P,
+                                            _SZ, _P]),
+    "spconv_combine_forward": (_I, [_I, _P, _I64, _P, _P, _P, _P, _I64, _I, _I, _P]),
+    "spconv_combine_backward": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I, _I, _P]),
+}
+
 
 class SpconvError(RuntimeError):
     def __init__(self, status, what=""):
@@ -69,7 +93,7 @@ def load():
         raise ImportError(
             f"{LIB_PATH} is missing: build it first (python -m paper_1706_01307_amd.build)")
     lib = ctypes.CDLL(LIB_PATH)
-    for name, (res, args) in SIGNATURES.items():
+    for name, (res, args) in {**SIGNATURES, **ROWS_SIGNATURES}.items():
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args

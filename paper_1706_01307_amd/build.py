@@ -13,7 +13,9 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libspconv.so")
 SOURCES = ["abi.hip", "rulebook.hip", "forward.hip", "forward_w0.hip", "forward_w1.hip",
            "forward_w2.hip", "forward_slab_ff.hip", "forward_slab_fb.hip", "forward_slab_bf.hip",
-           "forward_slab_bb.hip", "ops.hip", "sort.hip", "blockcache.hip", "noalloc.hip"]
+           "forward_slab_bb.hip", "ops.hip", "sort.hip", "blockcache.hip", "noalloc.hip",
+           "rows_norm.hip", "rows_dropout.hip", "rows_route.hip", "rows_grouped.hip",
+           "rows_combine.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -1,0 +1,496 @@
+// Routing: the k largest logits of every row, their softmax weights, and the
+// (row, slot) pairs grouped by expert in a stable order, without atomics that
+// decide an order.
+//
+//   k_route        a group of lanes per row picks the experts; the workgroup
+//                  ranks its own pairs per expert and leaves its counts;
+//   k_route_scan   per expert, the counts' running sums over the workgroups;
+//   k_route_place  every pair's position: its expert's start + its
+//                  workgroup's start + its rank.
+// Where one workgroup has every row, the first launch does it all.
+#include <cmath>
+
+#include "rows.h"
+
+namespace spc {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kMaxE = SPCONV_ROUTE_MAX_EXPERTS;
+constexpr int kMaxK = SPCONV_ROUTE_MAX_SLOTS;
+constexpr int kPairs = 2048;           // pairs a workgroup ranks at most
+
+// Rows a workgroup takes: a power of two, at most 256 (one row a lane).
+__host__ __device__ inline int rows_per_block(int64_t n, int E, int k) {
+  int r = 256;
+  while (r * k > kPairs) r /= 2;
+  // so few that one workgroup is done sooner than two more launches begin
+  if (n <= r && n * E <= 16384) return r;
+  // as long as there are fewer workgroups than compute units
+  while (r > 32 && (n + r - 1) / r < 256) r /= 2;
+  return r;
+}
+
+// A logit's order as an unsigned number: larger is larger, -0 equals +0, every
+// NaN is the largest.  0 is below -infinity (kNone).
+constexpr uint32_t kNone = 0x007fffffu;            // the order of -infinity
+__device__ __forceinline__ uint32_t order_of(float v) {
+  if (v != v) return 0xffffffffu;
+  const uint32_t u = __float_as_uint(v + 0.0f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+  return __uint_as_float(o == 0xffffffffu ? 0x7fc00000u : o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+
+// The largest (order, lowest column) of the group's lanes.
+template <int STEP> __device__ __forceinline__ void best_step(uint32_t& o, uint32_t& c) {
+  const uint32_t o2 = lane_other<STEP>(o), c2 = lane_other<STEP>(c);
+  const bool take = o2 > o || (o2 == o && c2 < c);
+  o = take ? o2 : o;
+  c = take ? c2 : c;
+}
+template <int LPR> __device__ __forceinline__ void group_best(uint32_t& o, uint32_t& c) {
+  if constexpr (LPR > 1) best_step<1>(o, c);
+  if constexpr (LPR > 2) best_step<2>(o, c);
+  if constexpr (LPR > 4) best_step<4>(o, c);
+  if constexpr (LPR > 8) best_step<8>(o, c);
+  if constexpr (LPR > 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(o, o, false, false);
+    const auto b = __builtin_amdgcn_permlane16_swap(c, c, false, false);
+    const bool take = a[1] > a[0] || (a[1] == a[0] && b[1] < b[0]);
+    o = take ? a[1] : a[0];
+    c = take ? b[1] : b[0];
+  }
+  if constexpr (LPR > 32) {
+    const auto a = __builtin_amdgcn_permlane32_swap(o, o, false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    const bool take = a[1] > a[0] || (a[1] == a[0] && b[1] < b[0]);
+    o = take ? a[1] : a[0];
+    c = take ? b[1] : b[0];
+  }
+}
+
+// The sum over a whole wave's lanes before this one.
+__device__ __forceinline__ int32_t wave_exclusive(int32_t v, int32_t* total) {
+  int32_t s = v;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int32_t o = __shfl_up(s, d, 64);
+    if (static_cast<int>(threadIdx.x & 63) >= d) s += o;
+  }
+  *total = __shfl(s, 63, 64);
+  return s - v;
+}
+
+// Exclusive running sums of v[0..E) in place, E <= kMaxE; the whole workgroup
+// calls it.  Returns the total.
+__device__ int32_t block_scan(int32_t* v, int E, int32_t* s_wave) {
+  constexpr int PER = kMaxE / kThreads;
+  const int wave = threadIdx.x >> 6;
+  int32_t a[PER], sum = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = threadIdx.x * PER + i;
+    a[i] = e < E ? v[e] : 0;
+    sum += a[i];
+  }
+  int32_t total;
+  int32_t base = wave_exclusive(sum, &total);
+  if ((threadIdx.x & 63) == 0) s_wave[wave] = total;
+  __syncthreads();
+  int32_t all = 0;
+#pragma unroll
+  for (int q = 0; q < kWaves; ++q) {
+    if (q < wave) base += s_wave[q];
+    all += s_wave[q];
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = threadIdx.x * PER + i;
+    if (e < E) v[e] = base;
+    base += a[i];
+  }
+  __syncthreads();
+  return all;
+}
+
+// LPR lanes hold a row of at most LPR * NV * VEC logits.
+template <typename T, int LPR, int NV, bool TAIL>
+__global__ __launch_bounds__(kThreads) void k_route(
+    const T* __restrict__ logits, int64_t n, int E, int k, int normalize, int rows_blk,
+    int32_t* __restrict__ experts, float* __restrict__ weights, int32_t* __restrict__ offsets,
+    int32_t* __restrict__ rows, int32_t* __restrict__ pos, int32_t* __restrict__ counts) {
+  constexpr int VEC = Row<T>::VEC, G = kThreads / LPR;
+  __shared__ int16_t s_expert[kPairs];
+  __shared__ float s_weight[kPairs];
+  __shared__ int32_t s_count[kWaves][kMaxE];       // running counts of the waves' runs of pairs
+  __shared__ int32_t s_start[kMaxE], s_wave[kWaves];
+  const int lane = threadIdx.x % LPR;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows_blk;
+  const int nrow = static_cast<int>(n - row0 < rows_blk ? n - row0 : rows_blk);
+  for (int e = threadIdx.x; e < E; e += kThreads)
+#pragma unroll
+    for (int q = 0; q < kWaves; ++q) s_count[q][e] = 0;
+
+  for (int q = threadIdx.x / LPR; q < nrow; q += G) {   // (a group's lanes stay together)
+    const int64_t r = row0 + q;
+    uint32_t o[NV][VEC];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (lane + LPR * j) * VEC;
+      float v[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = 0.0f;
+      if (c < E) load_row<T, TAIL>(logits + r * E, c, E, v);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) o[j][i] = c + i < E ? order_of(v[i]) : 0u;
+    }
+    float top = 0.0f, sum = 0.0f;
+    for (int s = 0; s < k; ++s) {
+      uint32_t bo = 0, bc = 0xffffffffu;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+          if (o[j][i] > bo) {                      // ascending columns: the lowest of equals
+            bo = o[j][i];
+            bc = (lane + LPR * j) * VEC + i;
+          }
+      group_best<LPR>(bo, bc);
+      const bool some = bo > kNone;
+      const float v = value_of(bo);
+      if (s == 0) {
+        top = some ? v : 0.0f;
+        if (!normalize) {
+          // the whole row's sum, before anything is taken out of it
+#pragma unroll
+          for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+              if (o[j][i]) sum += expf(value_of(o[j][i]) - top);
+          sum = group_sum<LPR>(sum);
+        }
+      }
+      const float w = some ? expf(v - top) : 0.0f;
+      if (normalize) sum += w;
+      if (lane == s % LPR) {
+        s_expert[q * k + s] = static_cast<int16_t>(some ? static_cast<int32_t>(bc) : -1);
+        s_weight[q * k + s] = w;
+      }
+      // take it out
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+          if (static_cast<uint32_t>((lane + LPR * j) * VEC + i) == bc) o[j][i] = 0u;
+    }
+    // (each lane divides the slots it wrote)
+    for (int s = lane; s < k; s += LPR)
+      if (s_expert[q * k + s] >= 0) s_weight[q * k + s] /= sum;
+  }
+  __syncthreads();
+  const int npair = nrow * k, wave = threadIdx.x >> 6, wl = threadIdx.x & 63;
+  for (int p = threadIdx.x; p < npair; p += kThreads) {
+    experts[row0 * k + p] = s_expert[p];
+    weights[row0 * k + p] = s_weight[p];
+  }
+
+  // Ranks: each wave takes a run of the pairs, counts it per expert, and then
+  // numbers it 64 pairs at a time from where the runs before it end.
+  const int run = (npair + kWaves * 64 - 1) / (kWaves * 64) * 64;
+  const int p0 = wave * run, p1 = p0 + run < npair ? p0 + run : npair;
+  for (int p = p0 + wl; p < p1; p += 64) {
+    const int e = s_expert[p];
+    if (e >= 0) atomicAdd(&s_count[wave][e], 1);   // (a count: no order in it)
+  }
+  __syncthreads();
+  const bool single = gridDim.x == 1;
+  for (int e = threadIdx.x; e < E; e += kThreads) {
+    int32_t a = 0;
+#pragma unroll
+    for (int q = 0; q < kWaves; ++q) {
+      const int32_t c = s_count[q][e];
+      s_count[q][e] = a;
+      a += c;
+    }
+    s_start[e] = a;
+    if (!single) counts[static_cast<int64_t>(e) * gridDim.x + blockIdx.x] = a;
+  }
+  int32_t total = 0;
+  if (single) {
+    total = block_scan(s_start, E, s_wave);
+    for (int e = threadIdx.x; e < E; e += kThreads) offsets[e] = s_start[e];
+    if (threadIdx.x == 0) offsets[E] = total;
+  }
+  __syncthreads();
+  int ebits = 0;
+  while ((1 << ebits) < E) ++ebits;
+  for (int b = p0; b < p1; b += 64) {              // (uniform over the wave)
+    const int p = b + wl;
+    const int e = p < p1 ? s_expert[p] : -1;
+    uint64_t same = __ballot(e >= 0);
+    for (int t = 0; t < ebits; ++t) {
+      const uint64_t m = __ballot((e >> t) & 1);
+      same &= (e >> t) & 1 ? m : ~m;
+    }
+    if (e >= 0) {
+      const int before = __popcll(same & ((1ull << wl) - 1));
+      const int32_t rank = s_count[wave][e] + before;
+      const int64_t at = row0 * k + p;
+      if (single) {
+        const int32_t where = s_start[e] + rank;
+        pos[at] = where;
+        rows[where] = static_cast<int32_t>(row0 + p / k);
+      } else {
+        pos[at] = rank;                            // k_route_place adds the starts
+      }
+    } else if (p < p1) {
+      pos[row0 * k + p] = -1;
+    }
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // the last of each expert's lanes moves its count on
+    if (e >= 0 && (same >> wl) == 1ull) s_count[wave][e] += __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (single)
+    for (int64_t p = total + threadIdx.x; p < n * k; p += kThreads) rows[p] = -1;
+}
+
+// A workgroup per expert: exclusive running sums of its counts over the
+// workgroups, in place; the total behind them.
+__global__ __launch_bounds__(1024) void k_route_scan(int32_t* __restrict__ counts, int nblk,
+                                                     int32_t* __restrict__ totals) {
+  __shared__ int32_t s_wave[16];
+  int32_t* c = counts + static_cast<int64_t>(blockIdx.x) * nblk;
+  const int wave = threadIdx.x >> 6;
+  int32_t carry = 0;
+  for (int b = 0; b < nblk; b += 1024) {
+    const int i = b + threadIdx.x;
+    const int32_t v = i < nblk ? c[i] : 0;
+    int32_t total;
+    int32_t ex = wave_exclusive(v, &total);
+    if ((threadIdx.x & 63) == 0) s_wave[wave] = total;
+    __syncthreads();
+    int32_t all = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      if (q < wave) ex += s_wave[q];
+      all += s_wave[q];
+    }
+    if (i < nblk) c[i] = carry + ex;
+    carry += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) totals[blockIdx.x] = carry;
+}
+
+__global__ __launch_bounds__(kThreads) void k_route_place(
+    const int32_t* __restrict__ experts, const int32_t* __restrict__ starts,
+    const int32_t* __restrict__ totals, int64_t n, int E, int k, int rows_blk,
+    int32_t* __restrict__ offsets, int32_t* __restrict__ rows, int32_t* __restrict__ pos) {
+  __shared__ int32_t s_start[kMaxE], s_wave[kWaves];
+  for (int e = threadIdx.x; e < E; e += kThreads) s_start[e] = totals[e];
+  const int32_t total = block_scan(s_start, E, s_wave);
+  if (blockIdx.x == 0) {
+    for (int e = threadIdx.x; e < E; e += kThreads) offsets[e] = s_start[e];
+    if (threadIdx.x == 0) offsets[E] = total;
+    __syncthreads();
+  }
+  for (int e = threadIdx.x; e < E; e += kThreads)
+    s_start[e] += starts[static_cast<int64_t>(e) * gridDim.x + blockIdx.x];
+  __syncthreads();
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows_blk;
+  const int64_t end = (row0 + rows_blk < n ? row0 + rows_blk : n) * k;
+  for (int64_t p = row0 * k + threadIdx.x; p < end; p += kThreads) {
+    const int32_t e = experts[p];
+    if (e < 0) continue;
+    const int32_t where = s_start[e] + pos[p];
+    pos[p] = where;
+    rows[where] = static_cast<int32_t>(row0 + static_cast<int32_t>(p - row0 * k) / k);
+  }
+  for (int64_t p = total + static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; p < n * k;
+       p += static_cast<int64_t>(gridDim.x) * kThreads)
+    rows[p] = -1;
+}
+
+// The gradient: every lane sums the row's slots itself (they are the same
+// addresses for the whole group), then finds its columns among them.
+template <typename T, int LPR, int NV, bool TAIL>
+__global__ __launch_bounds__(kThreads) void k_route_bwd(
+    const float* __restrict__ dweights, const T* __restrict__ logits,
+    const int32_t* __restrict__ experts, const float* __restrict__ weights, int64_t n, int E,
+    int k, int normalize, T* __restrict__ dlogits) {
+  constexpr int VEC = Row<T>::VEC, G = kThreads / LPR;
+  const int lane = threadIdx.x % LPR;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * G + threadIdx.x / LPR;
+  if (r >= n) return;
+  float v[NV][VEC];
+  float inv = 0.0f;
+  if (!normalize) {
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (lane + LPR * j) * VEC;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[j][i] = -INFINITY;
+      if (c < E) load_row<T, TAIL>(logits + r * E, c, E, v[j]);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        if (c + i >= E) v[j][i] = -INFINITY;
+        top = v[j][i] > top || v[j][i] != v[j][i] ? v[j][i] : top;
+      }
+    }
+    top = group_reduce<LPR>(top, [](float a, float b) { return b > a || b != b ? b : a; });
+    if (top == -INFINITY) top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        v[j][i] = expf(v[j][i] - top);
+        sum += v[j][i];
+      }
+    sum = group_sum<LPR>(sum);
+    inv = sum == 0.0f ? 0.0f : 1.0f / sum;         // (a row that is all closed)
+  }
+  float dot = 0.0f;
+  for (int s = 0; s < k; ++s)
+    if (experts[r * k + s] >= 0) dot += weights[r * k + s] * dweights[r * k + s];
+  float g[NV][VEC];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) g[j][i] = normalize ? 0.0f : -(v[j][i] * inv) * dot;
+  for (int s = 0; s < k; ++s) {
+    const int32_t e = experts[r * k + s];
+    if (e < 0) continue;
+    const float d = weights[r * k + s] * (normalize ? dweights[r * k + s] - dot
+                                                    : dweights[r * k + s]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i)
+        if ((lane + LPR * j) * VEC + i == e) g[j][i] += d;
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (lane + LPR * j) * VEC;
+    if (c < E) store_row<T, TAIL>(dlogits + r * E, c, E, g[j]);
+  }
+}
+
+struct Fwd {
+  const void* logits;
+  int64_t n;
+  int E, k, normalize;
+  int32_t* experts;
+  float* weights;
+  int32_t *offsets, *rows, *pos, *counts;
+  hipStream_t st;
+};
+template <typename T, int LPR, int NV> void run(const Fwd& a) {
+  const int rb = rows_per_block(a.n, a.E, a.k);
+  const int nblk = a.n ? static_cast<int>((a.n + rb - 1) / rb) : 1;
+  const T* l = static_cast<const T*>(a.logits);
+  if (a.E % Row<T>::VEC)
+    k_route<T, LPR, NV, true><<<nblk, kThreads, 0, a.st>>>(l, a.n, a.E, a.k, a.normalize, rb,
+                                                          a.experts, a.weights, a.offsets, a.rows,
+                                                          a.pos, a.counts);
+  else
+    k_route<T, LPR, NV, false><<<nblk, kThreads, 0, a.st>>>(l, a.n, a.E, a.k, a.normalize, rb,
+                                                           a.experts, a.weights, a.offsets, a.rows,
+                                                           a.pos, a.counts);
+  if (nblk > 1) {
+    int32_t* totals = a.counts + static_cast<int64_t>(nblk) * a.E;
+    k_route_scan<<<a.E, 1024, 0, a.st>>>(a.counts, nblk, totals);
+    k_route_place<<<nblk, kThreads, 0, a.st>>>(a.experts, a.counts, totals, a.n, a.E, a.k, rb,
+                                              a.offsets, a.rows, a.pos);
+  }
+}
+struct Bwd {
+  const float* dweights;
+  const void* logits;
+  const int32_t* experts;
+  const float* weights;
+  int64_t n;
+  int E, k, normalize;
+  void* dlogits;
+  hipStream_t st;
+};
+template <typename T, int LPR, int NV> void run(const Bwd& a) {
+  const uint32_t blocks = static_cast<uint32_t>((a.n + kThreads / LPR - 1) / (kThreads / LPR));
+  const T* l = static_cast<const T*>(a.logits);
+  T* d = static_cast<T*>(a.dlogits);
+  if (a.E % Row<T>::VEC)
+    k_route_bwd<T, LPR, NV, true><<<blocks, kThreads, 0, a.st>>>(
+        a.dweights, l, a.experts, a.weights, a.n, a.E, a.k, a.normalize, d);
+  else
+    k_route_bwd<T, LPR, NV, false><<<blocks, kThreads, 0, a.st>>>(
+        a.dweights, l, a.experts, a.weights, a.n, a.E, a.k, a.normalize, d);
+}
+// The fewest lanes whose registers hold the row, one piece a lane up to a wave.
+template <typename T, typename A> void by_width(const A& a) {
+  const int pieces = (a.E + Row<T>::VEC - 1) / Row<T>::VEC;
+  if (pieces <= 1) return run<T, 1, 1>(a);
+  if (pieces <= 2) return run<T, 2, 1>(a);
+  if (pieces <= 4) return run<T, 4, 1>(a);
+  if (pieces <= 8) return run<T, 8, 1>(a);
+  if (pieces <= 16) return run<T, 16, 1>(a);
+  if (pieces <= 32) return run<T, 32, 1>(a);
+  if (pieces <= 64) return run<T, 64, 1>(a);
+  if (pieces <= 128) return run<T, 64, 2>(a);
+  if constexpr (Row<T>::VEC == 4) run<T, 64, 4>(a);
+}
+
+bool sizes_ok(int64_t n, int E, int k) {
+  return rows_ok(n) && E >= 1 && E <= kMaxE && k >= 1 && k <= kMaxK && k <= E && rows_ok(n * k);
+}
+
+}  // namespace
+}  // namespace spc
+
+using namespace spc;
+
+extern "C" int spconv_route_workspace(int64_t n, int E, int k, size_t* bytes) {
+  if (!sizes_ok(n, E, k) || !bytes) return SPCONV_EINVAL;
+  const int rb = rows_per_block(n, E, k);
+  const int64_t nblk = (n + rb - 1) / rb;
+  *bytes = nblk > 1 ? static_cast<size_t>((nblk + 1) * E) * sizeof(int32_t) : 0;
+  return SPCONV_OK;
+}
+
+extern "C" int spconv_route_forward(int dt, const void* logits, int64_t n, int E, int k,
+                                    int normalize, int32_t* experts, float* weights,
+                                    int32_t* offsets, int32_t* rows, int32_t* pos, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  if (!dtype_ok(dt) || (normalize != 0 && normalize != 1) ||
+      spconv_route_workspace(n, E, k, &need) != SPCONV_OK || !ptr_ok(logits, n, elem_bytes(dt)) ||
+      !ptr_ok(experts, n, 4) || !ptr_ok(weights, n, 4) || !ptr_ok(offsets, 1, 4) ||
+      !ptr_ok(rows, n, 4) || !ptr_ok(pos, n, 4) ||
+      (need && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)))
+    return SPCONV_EINVAL;
+  // (no rows: one workgroup without rows writes the offsets)
+  const Fwd a{logits, n, E, k, normalize, experts, weights, offsets, rows, pos,
+              static_cast<int32_t*>(workspace), static_cast<hipStream_t>(stream)};
+  if (dt == SPCONV_BF16) by_width<bf16_t>(a); else by_width<float>(a);
+  return launched();
+}
+
+extern "C" int spconv_route_backward(int dt, const float* dweights, const void* logits,
+                                     const int32_t* experts, const float* weights, int64_t n, int E,
+                                     int k, int normalize, void* dlogits, void* stream) {
+  if (!dtype_ok(dt) || (normalize != 0 && normalize != 1) || !sizes_ok(n, E, k) ||
+      !ptr_ok(dweights, n, 4) || !ptr_ok(logits, normalize ? 0 : n, elem_bytes(dt)) ||
+      !ptr_ok(experts, n, 4) || !ptr_ok(weights, n, 4) || !ptr_ok(dlogits, n, elem_bytes(dt)))
+    return SPCONV_EINVAL;
+  if (n == 0) return SPCONV_OK;
+  const Bwd a{dweights, logits, experts, weights, n, E, k, normalize, dlogits,
+              static_cast<hipStream_t>(stream)};
+  if (dt == SPCONV_BF16) by_width<bf16_t>(a); else by_width<float>(a);
+  return launched();
+}
