@@ -141,7 +141,7 @@ int spconv_route_backward(int dt, const float* dweights, const void* logits,
  *            [0, n_x) reads a row of zeros
  *   bias     fp32 [E][C_out] or NULL
  *   y        dtype out_dt, [m][C_out]; positions from offsets[E] on are zero
- * 1 <= E <= 65535; offsets[0] must be 0.  Non-finite values reach the
+ * 1 <= E <= 65535, C_in and C_out up to 2^23; offsets[0] must be 0.  Non-finite values reach the
  * positions whose rows or group hold them, and no others. */
 int spconv_grouped_forward(int in_dt, const void* x, int64_t n_x, const void* w,
                            const int32_t* offsets, const int32_t* rows, const float* bias,

@@ -103,13 +103,16 @@ template <> struct Mma<float> {
   __device__ static Frag ones() { return Frag{1.0f, 1.0f, 1.0f, 1.0f}; }
 };
 
-// Staged tiles in LDS, in 16-byte pieces.
+// Staged tiles in LDS, in 16-byte pieces: a stage is 128 bytes of the reduction
+// (BK elements), so that a row's load is a whole cache line (with 64 bytes the
+// address unit took 55 cycles an instruction instead of 17 and bounded both
+// kernels).
 //
-// RTile: R rows of 128 bytes of the reduction.  A fragment read takes one piece
-// column of 16 rows per cycle, so pieces are permuted by the row's bits 1 to 3:
-// 16 rows then cover the 64 banks once.
+// RTile: R rows of BK elements.  A fragment read takes one piece column of 16
+// rows per cycle, so pieces are permuted by the row's bits 1 to 3: 16 rows then
+// cover the 64 banks once.
+template <typename T> constexpr int kBK = 128 / static_cast<int>(sizeof(T));
 template <typename T, int R> struct RTile {
-  static constexpr int VEC = Row<T>::VEC, BK = 128 / static_cast<int>(sizeof(T));
   static constexpr int PIECES = R * 8, BYTES = R * 128;
   __device__ static int at(int row, int piece) { return row * 8 + (piece ^ ((row >> 1) & 7)); }
   // rows r0..r0+31, reduction from piece 2 s
@@ -122,9 +125,8 @@ template <typename T, int R> struct RTile {
 // rows must lie in different banks.  fp32: one element a lane; the two halves of
 // a wave read rows 4 apart.
 template <typename T, int W> struct KTile {
-  static constexpr int VEC = Row<T>::VEC, BK = 128 / static_cast<int>(sizeof(T));
-  static constexpr int PR = W / VEC;                // pieces per row
-  static constexpr int PIECES = BK * PR, BYTES = PIECES * 16;
+  static constexpr int VEC = Row<T>::VEC, PR = W / VEC;   // pieces per row
+  static constexpr int PIECES = kBK<T> * PR, BYTES = PIECES * 16;
   __device__ static int at(int k, int piece) {
     if constexpr (sizeof(T) == 2) {
       const int x = W >= 128 ? (k & 3) << 2 : W == 64 ? ((k >> 1) & 1) << 2 : 0;
@@ -160,64 +162,29 @@ template <typename T, int W> struct KTile {
   }
 };
 
+// What a lane reads where there is nothing to read: a load that always happens
+// needs no branch, and its value no test.
+__device__ const u32x4_t g_zeros = {0u, 0u, 0u, 0u};
+
 // A piece of a row: `left` elements of it remain (<= 0: none, zeros).
 // WHOLE: remaining counts are multiples of a piece.
 template <typename T, bool WHOLE>
 __device__ __forceinline__ u32x4_t load_left(const T* p, int64_t left) {
   constexpr int VEC = Row<T>::VEC;
-  u32x4_t v = {0u, 0u, 0u, 0u};
-  if (WHOLE ? left > 0 : left >= VEC) {
-    v = load_piece(p);
-  } else if (!WHOLE && left > 0) {
-    T e[VEC];
+  if constexpr (WHOLE) {
+    return load_piece(left > 0 ? p : reinterpret_cast<const T*>(&g_zeros));
+  } else {
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (left >= VEC) {
+      v = load_piece(p);
+    } else if (left > 0) {
+      T e[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) e[i] = i < left ? p[i] : T(0);
-    __builtin_memcpy(&v, e, 16);
-  }
-  return v;
-}
-
-// Finished fp32 values [BR][BC] of the workgroup go through LDS, rounded to TO,
-// so that whole rows leave in 16-byte pieces.  FR x FC blocks of 32 x 32 per
-// wave at (r0, c0); acc[fc][fr] as Mma leaves them with the columns as the first
-// operand.
-template <typename TO, int BR, int BC, int FR, int FC>
-__device__ __forceinline__ void tile_to_lds(TO* s, const f32x16 (&acc)[FC][FR], int r0, int c0,
-                                            const float* __restrict__ bias, int64_t bias_left,
-                                            int relu) {
-  constexpr int VO = Row<TO>::VEC, PR = BC / VO;
-  const int lane = threadIdx.x & 63, h = lane >> 5;
-#pragma unroll
-  for (int fc = 0; fc < FC; ++fc)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int c = c0 + 32 * fc + 8 * q + 4 * h;
-      float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (bias) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] = c + i < bias_left ? bias[c + i] : 0.0f;
-      }
-#pragma unroll
-      for (int fr = 0; fr < FR; ++fr) {
-        const int r = r0 + 32 * fr + (lane & 31);
-        TO v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float z = acc[fc][fr][4 * q + i] + b[i];
-          if (relu && z < 0.0f) z = 0.0f;
-          v[i] = Row<TO>::put(z);
-        }
-        const int piece = (c / VO) ^ (r & (PR - 1));
-        __builtin_memcpy(__builtin_assume_aligned(s + (r * PR + piece) * VO + c % VO,
-                                                  4 * sizeof(TO)),
-                         v, sizeof v);
-      }
+      for (int i = 0; i < VEC; ++i) e[i] = i < left ? p[i] : T(0);
+      __builtin_memcpy(&v, e, 16);
     }
-}
-template <typename TO, int BR, int BC>
-__device__ __forceinline__ u32x4_t lds_piece(const TO* s, int r, int piece) {
-  constexpr int VO = Row<TO>::VEC, PR = BC / VO;
-  return reinterpret_cast<const u32x4_t*>(s)[r * PR + (piece ^ (r & (PR - 1)))];
+    return v;
+  }
 }
 template <typename TO>
 __device__ __forceinline__ void store_left(TO* p, u32x4_t v, int64_t left) {
@@ -233,6 +200,38 @@ __device__ __forceinline__ void store_left(TO* p, u32x4_t v, int64_t left) {
   }
 }
 
+// A wave's FM blocks of 32 x 32 of one column block go to LDS, rounded, as rows
+// of CW columns (the first operand's rows are the columns: a lane has 4 adjacent
+// ones of one row in every four registers).  Pieces are permuted by the row, so
+// that the 32 rows of a write and the rows of a read lie in different banks.
+template <typename TO, int CW> __device__ __forceinline__ int out_at(int r, int piece) {
+  constexpr int PR = CW / Row<TO>::VEC;
+  return r * PR + (piece ^ (r & (PR - 1)));
+}
+template <typename TO, int CW, int FM>
+__device__ __forceinline__ void block_to_lds(u32x4_t* s, const f32x16 (&acc)[FM], int r0, int c0,
+                                             const float (&bias)[16], int relu) {
+  constexpr int VO = Row<TO>::VEC;
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int c = c0 + 8 * q + 4 * h;
+#pragma unroll
+    for (int m = 0; m < FM; ++m) {
+      const int r = r0 + 32 * m + (lane & 31);
+      TO v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z = acc[m][4 * q + i] + bias[4 * q + i];
+        if (relu && z < 0.0f) z = 0.0f;
+        v[i] = Row<TO>::put(z);
+      }
+      TO* d = reinterpret_cast<TO*>(s + out_at<TO, CW>(r, c / VO)) + c % VO;
+      __builtin_memcpy(__builtin_assume_aligned(d, 4 * sizeof(TO)), v, sizeof v);
+    }
+  }
+}
+
 struct GroupedArgs {
   const void* x;               // [n_x][red]
   int64_t n_x;
@@ -245,48 +244,57 @@ struct GroupedArgs {
   void* y;                     // [m][cols]
   int64_t m;
   int E, red, cols;            // reduction, output columns
+  int strip;                   // column tiles a workgroup takes
   hipStream_t st;
 };
 
-// Rows x weights of a BM x BN tile: BT false: w[e] is [red][cols] (the forward),
-// BT true: w[e] is [cols][red] (the input gradient).  Four waves in 2 x 2.  The
-// pieces of the next 128 bytes of the reduction are requested into registers
-// while the present ones, in LDS, are multiplied; two LDS buffers, one barrier a
-// step.
+// Rows x weights: BT false: w[e] is [red][cols] (the forward), BT true: w[e] is
+// [cols][red] (the input gradient).  A workgroup takes BM positions of a group
+// and `strip` column tiles of BN one after the other, four waves in 2 x 2.  Its
+// stages (128 bytes of the reduction of one column tile) run on across the
+// column tiles: the next kDepth stages' pieces are on their way into registers
+// while one, in LDS, is multiplied; two LDS buffers, one barrier a stage.  A
+// finished tile leaves through the buffer that is free then, as whole rows (in
+// 32-byte parts of rows, stored from the registers, the forward wrote 1.8 times
+// its bytes to memory).
 template <typename T, typename TO, bool BT, int BM, int BN, bool WHOLE>
 __global__ __launch_bounds__(kThreads, 2) void k_grouped(GroupedArgs a) {
   typedef Mma<T> M;
   typedef RTile<T, BM> TA;
   typedef RTile<T, BN> TBr;
   typedef KTile<T, BN> TBk;
-  constexpr int VEC = Row<T>::VEC, BK = TA::BK, STEPS = BK / M::KS;
+  constexpr int VEC = Row<T>::VEC, BK = kBK<T>, STEPS = BK / M::KS, kDepth = 2;
   constexpr int FM = BM / 64, FN = BN / 64;
   constexpr int PA = TA::PIECES / kThreads;
   constexpr int PB = TBk::PIECES / kThreads;       // (as many as TBr's)
   constexpr int kStage = TA::BYTES + TBk::BYTES;
-  constexpr int kOut = BM * BN * static_cast<int>(sizeof(TO));
-  __shared__ __attribute__((aligned(16))) unsigned char
-      s_buf[2 * kStage > kOut ? 2 * kStage : kOut];
+  __shared__ __attribute__((aligned(16))) unsigned char s_buf[2 * kStage];
   const T* const x = static_cast<const T*>(a.x);
   TO* const y = static_cast<TO*>(a.y);
-  const int64_t ncol = (a.cols + BN - 1) / BN;
+  const int ncol = (a.cols + BN - 1) / BN, nstrip = (ncol + a.strip - 1) / a.strip;
   const int64_t id = die_order(blockIdx.x, gridDim.x);
-  const Tile t = find_tile<true>(a.offsets, a.E, a.m, BM, id / ncol);
+  const Tile t = find_tile<true>(a.offsets, a.E, a.m, BM, id / nstrip);
   if (t.group < 0) return;
-  const int64_t n0 = id % ncol * BN;
+  const int tile0 = static_cast<int>(id % nstrip) * a.strip;
+  const int ntile = ncol - tile0 < a.strip ? ncol - tile0 : a.strip;
   const int nrow = static_cast<int>(t.end - t.begin);
   if (t.group == a.E) {                            // behind the last group
-    for (int p = threadIdx.x; p < nrow * BN; p += kThreads) {
-      const int64_t c = n0 + p % BN;
-      if (c < a.cols) y[(t.begin + p / BN) * a.cols + c] = Row<TO>::put(0.0f);
-    }
+    const int64_t c0 = static_cast<int64_t>(tile0) * BN;
+    const int64_t c1 = c0 + static_cast<int64_t>(ntile) * BN;
+    const int64_t end = c1 < a.cols ? c1 : a.cols;
+    for (int r = 0; r < nrow; ++r)
+      for (int64_t c = c0 + threadIdx.x; c < end; c += kThreads)
+        y[(t.begin + r) * a.cols + c] = Row<TO>::put(0.0f);
     return;
   }
   const T* const w = static_cast<const T*>(a.w) + static_cast<int64_t>(t.group) * a.red * a.cols;
 
-  // what this lane stages
+  // what this lane stages of the rows: rows (threadIdx.x >> 3) + 32 i, the
+  // piece threadIdx.x & 7 of each stage.  A row that is not there is read as
+  // zeros, at one place all along (step 0).
+  const int ka = (threadIdx.x & 7) * VEC;
   const T* pa[PA];
-  bool oka[PA];
+  int step[PA];
 #pragma unroll
   for (int i = 0; i < PA; ++i) {
     const int r = (threadIdx.x >> 3) + 32 * i;
@@ -295,40 +303,82 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped(GroupedArgs a) {
       src = a.rows ? a.rows[t.begin + r] : t.begin + r;
       if (src >= a.n_x) src = -1;
     }
-    oka[i] = src >= 0;
-    pa[i] = x + (src < 0 ? 0 : src) * a.red;
+    step[i] = src >= 0 ? BK : 0;
+    pa[i] = src >= 0 ? x + src * a.red + ka : reinterpret_cast<const T*>(&g_zeros);
   }
-  const int ka = (threadIdx.x & 7) * VEC;
-  u32x4_t ra[PA], rb[PB];
-  auto request = [&](int64_t k0) {
-#pragma unroll
-    for (int i = 0; i < PA; ++i)
-      ra[i] = load_left<T, WHOLE>(pa[i] + k0 + ka, oka[i] ? a.red - k0 - ka : 0);
+  const int nk = (a.red + BK - 1) / BK, nstage = nk * ntile;
+  // and of the weights, from the stage's own place; columns past the last one
+  // are read as the last ones (nothing of them is stored)
+  uint32_t pb[PB];
+  auto weights_at = [&](int n0) {
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
       if constexpr (BT) {
-        const int64_t n = n0 + (threadIdx.x >> 3) + 32 * i;
-        rb[i] = load_left<T, WHOLE>(w + n * a.red + k0 + ka, n < a.cols ? a.red - k0 - ka : 0);
+        const int n = (threadIdx.x >> 3) + 32 * i;
+        pb[i] = static_cast<uint32_t>(n0 + n < a.cols ? n : 0) * a.red + ka;
       } else {
-        const int p = threadIdx.x + kThreads * i;
-        const int64_t k = k0 + p / TBk::PR, n = n0 + p % TBk::PR * VEC;
-        rb[i] = load_left<T, WHOLE>(w + k * a.cols + n, k < a.red ? a.cols - n : 0);
+        const int p = threadIdx.x + kThreads * i, n = p % TBk::PR * VEC;
+        pb[i] = static_cast<uint32_t>(p / TBk::PR) * a.cols + (n0 + n < a.cols ? n : 0);
       }
     }
   };
-  auto put = [&](int buf) {
+  u32x4_t ra[kDepth][PA], rb[kDepth][PB];
+  int rk = 0, rn = tile0 * BN;                     // the next stage to request
+  weights_at(rn);
+  auto request = [&](int d) {
+    if (WHOLE && rk + BK <= a.red) {
+#pragma unroll
+      for (int i = 0; i < PA; ++i) {
+        ra[d][i] = load_piece(pa[i]);
+        pa[i] += step[i];
+      }
+      const T* ws = BT ? w + static_cast<int64_t>(rn) * a.red + rk
+                       : w + static_cast<int64_t>(rk) * a.cols + rn;
+#pragma unroll
+      for (int i = 0; i < PB; ++i) rb[d][i] = load_piece(ws + pb[i]);
+    } else {
+      // the end of the reduction, or pieces that may be cut
+#pragma unroll
+      for (int i = 0; i < PA; ++i) {
+        ra[d][i] = load_left<T, WHOLE>(pa[i], step[i] ? a.red - rk - ka : 0);
+        pa[i] += step[i];
+      }
+#pragma unroll
+      for (int i = 0; i < PB; ++i) {
+        if constexpr (BT) {
+          const int n = rn + (threadIdx.x >> 3) + 32 * i;
+          rb[d][i] = load_left<T, WHOLE>(w + static_cast<int64_t>(n) * a.red + rk + ka,
+                                         n < a.cols ? a.red - rk - ka : 0);
+        } else {
+          const int p = threadIdx.x + kThreads * i;
+          const int k = rk + p / TBk::PR, n = rn + p % TBk::PR * VEC;
+          rb[d][i] = load_left<T, WHOLE>(w + static_cast<int64_t>(k) * a.cols + n,
+                                         k < a.red ? a.cols - n : 0);
+        }
+      }
+    }
+    rk += BK;
+    if (rk >= a.red) {                             // on to the next column tile
+      rk = 0;
+      rn += BN;
+#pragma unroll
+      for (int i = 0; i < PA; ++i) pa[i] -= static_cast<int64_t>(nk) * step[i];
+      weights_at(rn);
+    }
+  };
+  auto put = [&](int d, int buf) {
     u32x4_t* sa = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage);
     u32x4_t* sb = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage + TA::BYTES);
 #pragma unroll
     for (int i = 0; i < PA; ++i)
-      sa[TA::at((threadIdx.x >> 3) + 32 * i, threadIdx.x & 7)] = ra[i];
+      sa[TA::at((threadIdx.x >> 3) + 32 * i, threadIdx.x & 7)] = ra[d][i];
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
       if constexpr (BT) {
-        sb[TBr::at((threadIdx.x >> 3) + 32 * i, threadIdx.x & 7)] = rb[i];
+        sb[TBr::at((threadIdx.x >> 3) + 32 * i, threadIdx.x & 7)] = rb[d][i];
       } else {
         const int p = threadIdx.x + kThreads * i;
-        sb[TBk::at(p / TBk::PR, p % TBk::PR)] = rb[i];
+        sb[TBk::at(p / TBk::PR, p % TBk::PR)] = rb[d][i];
       }
     }
   };
@@ -336,59 +386,100 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped(GroupedArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int wr = (wave >> 1) * (BM / 2), wc = (wave & 1) * (BN / 2);
   f32x16 acc[FN][FM];
+  auto clear = [&] {
 #pragma unroll
-  for (int n = 0; n < FN; ++n)
+    for (int n = 0; n < FN; ++n)
 #pragma unroll
-    for (int m = 0; m < FM; ++m)
+      for (int m = 0; m < FM; ++m)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
-
-  const int64_t nk = (a.red + BK - 1ll) / BK;
-  request(0);
-  for (int64_t k = 0; k < nk; ++k) {
-    const int buf = static_cast<int>(k & 1);
-    put(buf);
-    __syncthreads();
-    if (k + 1 < nk) request((k + 1) * BK);
-    const u32x4_t* sa = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage);
-    const u32x4_t* sb = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage + TA::BYTES);
+        for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
+  };
+  // The tile's columns leave in parts of CW, FN / PARTS column blocks of each
+  // wave column, through one buffer.
+  constexpr int VO = Row<TO>::VEC;
+  constexpr int PARTS = BM * BN * static_cast<int>(sizeof(TO)) > kStage ? 2 : 1;
+  static_assert(FN % PARTS == 0 && BM * BN / PARTS * static_cast<int>(sizeof(TO)) <= kStage,
+                "a part of the tile fits a buffer");
+  constexpr int CW = BN / PARTS, HW = CW / 2;      // columns of a part; of a wave column's half
+  auto finish = [&](int n0, int buf) {
+    u32x4_t* so = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage);
+    const float* bias = a.bias ? a.bias + static_cast<int64_t>(t.group) * a.cols : nullptr;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      typename M::Frag fa[FM], fb[FN];
+    for (int part = 0; part < PARTS; ++part) {
+      if (part) __syncthreads();
 #pragma unroll
-      for (int m = 0; m < FM; ++m) fa[m] = TA::frag(sa, wr + 32 * m, s, lane);
+      for (int f = 0; f < FN / PARTS; ++f) {
+        const int n = part * (FN / PARTS) + f;
+        float b[16];
 #pragma unroll
-      for (int n = 0; n < FN; ++n) {
-        if constexpr (BT) fb[n] = TBr::frag(sb, wc + 32 * n, s, lane);
-        else fb[n] = TBk::frag(sb, wc + 32 * n, s, lane);
+        for (int i = 0; i < 16; ++i) b[i] = 0.0f;
+        if (bias) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int c = n0 + wc + 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+            b[i] = bias[c < a.cols ? c : 0];
+          }
+        }
+        block_to_lds<TO, CW, FM>(so, acc[n], wr, (wave & 1) * HW + 32 * f, b, a.relu);
       }
+      __syncthreads();
+      for (int p = threadIdx.x; p < BM * CW / VO; p += kThreads) {
+        const int r = p / (CW / VO), piece = p % (CW / VO), c = piece * VO;
+        const int col = n0 + (c / HW) * (BN / 2) + part * HW + c % HW, left = a.cols - col;
+        if (r >= nrow || left <= 0) continue;
+        const int64_t at = (t.begin + r) * a.cols + col;
+        u32x4_t u = so[out_at<TO, CW>(r, piece)];
+        if (a.mask) {
+          float v[VO], g[VO];
+          unpack(u, v);
+          unpack(load_left<TO, false>(static_cast<const TO*>(a.mask) + at, left), g);
 #pragma unroll
-      for (int n = 0; n < FN; ++n)
-#pragma unroll
-        for (int m = 0; m < FM; ++m) acc[n][m] = M::mma(fb[n], fa[m], acc[n][m]);
+          for (int i = 0; i < VO; ++i) v[i] = g[i] <= 0.0f ? 0.0f : v[i];
+          u = pack(v);
+        }
+        store_left(y + at, u, left);
+      }
     }
-  }
-  __syncthreads();
-  TO* so = reinterpret_cast<TO*>(s_buf);
-  const float* bias = a.bias ? a.bias + static_cast<int64_t>(t.group) * a.cols + n0 : nullptr;
-  tile_to_lds<TO, BM, BN, FM, FN>(so, acc, wr, wc, bias, a.cols - n0, a.relu);
-  __syncthreads();
-  constexpr int VO = Row<TO>::VEC, PO = BN / VO;
-  for (int p = threadIdx.x; p < BM * PO; p += kThreads) {
-    const int r = p / PO, piece = p % PO;
-    const int64_t left = a.cols - n0 - piece * VO;
-    if (r >= nrow || left <= 0) continue;
-    const int64_t at = (t.begin + r) * a.cols + n0 + piece * VO;
-    u32x4_t v = lds_piece<TO, BM, BN>(so, r, piece);
-    if (a.mask) {
-      float f[VO], g[VO];
-      unpack(v, f);
-      unpack(load_left<TO, false>(static_cast<const TO*>(a.mask) + at, left), g);
+    __syncthreads();
+  };
+
 #pragma unroll
-      for (int i = 0; i < VO; ++i) f[i] = g[i] <= 0.0f ? 0.0f : f[i];
-      v = pack(f);
+  for (int d = 0; d < kDepth; ++d)
+    if (d < nstage) request(d);
+  clear();
+  int k = 0, n0 = tile0 * BN;
+  for (int s0 = 0; s0 < nstage; s0 += kDepth) {
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) {
+      if (s0 + d >= nstage) break;
+      const int buf = d & 1;                       // (kDepth is even)
+      put(d, buf);
+      if (s0 + d + kDepth < nstage) request(d);
+      __syncthreads();
+      const u32x4_t* sa = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage);
+      const u32x4_t* sb = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage + TA::BYTES);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        typename M::Frag fa[FM], fb[FN];
+#pragma unroll
+        for (int m = 0; m < FM; ++m) fa[m] = TA::frag(sa, wr + 32 * m, s, lane);
+#pragma unroll
+        for (int n = 0; n < FN; ++n) {
+          if constexpr (BT) fb[n] = TBr::frag(sb, wc + 32 * n, s, lane);
+          else fb[n] = TBk::frag(sb, wc + 32 * n, s, lane);
+        }
+#pragma unroll
+        for (int n = 0; n < FN; ++n)
+#pragma unroll
+          for (int m = 0; m < FM; ++m) acc[n][m] = M::mma(fb[n], fa[m], acc[n][m]);
+      }
+      if (++k == nk) {
+        finish(n0, buf ^ 1);
+        clear();
+        k = 0;
+        n0 += BN;
+      }
     }
-    store_left(y + at, v, left);
   }
 }
 
@@ -414,12 +505,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_dw(WeightArgs a) {
   typedef Mma<T> M;
   typedef KTile<T, BC> TX;
   typedef KTile<T, BN> TY;
-  constexpr int VEC = Row<T>::VEC, BK = TX::BK, STEPS = BK / M::KS;
+  constexpr int VEC = Row<T>::VEC, BK = kBK<T>, STEPS = BK / M::KS, kDepth = 2;
   constexpr int FC = BC / 64, FN = BN / 64;
   constexpr int PX = TX::PIECES / kThreads, PY = TY::PIECES / kThreads;
-  constexpr int kStage = TX::BYTES + TY::BYTES, kOut = BC * BN * 4;
-  __shared__ __attribute__((aligned(16))) unsigned char
-      s_buf[2 * kStage > kOut ? 2 * kStage : kOut];
+  constexpr int kStage = TX::BYTES + TY::BYTES;
+  __shared__ __attribute__((aligned(16))) unsigned char s_buf[2 * kStage];
   const T *const x = static_cast<const T*>(a.x), *const dy = static_cast<const T*>(a.dy);
   const int64_t nc = (a.C_in + BC - 1) / BC, nn = (a.C_out + BN - 1) / BN;
   const int64_t id = die_order(blockIdx.x, gridDim.x);
@@ -434,39 +524,72 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_dw(WeightArgs a) {
     e = e < b ? b : e > a.m ? a.m : e;
     t = Tile{static_cast<int>(job), b, e, 0};
   }
-  u32x4_t rx[PX], ry[PY];
-  auto request = [&](int64_t j0) {
+  // The row numbers of kThreads positions at a time, three such runs in LDS: the
+  // one being requested, the next one, and the one a slower wave may still read.
+  __shared__ int32_t s_row[3][kThreads];
+  constexpr int RUN = kThreads / BK;               // stages of a run
+  auto row_of = [&](int64_t j) {
+    return j >= t.end ? -1 : a.rows ? a.rows[j] : static_cast<int32_t>(j);
+  };
+  int64_t rj = t.begin;                            // the next stage to request
+  int rq = 0, run = 0;                             // its place in its run, its run (mod 3)
+  s_row[0][threadIdx.x] = row_of(rj + threadIdx.x);
+  int32_t row_next = row_of(rj + kThreads + threadIdx.x);
+  __syncthreads();
+  u32x4_t rx[kDepth][PX], ry[kDepth][PY];
+  uint32_t py[PY];
+#pragma unroll
+  for (int i = 0; i < PY; ++i) {
+    const int p = threadIdx.x + kThreads * i, n = p % TY::PR * VEC;
+    py[i] = static_cast<uint32_t>(p / TY::PR) * a.C_out + (n0 + n < a.C_out ? n : 0);
+  }
+  auto request = [&](int d) {
 #pragma unroll
     for (int i = 0; i < PX; ++i) {
       const int p = threadIdx.x + kThreads * i;
-      const int64_t j = j0 + p / TX::PR, c = c0 + p % TX::PR * VEC;
-      int64_t src = -1;
-      if (j < t.end) {
-        src = a.rows ? a.rows[j] : j;
-        if (src >= a.n_x) src = -1;
-      }
-      rx[i] = load_left<T, WHOLE>(x + (src < 0 ? 0 : src) * a.C_in + c,
-                                  src >= 0 ? a.C_in - c : 0);
+      const int32_t row = s_row[run][rq * BK + p / TX::PR];
+      const int64_t c = c0 + p % TX::PR * VEC;
+      const bool ok = row >= 0 && row < a.n_x;
+      rx[d][i] = load_left<T, WHOLE>(x + static_cast<int64_t>(row) * a.C_in + c,
+                                     ok ? a.C_in - c : 0);
     }
+    if (WHOLE && rj + BK <= t.end) {
+      // (columns past the last one are read as others: nothing of them is stored)
+      const T* ys = dy + rj * a.C_out + n0;
 #pragma unroll
-    for (int i = 0; i < PY; ++i) {
-      const int p = threadIdx.x + kThreads * i;
-      const int64_t j = j0 + p / TY::PR, n = n0 + p % TY::PR * VEC;
-      ry[i] = load_left<T, WHOLE>(dy + j * a.C_out + n, j < t.end ? a.C_out - n : 0);
+      for (int i = 0; i < PY; ++i) ry[d][i] = load_piece(ys + py[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PY; ++i) {
+        const int p = threadIdx.x + kThreads * i;
+        const int64_t j = rj + p / TY::PR, n = n0 + p % TY::PR * VEC;
+        ry[d][i] = load_left<T, WHOLE>(dy + j * a.C_out + n, j < t.end ? a.C_out - n : 0);
+      }
+    }
+    if (rq == 0) {
+      // (read from the next stage but RUN - 1 on, with barriers between)
+      const int to = run == 2 ? 0 : run + 1;
+      s_row[to][threadIdx.x] = row_next;
+      row_next = row_of(rj + 2 * kThreads + threadIdx.x);
+    }
+    rj += BK;
+    if (++rq == RUN) {
+      rq = 0;
+      run = run == 2 ? 0 : run + 1;
     }
   };
-  auto put = [&](int buf) {
+  auto put = [&](int d, int buf) {
     u32x4_t* sx = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage);
     u32x4_t* sy = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage + TX::BYTES);
 #pragma unroll
     for (int i = 0; i < PX; ++i) {
       const int p = threadIdx.x + kThreads * i;
-      sx[TX::at(p / TX::PR, p % TX::PR)] = rx[i];
+      sx[TX::at(p / TX::PR, p % TX::PR)] = rx[d][i];
     }
 #pragma unroll
     for (int i = 0; i < PY; ++i) {
       const int p = threadIdx.x + kThreads * i;
-      sy[TY::at(p / TY::PR, p % TY::PR)] = ry[i];
+      sy[TY::at(p / TY::PR, p % TY::PR)] = ry[d][i];
     }
   };
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -482,28 +605,34 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_dw(WeightArgs a) {
       for (int m = 0; m < FC; ++m) acc[n][m][i] = 0.0f;
     }
   const int64_t nk = (t.end - t.begin + BK - 1) / BK;
-  if (nk) request(t.begin);
-  for (int64_t k = 0; k < nk; ++k) {
-    const int buf = static_cast<int>(k & 1);
-    put(buf);
-    __syncthreads();
-    if (k + 1 < nk) request(t.begin + (k + 1) * BK);
-    const u32x4_t* sx = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage);
-    const u32x4_t* sy = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage + TX::BYTES);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      typename M::Frag fx[FC], fy[FN];
+  for (int d = 0; d < kDepth; ++d)
+    if (d < nk) request(d);
+  for (int64_t k0 = 0; k0 < nk; k0 += kDepth) {
 #pragma unroll
-      for (int m = 0; m < FC; ++m) fx[m] = TX::frag(sx, wr + 32 * m, s, lane);
+    for (int d = 0; d < kDepth; ++d) {
+      if (k0 + d >= nk) break;
+      const int buf = d & 1;
+      put(d, buf);
+      if (k0 + d + kDepth < nk) request(d);
+      __syncthreads();
+      const u32x4_t* sx = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage);
+      const u32x4_t* sy = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage + TX::BYTES);
 #pragma unroll
-      for (int n = 0; n < FN; ++n) fy[n] = TY::frag(sy, wc + 32 * n, s, lane);
+      for (int s = 0; s < STEPS; ++s) {
+        typename M::Frag fx[FC], fy[FN];
 #pragma unroll
-      for (int n = 0; n < FN; ++n)
+        for (int m = 0; m < FC; ++m) fx[m] = TX::frag(sx, wr + 32 * m, s, lane);
 #pragma unroll
-        for (int m = 0; m < FC; ++m) acc[n][m] = M::mma(fy[n], fx[m], acc[n][m]);
-      if (bias) {
+        for (int n = 0; n < FN; ++n) fy[n] = TY::frag(sy, wc + 32 * n, s, lane);
 #pragma unroll
-        for (int n = 0; n < FN; ++n) accb[n] = M::mma(fy[n], M::ones(), accb[n]);
+        for (int n = 0; n < FN; ++n)
+#pragma unroll
+          for (int m = 0; m < FC; ++m) acc[n][m] = M::mma(fy[n], fx[m], acc[n][m]);
+        if (bias) {
+#pragma unroll
+          for (int n = 0; n < FN; ++n) accb[n] = M::mma(fy[n], M::ones(), accb[n]);
+        }
       }
     }
   }
@@ -517,19 +646,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_dw(WeightArgs a) {
         if (col < a.C_out) a.db[job * a.C_out + col] = accb[n][i];
       }
   }
-  __syncthreads();
-  float* so = reinterpret_cast<float*>(s_buf);
-  tile_to_lds<float, BC, BN, FC, FN>(so, acc, wr, wc, nullptr, 0, 0);
-  __syncthreads();
   float* out = a.dw + job * a.C_in * a.C_out;
-  constexpr int PO = BN / 4;
-  for (int p = threadIdx.x; p < BC * PO; p += kThreads) {
-    const int r = p / PO, piece = p % PO;
-    const int64_t left = a.C_out - n0 - piece * 4;
-    if (c0 + r >= a.C_in || left <= 0) continue;
-    store_left(out + (c0 + r) * a.C_out + n0 + piece * 4, lds_piece<float, BC, BN>(so, r, piece),
-               left);
-  }
+#pragma unroll
+  for (int n = 0; n < FN; ++n)
+#pragma unroll
+    for (int m = 0; m < FC; ++m) {
+      const int64_t r = c0 + wr + 32 * m + (lane & 31);
+      if (r >= a.C_in) continue;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t c = n0 + wc + 32 * n + 8 * q + 4 * (lane >> 5);
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = acc[n][m][4 * q + i];
+        if (c < a.C_out) store_left(out + r * a.C_out + c, pack(v), a.C_out - c);
+      }
+    }
 }
 
 // The chunks' sums of a group, in ascending order: dw | db of one group as a
@@ -611,8 +743,13 @@ inline int64_t tile_bound(int64_t m, int64_t groups, int64_t BM) {
   return m / BM + (groups < m ? groups : m);
 }
 
-template <typename T, typename TO, bool BT, int BM, int BN> int run_tile(const GroupedArgs& a) {
-  const int64_t blocks = tile_bound(a.m, a.E + 1, BM) * ((a.cols + BN - 1) / BN);
+template <typename T, typename TO, bool BT, int BM, int BN> int run_tile(GroupedArgs a) {
+  const int64_t tiles = tile_bound(a.m, a.E + 1, BM), ncol = (a.cols + BN - 1) / BN;
+  // longer strips while they leave four workgroups a compute unit
+  int64_t strip = tiles * ncol / 1024;
+  strip = strip < 1 ? 1 : strip > ncol ? ncol : strip;
+  a.strip = static_cast<int>(strip);
+  const int64_t blocks = tiles * ((ncol + strip - 1) / strip);
   if (blocks > 0x7fffffff) return SPCONV_EINVAL;
   const bool whole = a.red % Row<T>::VEC == 0 && (BT || a.cols % Row<T>::VEC == 0);
   if (whole)
@@ -643,8 +780,8 @@ template <typename T, int BC, int BN> void run_dw(const WeightArgs& a, int64_t j
 }
 
 bool sizes_ok(int64_t m, int E, int C_in, int C_out) {
-  return rows_ok(m) && E >= 1 && E <= 65535 && C_in >= 1 && C_out >= 1 && C_in <= (1 << 24) &&
-         C_out <= (1 << 24);
+  return rows_ok(m) && E >= 1 && E <= 65535 && C_in >= 1 && C_out >= 1 && C_in <= (1 << 23) &&
+         C_out <= (1 << 23);
 }
 
 }  // namespace
@@ -666,7 +803,7 @@ extern "C" int spconv_grouped_forward(int in_dt, const void* x, int64_t n_x, con
   if (m == 0) return SPCONV_OK;
   return run_types<false>(in_dt, out_dt,
                           GroupedArgs{x, n_x, w, offsets, rows, bias, nullptr, relu, y, m, E, C_in,
-                                      C_out, static_cast<hipStream_t>(stream)});
+                                      C_out, 1, static_cast<hipStream_t>(stream)});
 }
 
 extern "C" int spconv_grouped_backward_data(int dt, const void* dy, const void* w,
@@ -681,7 +818,7 @@ extern "C" int spconv_grouped_backward_data(int dt, const void* dy, const void* 
   if (m == 0) return SPCONV_OK;
   return run_types<true>(dt, out_dt,
                          GroupedArgs{dy, m, w, offsets, nullptr, nullptr, mask, 0, dx, m, E, C_out,
-                                     C_in, static_cast<hipStream_t>(stream)});
+                                     C_in, 1, static_cast<hipStream_t>(stream)});
 }
 
 extern "C" int spconv_grouped_backward_weight_workspace(int dt, int64_t m, int E, int C_in,
