@@ -58,11 +58,16 @@ __device__ __forceinline__ u32x4_t pack(const float (&v)[4]) {
   for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(v[i]);
   return u;
 }
+// Two values rounded to bf16 by one instruction.
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), b2));
+}
 __device__ __forceinline__ u32x4_t pack(const float (&v)[8]) {
   u32x4_t u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    u[i] = Row<bf16_t>::put(v[2 * i]) | static_cast<uint32_t>(Row<bf16_t>::put(v[2 * i + 1])) << 16;
+  for (int i = 0; i < 4; ++i) u[i] = pack2(v[2 * i], v[2 * i + 1]);
   return u;
 }
 

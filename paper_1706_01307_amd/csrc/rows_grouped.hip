@@ -4,6 +4,8 @@
 // Which rows a workgroup has is found on the device: the groups' row tiles are
 // numbered in order, and each wave finds the tile's group by a running sum over
 // the offsets, 64 groups at a time.  No host knows the group sizes.
+#include <type_traits>
+
 #include "rows.h"
 
 namespace spc {
@@ -85,12 +87,6 @@ template <> struct Mma<bf16_t> {
   __device__ static f32x16 mma(Frag a, Frag b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
-  __device__ static Frag ones() {
-    Frag f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = static_cast<__bf16>(1.0f);
-    return f;
-  }
 };
 template <> struct Mma<float> {
   static constexpr int KS = 8;
@@ -100,33 +96,53 @@ template <> struct Mma<float> {
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
     return c;
   }
-  __device__ static Frag ones() { return Frag{1.0f, 1.0f, 1.0f, 1.0f}; }
 };
 
-// Staged tiles in LDS, in 16-byte pieces: a stage is 128 bytes of the reduction
-// (BK elements), so that a row's load is a whole cache line (with 64 bytes the
-// address unit took 55 cycles an instruction instead of 17 and bounded both
-// kernels).
+// Staged tiles in LDS, in 16-byte pieces; a stage is KB bytes of the reduction,
+// BK elements.
 //
-// RTile: R rows of BK elements.  A fragment read takes one piece column of 16
-// rows per cycle, so pieces are permuted by the row's bits 1 to 3: 16 rows then
-// cover the 64 banks once.
-template <typename T> constexpr int kBK = 128 / static_cast<int>(sizeof(T));
-template <typename T, int R> struct RTile {
-  static constexpr int PIECES = R * 8, BYTES = R * 128;
-  __device__ static int at(int row, int piece) { return row * 8 + (piece ^ ((row >> 1) & 7)); }
-  // rows r0..r0+31, reduction from piece 2 s
-  __device__ static typename Mma<T>::Frag frag(const u32x4_t* t, int r0, int s, int lane) {
-    return __builtin_bit_cast(typename Mma<T>::Frag, t[at(r0 + (lane & 31), 2 * s + (lane >> 5))]);
+// RTile: R rows of KB bytes.  A fragment read takes one piece column of 16 rows
+// per cycle, so pieces are permuted by the row: 16 rows then cover the 64 banks
+// once.
+template <typename T, int KB> constexpr int kBK = KB / static_cast<int>(sizeof(T));
+
+// A lane's place in a tile, for reads at constant distances from it: hidden from
+// the compiler, which would otherwise keep every sum with a tile's address and
+// step in a register of its own.
+__device__ __forceinline__ int lane_place(int byte) {
+  asm volatile("" : "+v"(byte));
+  return byte;
+}
+template <typename V> __device__ __forceinline__ V lds_at(const u32x4_t* t, int byte) {
+  return *reinterpret_cast<const V*>(reinterpret_cast<const char*>(t) + byte);
+}
+
+template <typename T, int R, int KB> struct RTile {
+  static constexpr int PR = KB / 16;               // pieces per row
+  static constexpr int PIECES = R * PR, STEPS = PR / 2;
+  __device__ static int at(int row, int piece) {
+    return row * PR + (piece ^ (KB == 128 ? (row >> 1) & 7 : (row >> 2) & 3));
   }
+  // fragments of rows r0 + 32 b .. + 31, the reduction's step s (pieces 2 s, 2 s + 1)
+  struct Reader {
+    int place[STEPS];
+    __device__ Reader(int r0, int lane) {
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+        place[s] = lane_place(at(r0 + (lane & 31), 2 * s + (lane >> 5)) * 16);
+    }
+    __device__ typename Mma<T>::Frag operator()(const u32x4_t* t, int b, int s) const {
+      return lds_at<typename Mma<T>::Frag>(t, place[s] + b * 32 * KB);
+    }
+  };
 };
 // KTile: BK rows of the reduction of W columns each; fragments are read across
 // the rows.  bf16: LDS reads that transpose 4 x 16 blocks; 64-byte spans of four
 // rows must lie in different banks.  fp32: one element a lane; the two halves of
 // a wave read rows 4 apart.
-template <typename T, int W> struct KTile {
+template <typename T, int W, int KB> struct KTile {
   static constexpr int VEC = Row<T>::VEC, PR = W / VEC;   // pieces per row
-  static constexpr int PIECES = kBK<T> * PR, BYTES = PIECES * 16;
+  static constexpr int PIECES = kBK<T, KB> * PR;
   __device__ static int at(int k, int piece) {
     if constexpr (sizeof(T) == 2) {
       const int x = W >= 128 ? (k & 3) << 2 : W == 64 ? ((k >> 1) & 1) << 2 : 0;
@@ -135,31 +151,43 @@ template <typename T, int W> struct KTile {
       return k * PR + (piece ^ (W >= 64 ? ((k >> 2) & 1) << 3 : 0));
     }
   }
-  // columns c0..c0+31, reduction from row KS * s
-  __device__ static typename Mma<T>::Frag frag(const u32x4_t* t, int c0, int s, int lane) {
-    if constexpr (sizeof(T) == 2) {
-      // lanes 16 q + j ask for row 8 (q / 2) + j / 4, columns 16 (q % 2) + 4 (j % 4) .. + 3,
-      // and receive column lane % 32 of rows 8 (lane / 32) .. + 3
-      const int j = lane & 15, q = lane >> 4;
-      const int row = 16 * s + 8 * (q >> 1) + (j >> 2), col = c0 + 16 * (q & 1) + 4 * (j & 3);
-      typedef __attribute__((address_space(3))) s16x4 lds_s4;
-      const uint16_t* b = reinterpret_cast<const uint16_t*>(t);
-      lds_s4* lo = (lds_s4*)(const_cast<uint16_t*>(b) + at(row, col >> 3) * 8 + (col & 7));
-      lds_s4* hi = (lds_s4*)(const_cast<uint16_t*>(b) + at(row + 4, col >> 3) * 8 + (col & 7));
-      const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lo);
-      const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(hi);
-      const s16x8 r = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-      return __builtin_bit_cast(bf16x8, r);
-    } else {
-      const float* b = reinterpret_cast<const float*>(t);
-      const int col = c0 + (lane & 31);
-      f32x4_t f;
+  // fragments of columns c0 + B b .. + 31 (b < NB), the reduction's step s
+  template <int B, int NB> struct Reader {
+    int place[NB];
+    __device__ Reader(int c0, int lane) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        f[i] = b[at(8 * s + 4 * (lane >> 5) + i, col >> 2) * 4 + (col & 3)];
-      return f;
+      for (int b = 0; b < NB; ++b) {
+        if constexpr (sizeof(T) == 2) {
+          // lanes 16 q + j ask for row 8 (q / 2) + j / 4, columns 16 (q % 2) + 4 (j % 4) .. + 3,
+          // and receive column lane % 32 of rows 8 (lane / 32) .. + 3
+          const int j = lane & 15, q = lane >> 4;
+          const int row = 8 * (q >> 1) + (j >> 2), col = c0 + B * b + 16 * (q & 1) + 4 * (j & 3);
+          place[b] = lane_place(at(row, col >> 3) * 16 + (col & 7) * 2);
+        } else {
+          const int col = c0 + B * b + (lane & 31);
+          place[b] = lane_place(at(4 * (lane >> 5), col >> 2) * 16 + (col & 3) * 4);
+        }
+      }
     }
-  }
+    __device__ typename Mma<T>::Frag operator()(const u32x4_t* t, int b, int s) const {
+      const int at = place[b] + s * Mma<T>::KS * PR * 16;
+      if constexpr (sizeof(T) == 2) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s4;
+        const char* p = reinterpret_cast<const char*>(t) + at;
+        lds_s4* lo = (lds_s4*)(const_cast<char*>(p));
+        lds_s4* hi = (lds_s4*)(const_cast<char*>(p) + 4 * PR * 16);
+        const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lo);
+        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(hi);
+        const s16x8 r = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+        return __builtin_bit_cast(bf16x8, r);
+      } else {
+        f32x4_t f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = lds_at<float>(t, at + i * PR * 16);
+        return f;
+      }
+    }
+  };
 };
 
 // What a lane reads where there is nothing to read: a load that always happens
@@ -200,36 +228,31 @@ __device__ __forceinline__ void store_left(TO* p, u32x4_t v, int64_t left) {
   }
 }
 
-// A wave's FM blocks of 32 x 32 of one column block go to LDS, rounded, as rows
-// of CW columns (the first operand's rows are the columns: a lane has 4 adjacent
-// ones of one row in every four registers).  Pieces are permuted by the row, so
+// 16 bytes a lane from global memory (16-byte aligned) straight to LDS: lane i's
+// go to l + 16 i, l the same for the whole wave.  They are read behind a
+// stage_barrier().
+__device__ __forceinline__ void load_to_lds(const void* g, u32x4_t* l) {
+  typedef __attribute__((address_space(3))) void lds_void;
+  typedef __attribute__((address_space(1))) const void global_void;
+  __builtin_amdgcn_global_load_lds((global_void*)g, (lds_void*)l, 16, 0, 0);
+}
+// The barrier of a ring of stages: every wave waits for its own loads, all but the
+// LATER last ones (those of later stages), and for its LDS reads.  Behind it this
+// stage is in LDS and the buffer of the one before is free.  (__syncthreads would
+// wait for all loads.)
+template <int LATER> __device__ __forceinline__ void stage_barrier() {
+  asm volatile("" ::: "memory");
+  // vmcnt(LATER), lgkmcnt(0)
+  __builtin_amdgcn_s_waitcnt(0x0070 | (LATER & 15) | (LATER >> 4) << 14);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Finished rows in LDS as rows of CW columns; pieces are permuted by the row, so
 // that the 32 rows of a write and the rows of a read lie in different banks.
 template <typename TO, int CW> __device__ __forceinline__ int out_at(int r, int piece) {
   constexpr int PR = CW / Row<TO>::VEC;
   return r * PR + (piece ^ (r & (PR - 1)));
-}
-template <typename TO, int CW, int FM>
-__device__ __forceinline__ void block_to_lds(u32x4_t* s, const f32x16 (&acc)[FM], int r0, int c0,
-                                             const float (&bias)[16], int relu) {
-  constexpr int VO = Row<TO>::VEC;
-  const int lane = threadIdx.x & 63, h = lane >> 5;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int c = c0 + 8 * q + 4 * h;
-#pragma unroll
-    for (int m = 0; m < FM; ++m) {
-      const int r = r0 + 32 * m + (lane & 31);
-      TO v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float z = acc[m][4 * q + i] + bias[4 * q + i];
-        if (relu && z < 0.0f) z = 0.0f;
-        v[i] = Row<TO>::put(z);
-      }
-      TO* d = reinterpret_cast<TO*>(s + out_at<TO, CW>(r, c / VO)) + c % VO;
-      __builtin_memcpy(__builtin_assume_aligned(d, 4 * sizeof(TO)), v, sizeof v);
-    }
-  }
 }
 
 struct GroupedArgs {
@@ -244,250 +267,600 @@ struct GroupedArgs {
   void* y;                     // [m][cols]
   int64_t m;
   int E, red, cols;            // reduction, output columns
-  int strip;                   // column tiles a workgroup takes
   hipStream_t st;
 };
 
-// Rows x weights: BT false: w[e] is [red][cols] (the forward), BT true: w[e] is
-// [cols][red] (the input gradient).  A workgroup takes BM positions of a group
-// and `strip` column tiles of BN one after the other, four waves in 2 x 2.  Its
-// stages (128 bytes of the reduction of one column tile) run on across the
-// column tiles: the next kDepth stages' pieces are on their way into registers
-// while one, in LDS, is multiplied; two LDS buffers, one barrier a stage.  A
-// finished tile leaves through the buffer that is free then, as whole rows (in
-// 32-byte parts of rows, stored from the registers, the forward wrote 1.8 times
-// its bytes to memory).
-template <typename T, typename TO, bool BT, int BM, int BN, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 2) void k_grouped(GroupedArgs a) {
+// A stage's products of a wave: FM x FN blocks.  (Fragments read a step ahead into
+// a second set of registers, with or without an order given to the scheduler,
+// were no faster: the two waves a SIMD has take turns.)
+template <typename T, int KB, int FM, int FN, typename LoadA, typename LoadB>
+__device__ __forceinline__ void multiply_stage(f32x16 (&acc)[FN][FM], LoadA la, LoadB lb) {
   typedef Mma<T> M;
-  typedef RTile<T, BM> TA;
-  typedef RTile<T, BN> TBr;
-  typedef KTile<T, BN> TBk;
-  constexpr int VEC = Row<T>::VEC, BK = kBK<T>, STEPS = BK / M::KS, kDepth = 2;
-  constexpr int FM = BM / 64, FN = BN / 64;
-  constexpr int PA = TA::PIECES / kThreads;
-  constexpr int PB = TBk::PIECES / kThreads;       // (as many as TBr's)
-  constexpr int kStage = TA::BYTES + TBk::BYTES;
-  __shared__ __attribute__((aligned(16))) unsigned char s_buf[2 * kStage];
-  const T* const x = static_cast<const T*>(a.x);
-  TO* const y = static_cast<TO*>(a.y);
-  const int ncol = (a.cols + BN - 1) / BN, nstrip = (ncol + a.strip - 1) / a.strip;
-  const int64_t id = die_order(blockIdx.x, gridDim.x);
-  const Tile t = find_tile<true>(a.offsets, a.E, a.m, BM, id / nstrip);
-  if (t.group < 0) return;
-  const int tile0 = static_cast<int>(id % nstrip) * a.strip;
-  const int ntile = ncol - tile0 < a.strip ? ncol - tile0 : a.strip;
-  const int nrow = static_cast<int>(t.end - t.begin);
-  if (t.group == a.E) {                            // behind the last group
-    const int64_t c0 = static_cast<int64_t>(tile0) * BN;
-    const int64_t c1 = c0 + static_cast<int64_t>(ntile) * BN;
-    const int64_t end = c1 < a.cols ? c1 : a.cols;
-    for (int r = 0; r < nrow; ++r)
-      for (int64_t c = c0 + threadIdx.x; c < end; c += kThreads)
-        y[(t.begin + r) * a.cols + c] = Row<TO>::put(0.0f);
-    return;
+#pragma unroll
+  for (int q = 0; q < kBK<T, KB> / M::KS; ++q) {
+    typename M::Frag fa[FM], fb[FN];
+#pragma unroll
+    for (int m = 0; m < FM; ++m) fa[m] = la(m, q);
+#pragma unroll
+    for (int n = 0; n < FN; ++n) fb[n] = lb(n, q);
+#pragma unroll
+    for (int n = 0; n < FN; ++n)
+#pragma unroll
+      for (int m = 0; m < FM; ++m) acc[n][m] = M::mma(fb[n], fa[m], acc[n][m]);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  const T* const w = static_cast<const T*>(a.w) + static_cast<int64_t>(t.group) * a.red * a.cols;
+}
 
-  // what this lane stages of the rows: rows (threadIdx.x >> 3) + 32 i, the
-  // piece threadIdx.x & 7 of each stage.  A row that is not there is read as
-  // zeros, at one place all along (step 0).
-  const int ka = (threadIdx.x & 7) * VEC;
+// What a workgroup of the products has to do: `nrow` positions from `begin` of a
+// group, the columns from n0.
+struct Job {
+  int group, nrow, n0;
+  int64_t begin;
+};
+// Workgroup -> job, `span` columns each.  False: nothing (or only zeros, written
+// here).
+template <typename TO, int BM>
+__device__ __forceinline__ bool grouped_job(const GroupedArgs& a, int span, Job* j) {
+  const int nspan = (a.cols + span - 1) / span;
+  const int64_t id = die_order(blockIdx.x, gridDim.x);
+  const Tile t = find_tile<true>(a.offsets, a.E, a.m, BM, id / nspan);
+  if (t.group < 0) return false;
+  j->group = t.group;
+  j->begin = t.begin;
+  j->nrow = static_cast<int>(t.end - t.begin);
+  j->n0 = static_cast<int>(id % nspan) * span;
+  if (t.group < a.E) return true;
+  // behind the last group
+  const int end = a.cols - j->n0 < span ? a.cols : j->n0 + span;
+  TO* y = static_cast<TO*>(a.y);
+  for (int r = 0; r < j->nrow; ++r)
+    for (int c = j->n0 + threadIdx.x; c < end; c += blockDim.x)
+      y[(t.begin + r) * a.cols + c] = Row<TO>::put(0.0f);
+  return false;
+}
+// The row that position `begin + r` reads, -1 for a row of zeros.
+__device__ __forceinline__ int64_t source_row(const GroupedArgs& a, const Job& j, int r) {
+  if (r >= j.nrow) return -1;
+  const int64_t src = a.rows ? a.rows[j.begin + r] : j.begin + r;
+  return src < a.n_x ? src : -1;
+}
+
+// The bias of columns n0 .. n0 + N, zeros without one, in LDS before a tile is
+// finished (a load then would wait for every load in flight).
+template <int N>
+__device__ __forceinline__ void load_bias(const GroupedArgs& a, const Job& j, int n0,
+                                          float* s_bias) {
+  const float* b = a.bias ? a.bias + static_cast<int64_t>(j.group) * a.cols : nullptr;
+  for (int c = threadIdx.x; c < N; c += blockDim.x)
+    s_bias[c] = b && n0 + c < a.cols ? b[n0 + c] : 0.0f;
+}
+
+// Where a wave's column block n starts: the blocks of a tile's waves lie side by
+// side, so that a part of the finished tile is of adjacent columns.
+template <int WC> __device__ __forceinline__ int col_of(int wcol, int n) {
+  return 32 * (wcol + WC * n);
+}
+
+__device__ __forceinline__ void put4(float* d, const float (&v)[4]) {
+  *reinterpret_cast<float4*>(d) = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void put4(bf16_t* d, const float (&v)[4]) {
+  *reinterpret_cast<uint2*>(d) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+}
+
+// The finished tile of a workgroup of WR x WC waves, FM x FN blocks each, leaves
+// through LDS as whole rows, in parts that fit `lds` (BYTES): FNP column and FMP
+// row blocks of every wave at a time.  A barrier before and within each part.
+template <typename TO, int BM, int BN, int WR, int WC, int BYTES>
+__device__ __forceinline__ void store_tile_rows(
+    u32x4_t* lds, const f32x16 (&acc)[BN / WC / 32][BM / WR / 32], const float* s_bias,
+    const GroupedArgs& a, const Job& j, int n0) {
+  constexpr int FM = BM / WR / 32, FN = BN / WC / 32, VO = Row<TO>::VEC;
+  constexpr int TOB = static_cast<int>(sizeof(TO));
+  constexpr int FNP = BM * BN * TOB <= BYTES ? FN : 1;
+  constexpr int CW = WC * 32 * FNP;                // columns of a part
+  constexpr int FMP = BM * CW * TOB <= BYTES ? FM : BM * CW * TOB <= 2 * BYTES ? FM / 2 : FM / 4;
+  constexpr int RW = WR * 32 * FMP;                // rows of a part
+  static_assert(FMP >= 1 && RW * CW * TOB <= BYTES, "a part fits the buffer");
+  constexpr int NT = 64 * WR * WC, PR = CW / VO, NPC = RW * PR / NT;
+  constexpr int NB = NPC < 4 ? NPC : 4;            // pieces a lane stores together
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
+  const int wrow = wave / WC, wcol = wave % WC;
+  TO* const y = static_cast<TO*>(a.y);
+  const TO* const mask = static_cast<const TO*>(a.mask);
+#pragma unroll
+  for (int np = 0; np < FN; np += FNP)
+#pragma unroll
+    for (int mp = 0; mp < FM; mp += FMP) {
+      __syncthreads();
+      auto write = [&](auto relu) {
+#pragma unroll
+        for (int f = 0; f < FNP; ++f)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            // 4 adjacent columns of one row in every four registers of a lane
+            const int c = col_of<WC>(wcol, f) + 8 * q + 4 * h;
+            const float4 b = *reinterpret_cast<const float4*>(s_bias + WC * 32 * np + c);
+            const float bias[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int m = 0; m < FMP; ++m) {
+              const int r = wrow * 32 * FMP + 32 * m + (lane & 31);
+              float v[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                v[i] = acc[np + f][mp + m][4 * q + i] + bias[i];
+                if (relu.value) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+              }
+              put4(reinterpret_cast<TO*>(lds + out_at<TO, CW>(r, c / VO)) + c % VO, v);
+            }
+          }
+      };
+      if (a.relu) write(std::true_type{}); else write(std::false_type{});
+      __syncthreads();
+      for (int p0 = threadIdx.x; p0 < RW * PR; p0 += NT * NB) {
+        int64_t at[NB];
+        int left[NB];
+        u32x4_t g[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const int p = p0 + NT * i, lr = p / PR;
+          const int r = lr / (32 * FMP) * (BM / WR) + 32 * mp + lr % (32 * FMP);
+          const int col = n0 + WC * 32 * np + p % PR * VO;
+          left[i] = r < j.nrow ? a.cols - col : 0;
+          at[i] = (j.begin + r) * a.cols + col;
+        }
+        if (mask) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i)
+            g[i] = left[i] >= VO || left[i] <= 0 ? load_left<TO, true>(mask + at[i], left[i])
+                                                 : load_left<TO, false>(mask + at[i], left[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          if (left[i] <= 0) continue;
+          const int p = p0 + NT * i;
+          u32x4_t u = lds[out_at<TO, CW>(p / PR, p % PR)];
+          if (mask) {
+            float v[VO], z[VO];
+            unpack(u, v);
+            unpack(g[i], z);
+#pragma unroll
+            for (int e = 0; e < VO; ++e) v[e] = z[e] <= 0.0f ? 0.0f : v[e];
+            u = pack(v);
+          }
+          store_left(y + at[i], u, left[i]);
+        }
+      }
+    }
+}
+
+// Rows x weights: BT false: w[e] is [red][cols] (the forward), BT true: w[e] is
+// [cols][red] (the input gradient).  A workgroup of WR x WC waves takes a tile of
+// BM positions by BN columns, in stages of 64 bytes of the reduction through a
+// ring of four LDS buffers: three stages are on their way while one is multiplied,
+// one barrier a stage.  Whole 16-byte pieces at aligned addresses only
+// (k_grouped_any takes the others).
+template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped(GroupedArgs a) {
+  constexpr int KB = 64, kRing = 4;
+  typedef RTile<T, BM, KB> TA;
+  typedef RTile<T, BN, KB> TBr;
+  typedef KTile<T, BN, KB> TBk;
+  constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = 64 * WR * WC;
+  constexpr int FM = BM / WR / 32, FN = BN / WC / 32;
+  constexpr int PA = TA::PIECES / NT, PB = TBk::PIECES / NT;   // (as many as TBr's)
+  constexpr int NP = TA::PIECES + TBk::PIECES;
+  static_assert(NT % 256 == 0, "a lane's pieces of a stage have one place in their rows");
+  // (the first one also takes the finished tile; separate arrays, so that the
+  // compiler knows which loads a read waits for)
+  constexpr int kOut = BM * BN * static_cast<int>(sizeof(TO)) / 16;
+  constexpr int NP0 = kOut > NP && BM * BN <= 128 * 128 ? (kOut > 2 * NP ? 2 * NP : kOut) : NP;
+  __shared__ u32x4_t s_buf0[NP0], s_buf1[NP], s_buf2[NP], s_buf3[NP];
+  __shared__ __attribute__((aligned(16))) float s_bias[BN];
+  const T* const x = static_cast<const T*>(a.x);
+  Job j;
+  if (!grouped_job<TO, BM>(a, BN, &j)) return;
+  const T* const w = static_cast<const T*>(a.w) + static_cast<int64_t>(j.group) * a.red * a.cols;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  load_bias<BN>(a, j, j.n0, s_bias);
+
+  // What this lane stages of the rows: rows ra0 + NT / PR * i, of each the piece
+  // that belongs at its place in LDS.  A row that is not there is read as zeros,
+  // at one place all along (step 0).
+  constexpr int PR = TA::PR;
+  const T* const zero = reinterpret_cast<const T*>(&g_zeros);
+  const int ra0 = threadIdx.x / PR, ka = (TA::at(ra0, threadIdx.x % PR) - ra0 * PR) * VEC;
   const T* pa[PA];
   int step[PA];
 #pragma unroll
   for (int i = 0; i < PA; ++i) {
-    const int r = (threadIdx.x >> 3) + 32 * i;
-    int64_t src = -1;
-    if (r < nrow) {
-      src = a.rows ? a.rows[t.begin + r] : t.begin + r;
-      if (src >= a.n_x) src = -1;
-    }
+    const int64_t src = source_row(a, j, ra0 + NT / PR * i);
     step[i] = src >= 0 ? BK : 0;
-    pa[i] = src >= 0 ? x + src * a.red + ka : reinterpret_cast<const T*>(&g_zeros);
+    pa[i] = src >= 0 ? x + src * a.red + ka : zero;
   }
-  const int nk = (a.red + BK - 1) / BK, nstage = nk * ntile;
-  // and of the weights, from the stage's own place; columns past the last one
-  // are read as the last ones (nothing of them is stored)
+  const int nk = (a.red + BK - 1) / BK;
+  // And of the weights, from the stage's own place; columns past the last one
+  // are read as others (nothing of them is stored).
+  const int kb = threadIdx.x / TBk::PR;            // (BT false) first row of the stage
   uint32_t pb[PB];
-  auto weights_at = [&](int n0) {
 #pragma unroll
-    for (int i = 0; i < PB; ++i) {
-      if constexpr (BT) {
-        const int n = (threadIdx.x >> 3) + 32 * i;
-        pb[i] = static_cast<uint32_t>(n0 + n < a.cols ? n : 0) * a.red + ka;
-      } else {
-        const int p = threadIdx.x + kThreads * i, n = p % TBk::PR * VEC;
-        pb[i] = static_cast<uint32_t>(p / TBk::PR) * a.cols + (n0 + n < a.cols ? n : 0);
-      }
-    }
-  };
-  u32x4_t ra[kDepth][PA], rb[kDepth][PB];
-  int rk = 0, rn = tile0 * BN;                     // the next stage to request
-  weights_at(rn);
-  auto request = [&](int d) {
-    if (WHOLE && rk + BK <= a.red) {
-#pragma unroll
-      for (int i = 0; i < PA; ++i) {
-        ra[d][i] = load_piece(pa[i]);
-        pa[i] += step[i];
-      }
-      const T* ws = BT ? w + static_cast<int64_t>(rn) * a.red + rk
-                       : w + static_cast<int64_t>(rk) * a.cols + rn;
-#pragma unroll
-      for (int i = 0; i < PB; ++i) rb[d][i] = load_piece(ws + pb[i]);
+  for (int i = 0; i < PB; ++i) {
+    if constexpr (BT) {
+      const int n = ra0 + NT / PR * i;
+      pb[i] = static_cast<uint32_t>(j.n0 + n < a.cols ? n : 0) * a.red + ka;
     } else {
-      // the end of the reduction, or pieces that may be cut
+      const int n = (TBk::at(kb, threadIdx.x % TBk::PR) - kb * TBk::PR) * VEC;
+      pb[i] = static_cast<uint32_t>(kb + NT / TBk::PR * i) * a.cols + (j.n0 + n < a.cols ? n : 0);
+    }
+  }
+  // Stages past the last one are asked for too, as zeros, so that the number of
+  // loads behind a stage's own is known.
+  int rk = 0;                                      // the next stage to request
+  auto request = [&](u32x4_t* buf) {
+    const int left = a.red - rk;                   // of the reduction
+    const T* const ws = BT ? w + static_cast<int64_t>(j.n0) * a.red + rk
+                           : w + static_cast<int64_t>(rk) * a.cols + j.n0;
+    if (left >= BK) {
 #pragma unroll
       for (int i = 0; i < PA; ++i) {
-        ra[d][i] = load_left<T, WHOLE>(pa[i], step[i] ? a.red - rk - ka : 0);
+        load_to_lds(pa[i], buf + NT * i + 64 * wave);
         pa[i] += step[i];
       }
 #pragma unroll
-      for (int i = 0; i < PB; ++i) {
-        if constexpr (BT) {
-          const int n = rn + (threadIdx.x >> 3) + 32 * i;
-          rb[d][i] = load_left<T, WHOLE>(w + static_cast<int64_t>(n) * a.red + rk + ka,
-                                         n < a.cols ? a.red - rk - ka : 0);
-        } else {
-          const int p = threadIdx.x + kThreads * i;
-          const int k = rk + p / TBk::PR, n = rn + p % TBk::PR * VEC;
-          rb[d][i] = load_left<T, WHOLE>(w + static_cast<int64_t>(k) * a.cols + n,
-                                         k < a.red ? a.cols - n : 0);
-        }
-      }
+      for (int i = 0; i < PB; ++i)
+        load_to_lds(ws + pb[i], buf + TA::PIECES + NT * i + 64 * wave);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PA; ++i)
+        load_to_lds(ka < left ? pa[i] : zero, buf + NT * i + 64 * wave);
+#pragma unroll
+      for (int i = 0; i < PB; ++i)
+        load_to_lds((BT ? ka : kb + NT / TBk::PR * i) < left ? ws + pb[i] : zero,
+                    buf + TA::PIECES + NT * i + 64 * wave);
     }
     rk += BK;
-    if (rk >= a.red) {                             // on to the next column tile
-      rk = 0;
-      rn += BN;
-#pragma unroll
-      for (int i = 0; i < PA; ++i) pa[i] -= static_cast<int64_t>(nk) * step[i];
-      weights_at(rn);
-    }
-  };
-  auto put = [&](int d, int buf) {
-    u32x4_t* sa = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage);
-    u32x4_t* sb = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage + TA::BYTES);
-#pragma unroll
-    for (int i = 0; i < PA; ++i)
-      sa[TA::at((threadIdx.x >> 3) + 32 * i, threadIdx.x & 7)] = ra[d][i];
-#pragma unroll
-    for (int i = 0; i < PB; ++i) {
-      if constexpr (BT) {
-        sb[TBr::at((threadIdx.x >> 3) + 32 * i, threadIdx.x & 7)] = rb[d][i];
-      } else {
-        const int p = threadIdx.x + kThreads * i;
-        sb[TBk::at(p / TBk::PR, p % TBk::PR)] = rb[d][i];
-      }
-    }
   };
 
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int wr = (wave >> 1) * (BM / 2), wc = (wave & 1) * (BN / 2);
+  const typename TA::Reader rows_of(wave / WC * (BM / WR), lane);
+  const std::conditional_t<BT, typename TBr::Reader, typename TBk::template Reader<32 * WC, FN>>
+      weights_of(32 * (wave % WC), lane);
   f32x16 acc[FN][FM];
-  auto clear = [&] {
 #pragma unroll
-    for (int n = 0; n < FN; ++n)
+  for (int n = 0; n < FN; ++n)
 #pragma unroll
-      for (int m = 0; m < FM; ++m)
+    for (int m = 0; m < FM; ++m)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
+      for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
+  auto stage = [&](const u32x4_t* buf, u32x4_t* before) {
+    stage_barrier<(PA + PB) * (kRing - 2)>();
+    request(before);
+    multiply_stage<T, KB, FM, FN>(
+        acc, [&](int m, int q) { return rows_of(buf, m, q); },
+        [&](int n, int q) { return weights_of(buf + TA::PIECES, BT ? WC * n : n, q); });
   };
-  // The tile's columns leave in parts of CW, FN / PARTS column blocks of each
-  // wave column, through one buffer.
-  constexpr int VO = Row<TO>::VEC;
-  constexpr int PARTS = BM * BN * static_cast<int>(sizeof(TO)) > kStage ? 2 : 1;
-  static_assert(FN % PARTS == 0 && BM * BN / PARTS * static_cast<int>(sizeof(TO)) <= kStage,
-                "a part of the tile fits a buffer");
-  constexpr int CW = BN / PARTS, HW = CW / 2;      // columns of a part; of a wave column's half
-  auto finish = [&](int n0, int buf) {
-    u32x4_t* so = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage);
-    const float* bias = a.bias ? a.bias + static_cast<int64_t>(t.group) * a.cols : nullptr;
-#pragma unroll
-    for (int part = 0; part < PARTS; ++part) {
-      if (part) __syncthreads();
-#pragma unroll
-      for (int f = 0; f < FN / PARTS; ++f) {
-        const int n = part * (FN / PARTS) + f;
-        float b[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) b[i] = 0.0f;
-        if (bias) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int c = n0 + wc + 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-            b[i] = bias[c < a.cols ? c : 0];
-          }
-        }
-        block_to_lds<TO, CW, FM>(so, acc[n], wr, (wave & 1) * HW + 32 * f, b, a.relu);
-      }
-      __syncthreads();
-      for (int p = threadIdx.x; p < BM * CW / VO; p += kThreads) {
-        const int r = p / (CW / VO), piece = p % (CW / VO), c = piece * VO;
-        const int col = n0 + (c / HW) * (BN / 2) + part * HW + c % HW, left = a.cols - col;
-        if (r >= nrow || left <= 0) continue;
-        const int64_t at = (t.begin + r) * a.cols + col;
-        u32x4_t u = so[out_at<TO, CW>(r, piece)];
-        if (a.mask) {
-          float v[VO], g[VO];
-          unpack(u, v);
-          unpack(load_left<TO, false>(static_cast<const TO*>(a.mask) + at, left), g);
-#pragma unroll
-          for (int i = 0; i < VO; ++i) v[i] = g[i] <= 0.0f ? 0.0f : v[i];
-          u = pack(v);
-        }
-        store_left(y + at, u, left);
-      }
-    }
-    __syncthreads();
-  };
+  request(s_buf0);
+  request(s_buf1);
+  request(s_buf2);
+  for (int s = 0; s < nk; s += kRing) {
+    stage(s_buf0, s_buf3);
+    if (s + 1 < nk) stage(s_buf1, s_buf0);
+    if (s + 2 < nk) stage(s_buf2, s_buf1);
+    if (s + 3 < nk) stage(s_buf3, s_buf2);
+  }
+  stage_barrier<0>();                              // (no load is on its way to s_buf0)
+  store_tile_rows<TO, BM, BN, WR, WC, NP0 * 16>(s_buf0, acc, s_bias, a, j, j.n0);
+}
 
+// 4 x 4 exchange among the four lanes of a quad: lane i's v[j] becomes lane j's
+// v[i].
+__device__ __forceinline__ void quad_transpose(uint32_t (&v)[4]) {
+  const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
 #pragma unroll
-  for (int d = 0; d < kDepth; ++d)
-    if (d < nstage) request(d);
-  clear();
-  int k = 0, n0 = tile0 * BN;
-  for (int s0 = 0; s0 < nstage; s0 += kDepth) {
+  for (int j = 0; j < 4; j += 2) {
+    const uint32_t r = lane_other<1>(odd ? v[j] : v[j + 1]);
+    if (odd) v[j] = r; else v[j + 1] = r;
+  }
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) {
-      if (s0 + d >= nstage) break;
-      const int buf = d & 1;                       // (kDepth is even)
-      put(d, buf);
-      if (s0 + d + kDepth < nstage) request(d);
-      __syncthreads();
-      const u32x4_t* sa = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage);
-      const u32x4_t* sb = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage + TA::BYTES);
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t r = lane_other<2>(high ? v[j] : v[j + 2]);
+    if (high) v[j] = r; else v[j + 2] = r;
+  }
+}
+
+// A wave's finished FM x 2 blocks, rows r0 .. of the job, columns c0 .. c0 + 63 (of
+// whole pieces), straight from the registers.  The halves of the wave exchange so
+// that a lane has all 32 columns of one block of its row, and the lanes of a quad
+// so that four of them store 64 adjacent bytes of one row at a time.
+template <typename TO, int FM, bool RELU, bool MASK>
+__device__ __forceinline__ void store_wave_rows(const f32x16 (&acc)[2][FM], const GroupedArgs& a,
+                                                const Job& j, int r0, int c0) {
+  constexpr int VO = Row<TO>::VEC, TOB = static_cast<int>(sizeof(TO));
+  constexpr int NU = 8 * TOB, W4 = TOB;            // words of 32 columns, of 4
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int64_t base = (j.begin + r0 + (lane & 28)) * a.cols;
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        typename M::Frag fa[FM], fb[FN];
+  for (int m = 0; m < FM; ++m) {
+    // u[n]: this lane's words of block n, those of 4 columns of every 8
+    uint32_t u[2][NU / 2];
 #pragma unroll
-        for (int m = 0; m < FM; ++m) fa[m] = TA::frag(sa, wr + 32 * m, s, lane);
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int n = 0; n < FN; ++n) {
-          if constexpr (BT) fb[n] = TBr::frag(sb, wc + 32 * n, s, lane);
-          else fb[n] = TBk::frag(sb, wc + 32 * n, s, lane);
+      for (int q = 0; q < 4; ++q) {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = acc[n][m][4 * q + i];
+          if (RELU) v[i] = v[i] < 0.0f ? 0.0f : v[i];
         }
+        if constexpr (TOB == 2) {
+          u[n][2 * q] = pack2(v[0], v[1]);
+          u[n][2 * q + 1] = pack2(v[2], v[3]);
+        } else {
 #pragma unroll
-        for (int n = 0; n < FN; ++n)
-#pragma unroll
-          for (int m = 0; m < FM; ++m) acc[n][m] = M::mma(fb[n], fa[m], acc[n][m]);
+          for (int i = 0; i < 4; ++i) u[n][4 * q + i] = __float_as_uint(v[i]);
+        }
       }
-      if (++k == nk) {
-        finish(n0, buf ^ 1);
-        clear();
-        k = 0;
-        n0 += BN;
+    // word[k]: the row's words of block h in order
+    uint32_t word[NU];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int i = 0; i < W4; ++i) {
+        const auto r = __builtin_amdgcn_permlane32_swap(u[0][W4 * q + i], u[1][W4 * q + i], false,
+                                                        false);
+        word[2 * W4 * q + i] = r[0];
+        word[2 * W4 * q + W4 + i] = r[1];
+      }
+#pragma unroll
+    for (int half = 0; half < NU / 16; ++half) {
+      // 64 bytes of each of the quad's rows: piece p of lane i is words 4 p .. + 3
+      u32x4_t piece[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t v[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) v[p] = word[16 * half + 4 * p + i];
+        quad_transpose(v);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) piece[p][i] = v[p];
+      }
+      // now piece[t] is piece lane % 4 of the row of the quad's lane t
+      const int col = c0 + 32 * h + (16 * half + 4 * (lane & 3)) * 4 / TOB;
+      const int rows = col < a.cols ? j.nrow - r0 - 32 * m - (lane & 28) : 0;
+      const int64_t at = base + static_cast<int64_t>(32 * m) * a.cols + col;
+      TO* const y = static_cast<TO*>(a.y) + at;
+      u32x4_t g[4];
+      if constexpr (MASK) {
+        const TO* const mask = static_cast<const TO*>(a.mask) + at;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          g[t] = load_left<TO, true>(mask + static_cast<int64_t>(t) * a.cols, t < rows ? VO : 0);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if constexpr (MASK) {
+          float v[VO], z[VO];
+          unpack(piece[t], v);
+          unpack(g[t], z);
+#pragma unroll
+          for (int e = 0; e < VO; ++e) v[e] = z[e] <= 0.0f ? 0.0f : v[e];
+          piece[t] = pack(v);
+        }
+        if (t < rows) store_piece(y + static_cast<int64_t>(t) * a.cols, piece[t]);
       }
     }
   }
 }
 
+// Short reductions of bf16 (NK stages): a workgroup keeps its 64 * WR rows in
+// registers, as fragments, and takes the columns `span` by 128 at a time.  Only
+// the weights go through LDS, kRing stages of them, all but one on their way while
+// that one is multiplied, and finished tiles leave from the registers: nothing in
+// the loop waits for memory asked for in the same tile.  (k_grouped would read the
+// rows once per 256 columns, wait for memory every stage, and drain and refill for
+// every tile of a few stages.)
+constexpr int short_ring(int nk) { return nk == 3 ? 3 : 4; }
+template <typename TO, bool BT, int NK, int WR, bool RELU, bool MASK>
+__global__ __launch_bounds__(128 * WR, 2) void k_grouped_short(GroupedArgs a, int span) {
+  typedef bf16_t T;
+  typedef Mma<T> M;
+  constexpr int BM = 64 * WR, BN = 128, NT = 128 * WR, WC = 2, FM = 2, FN = 2;
+  constexpr int kRing = short_ring(NK), U = kRing / NK;   // tiles until the ring repeats
+  constexpr int KB = 128;
+  typedef RTile<T, BN, KB> TBr;
+  typedef KTile<T, BN, KB> TBk;
+  constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, STEPS = BK / M::KS;
+  constexpr int PB = TBk::PIECES / NT;
+  // (separate arrays, so that the compiler knows which loads a read waits for)
+  __shared__ u32x4_t s_w0[TBk::PIECES], s_w1[TBk::PIECES], s_w2[TBk::PIECES],
+      s_w3[kRing > 3 ? TBk::PIECES : 1];
+  const T* const x = static_cast<const T*>(a.x);
+  Job j;
+  if (!grouped_job<TO, BM>(a, span, &j)) return;
+  const T* const w = static_cast<const T*>(a.w) + static_cast<int64_t>(j.group) * a.red * a.cols;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wr = wave / WC * 64, wc = wave % WC * 64;
+  const T* const zero = reinterpret_cast<const T*>(&g_zeros);
+  const int end = a.cols - j.n0 < span ? a.cols : j.n0 + span;
+  // A lane's pieces of a weights' stage are those that belong at its place in LDS.
+  // Stages past the last one are asked for too (as zeros or as columns of others),
+  // so that the number of loads behind a stage's own is known.
+  const int ra0 = threadIdx.x >> 3, ka = ((threadIdx.x & 7) ^ ((ra0 >> 1) & 7)) * VEC;
+  const int kb = threadIdx.x / TBk::PR;
+  const int nb = (TBk::at(kb, threadIdx.x % TBk::PR) - kb * TBk::PR) * VEC;
+  // (columns past the last one are read as others: nothing of them is stored)
+  const int own = lane_place(BT ? ra0 * a.red + ka : kb * a.cols + nb);
+  const int next = BT ? NT / 8 * a.red : NT / TBk::PR * a.cols;
+  auto request = [&](int k, int n0, u32x4_t* buf) {
+    const bool whole = n0 + BN <= a.cols && (k + 1) * BK <= a.red;
+    const T* const ws = w + (BT ? static_cast<int64_t>(n0) * a.red + k * BK
+                                : static_cast<int64_t>(k) * BK * a.cols + n0);
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < PB; ++i) load_to_lds(ws + (own + i * next), buf + NT * i + 64 * wave);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PB; ++i) {
+        const int n = n0 + (BT ? ra0 + NT / 8 * i : nb);
+        const int c = k * BK + (BT ? ka : kb + NT / TBk::PR * i);
+        load_to_lds(n < a.cols && c < a.red ? ws + (own + i * next) : zero,
+                    buf + NT * i + 64 * wave);
+      }
+    }
+  };
+  const std::conditional_t<BT, typename TBr::Reader, typename TBk::template Reader<32, FN>>
+      weights_of(wc, lane);
+  auto ring = [&](int r) { return r == 0 ? s_w0 : r == 1 ? s_w1 : r == 2 ? s_w2 : s_w3; };
+  // A tile starts from its bias: lane i has that of column wc + i, asked for a
+  // tile before.
+  const float* const b = a.bias ? a.bias + static_cast<int64_t>(j.group) * a.cols : nullptr;
+  auto bias_of = [&](int n0) {
+    const int c = n0 + wc + lane;
+    return b && c < a.cols ? b[c] : 0.0f;
+  };
+  // The rows.
+  typename M::Frag fa[FM][NK * STEPS];
+#pragma unroll
+  for (int m = 0; m < FM; ++m) {
+    const int64_t src = source_row(a, j, wr + 32 * m + (lane & 31));
+    const T* const p = x + (src < 0 ? 0 : src) * a.red;
+#pragma unroll
+    for (int q = 0; q < NK * STEPS; ++q) {
+      const int c = 16 * q + 8 * (lane >> 5);
+      fa[m][q] = __builtin_bit_cast(typename M::Frag,
+                                    load_left<T, true>(p + c, src < 0 ? 0 : a.red - c));
+    }
+  }
+  float bias = bias_of(j.n0);
+#pragma unroll
+  for (int s = 0; s < kRing - 1; ++s) request(s % NK, j.n0 + s / NK * BN, ring(s));
+  for (int n1 = j.n0; n1 < end; n1 += U * BN) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int n0 = n1 + u * BN;
+      if (n0 >= end) break;
+      f32x16 acc[FN][FM];
+#pragma unroll
+      for (int n = 0; n < FN; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float v = __shfl(bias, 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4, 64);
+#pragma unroll
+          for (int m = 0; m < FM; ++m) acc[n][m][i] = v;
+        }
+      bias = bias_of(n0 + BN);
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        const int s = u * NK + k;                  // (of the ring's U tiles)
+        u32x4_t* const buf = ring(s);
+        // kRing - 2 stages' loads are behind this one's
+        stage_barrier<PB * (kRing - 2)>();
+        const int ahead = s + kRing - 1;
+        request(ahead % NK, n1 + ahead / NK * BN, ring(ahead % kRing));
+#pragma unroll
+        for (int q = 0; q < STEPS; ++q) {
+          typename M::Frag fb[FN];
+#pragma unroll
+          for (int n = 0; n < FN; ++n) fb[n] = weights_of(buf, n, q);
+#pragma unroll
+          for (int n = 0; n < FN; ++n)
+#pragma unroll
+            for (int m = 0; m < FM; ++m)
+              acc[n][m] = M::mma(fb[n], fa[m][k * STEPS + q], acc[n][m]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      store_wave_rows<TO, FM, RELU, MASK>(acc, a, j, wr, n0 + wc);
+    }
+  }
+  stage_barrier<0>();                              // (no load to LDS outlives the workgroup)
+}
+
+// The same for rows and weights whose pieces may be cut (widths that are no
+// multiple of a piece) or unaligned: through registers, 128 x 128 or 64 x 64 by
+// four waves in 2 x 2.
+template <typename T, typename TO, bool BT, int BM, int BN>
+__global__ __launch_bounds__(kThreads, 2) void k_grouped_any(GroupedArgs a) {
+  constexpr int KB = 128;
+  typedef RTile<T, BM, KB> TA;
+  typedef RTile<T, BN, KB> TBr;
+  typedef KTile<T, BN, KB> TBk;
+  constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>;
+  constexpr int FM = BM / 64, FN = BN / 64;
+  constexpr int PA = TA::PIECES / kThreads, PB = TBk::PIECES / kThreads;
+  constexpr int NP = TA::PIECES + TBk::PIECES;
+  __shared__ u32x4_t s_buf[NP];
+  __shared__ __attribute__((aligned(16))) float s_bias[BN];
+  const T* const x = static_cast<const T*>(a.x);
+  Job j;
+  if (!grouped_job<TO, BM>(a, BN, &j)) return;
+  const int n0 = j.n0;
+  load_bias<BN>(a, j, n0, s_bias);
+  const T* const w = static_cast<const T*>(a.w) + static_cast<int64_t>(j.group) * a.red * a.cols;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int ra0 = threadIdx.x >> 3, ka = (threadIdx.x & 7) * VEC;
+  const T* pa[PA];
+  bool oka[PA];
+#pragma unroll
+  for (int i = 0; i < PA; ++i) {
+    const int64_t src = source_row(a, j, ra0 + 32 * i);
+    oka[i] = src >= 0;
+    pa[i] = x + (src < 0 ? 0 : src) * a.red;
+  }
+  u32x4_t ra[PA], rb[PB];
+  auto request = [&](int k0, int n0) {
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+      ra[i] = load_left<T, false>(pa[i] + k0 + ka, oka[i] ? a.red - k0 - ka : 0);
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      if constexpr (BT) {
+        const int n = n0 + ra0 + 32 * i;
+        rb[i] = load_left<T, false>(w + static_cast<int64_t>(n) * a.red + k0 + ka,
+                                    n < a.cols ? a.red - k0 - ka : 0);
+      } else {
+        const int p = threadIdx.x + kThreads * i;
+        const int k = k0 + p / TBk::PR, n = n0 + p % TBk::PR * VEC;
+        rb[i] = load_left<T, false>(w + static_cast<int64_t>(k) * a.cols + n,
+                                    k < a.red ? a.cols - n : 0);
+      }
+    }
+  };
+  const typename TA::Reader rows_of((wave >> 1) * (BM / 2), lane);
+  const std::conditional_t<BT, typename TBr::Reader, typename TBk::template Reader<64, FN>>
+      weights_of(32 * (wave & 1), lane);
+  f32x16 acc[FN][FM];
+#pragma unroll
+  for (int n = 0; n < FN; ++n)
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
+  request(0, n0);
+  for (int k0 = 0; k0 < a.red; k0 += BK) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PA; ++i) s_buf[TA::at(ra0 + 32 * i, threadIdx.x & 7)] = ra[i];
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      const int p = threadIdx.x + kThreads * i;
+      s_buf[TA::PIECES + (BT ? TBr::at(ra0 + 32 * i, threadIdx.x & 7)
+                             : TBk::at(p / TBk::PR, p % TBk::PR))] = rb[i];
+    }
+    __syncthreads();
+    if (k0 + BK < a.red) request(k0 + BK, n0);
+    multiply_stage<T, KB, FM, FN>(
+        acc, [&](int m, int q) { return rows_of(s_buf, m, q); },
+        [&](int n, int q) { return weights_of(s_buf + TA::PIECES, BT ? 2 * n : n, q); });
+  }
+  store_tile_rows<TO, BM, BN, 2, 2, NP * 16>(s_buf, acc, s_bias, a, j, n0);
+}
+
 // Weight gradient of a BC x BN tile of one group, over a chunk of its
 // positions: dw[c][n] = sum_j x[row j][c] dy[j][n].  Both operands are staged
-// with the positions as the reduction's rows.  Chunk `id` leaves its sums as
-// part[id] (one chunk per group: dw[group] itself).  The column-tile-0
-// workgroups also sum dy, as the product of ones with it.
+// with the positions as the reduction's rows.  Chunk `job` leaves its sums as
+// part[job] (one chunk per group: dw[group] itself).  The workgroups of the
+// first rows of dw also sum dy.
 struct WeightArgs {
   const void* x;
   int64_t n_x;
@@ -500,20 +873,40 @@ struct WeightArgs {
   hipStream_t st;
 };
 
-template <typename T, int BC, int BN, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 2) void k_grouped_dw(WeightArgs a) {
-  typedef Mma<T> M;
-  typedef KTile<T, BC> TX;
-  typedef KTile<T, BN> TY;
-  constexpr int VEC = Row<T>::VEC, BK = kBK<T>, STEPS = BK / M::KS, kDepth = 2;
-  constexpr int FC = BC / 64, FN = BN / 64;
-  constexpr int PX = TX::PIECES / kThreads, PY = TY::PIECES / kThreads;
-  constexpr int kStage = TX::BYTES + TY::BYTES;
-  __shared__ __attribute__((aligned(16))) unsigned char s_buf[2 * kStage];
+// A lane's part of the column sums of a fragment (the same column in both halves
+// of the wave, other rows).
+__device__ __forceinline__ float frag_sum(float s, bf16x8 f) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s += static_cast<float>(f[i]);
+  return s;
+}
+__device__ __forceinline__ float frag_sum(float s, f32x4_t f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s += f[i];
+  return s;
+}
+
+// DMA: whole 16-byte pieces at aligned addresses, straight to LDS, through
+// a ring of four buffers as k_grouped's; else through registers, one buffer.
+template <typename T, int BC, int BN, int WR, int WC, bool DMA>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped_dw(WeightArgs a) {
+  constexpr int KB = DMA ? 64 : 128, kRing = 4;
+  typedef KTile<T, BC, KB> TX;
+  typedef KTile<T, BN, KB> TY;
+  constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = 64 * WR * WC;
+  constexpr int FC = BC / WR / 32, FN = BN / WC / 32;
+  constexpr int PX = TX::PIECES / NT, PY = TY::PIECES / NT, NP = TX::PIECES + TY::PIECES;
+  static_assert(NT % 256 == 0, "a lane's pieces of a stage have one place in their rows");
+  constexpr int NR = DMA ? NP : 1;
+  __shared__ u32x4_t s_buf0[NP], s_buf1[NR], s_buf2[NR], s_buf3[NR];
+  // The row numbers of NT positions at a time, three such runs: the one being
+  // requested, the next one, and the one a slower wave may still read.
+  __shared__ int32_t s_row[3][NT];
   const T *const x = static_cast<const T*>(a.x), *const dy = static_cast<const T*>(a.dy);
   const int64_t nc = (a.C_in + BC - 1) / BC, nn = (a.C_out + BN - 1) / BN;
   const int64_t id = die_order(blockIdx.x, gridDim.x);
-  const int64_t job = id / (nc * nn), c0 = id / nn % nc * BC, n0 = id % nn * BN;
+  const int64_t job = id / (nc * nn);
+  const int c0 = static_cast<int>(id / nn % nc) * BC, n0 = static_cast<int>(id % nn) * BN;
   Tile t;
   if (a.chunk) {
     t = find_tile<false>(a.offsets, a.E, a.m, a.chunk, job);
@@ -524,53 +917,47 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_dw(WeightArgs a) {
     e = e < b ? b : e > a.m ? a.m : e;
     t = Tile{static_cast<int>(job), b, e, 0};
   }
-  // The row numbers of kThreads positions at a time, three such runs in LDS: the
-  // one being requested, the next one, and the one a slower wave may still read.
-  __shared__ int32_t s_row[3][kThreads];
-  constexpr int RUN = kThreads / BK;               // stages of a run
+  constexpr int RUN = NT / BK;                     // stages of a run
   auto row_of = [&](int64_t j) {
     return j >= t.end ? -1 : a.rows ? a.rows[j] : static_cast<int32_t>(j);
   };
   int64_t rj = t.begin;                            // the next stage to request
   int rq = 0, run = 0;                             // its place in its run, its run (mod 3)
   s_row[0][threadIdx.x] = row_of(rj + threadIdx.x);
-  int32_t row_next = row_of(rj + kThreads + threadIdx.x);
+  int32_t row_next = row_of(rj + NT + threadIdx.x);
   __syncthreads();
-  u32x4_t rx[kDepth][PX], ry[kDepth][PY];
-  uint32_t py[PY];
-#pragma unroll
-  for (int i = 0; i < PY; ++i) {
-    const int p = threadIdx.x + kThreads * i, n = p % TY::PR * VEC;
-    py[i] = static_cast<uint32_t>(p / TY::PR) * a.C_out + (n0 + n < a.C_out ? n : 0);
-  }
-  auto request = [&](int d) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  // a lane's first row of a stage and its column there, per operand: the place
+  // in LDS that a lane's piece goes to is its own (DMA) or its piece's
+  const int jx = threadIdx.x / TX::PR, px = threadIdx.x % TX::PR;
+  const int jy = threadIdx.x / TY::PR, py = threadIdx.x % TY::PR;
+  const int cx = c0 + (DMA ? TX::at(jx, px) - jx * TX::PR : px) * VEC;
+  const int cy = n0 + (DMA ? TY::at(jy, py) - jy * TY::PR : py) * VEC;
+  // (DMA) columns past the last one are read as others: nothing of them is stored
+  const int cxr = cx < a.C_in ? cx : 0, cyr = cy < a.C_out ? cy : 0;
+  u32x4_t rx[DMA ? 1 : PX], ry[DMA ? 1 : PY];
+  auto request = [&](u32x4_t* buf) {
+    const T* const zero = reinterpret_cast<const T*>(&g_zeros);
 #pragma unroll
     for (int i = 0; i < PX; ++i) {
-      const int p = threadIdx.x + kThreads * i;
-      const int32_t row = s_row[run][rq * BK + p / TX::PR];
-      const int64_t c = c0 + p % TX::PR * VEC;
+      const int32_t row = s_row[run][rq * BK + jx + NT / TX::PR * i];
       const bool ok = row >= 0 && row < a.n_x;
-      rx[d][i] = load_left<T, WHOLE>(x + static_cast<int64_t>(row) * a.C_in + c,
-                                     ok ? a.C_in - c : 0);
+      const T* const p = x + static_cast<int64_t>(row) * a.C_in;
+      if constexpr (DMA) load_to_lds(ok ? p + cxr : zero, buf + NT * i + 64 * wave);
+      else rx[i] = load_left<T, false>(p + cx, ok ? a.C_in - cx : 0);
     }
-    if (WHOLE && rj + BK <= t.end) {
-      // (columns past the last one are read as others: nothing of them is stored)
-      const T* ys = dy + rj * a.C_out + n0;
 #pragma unroll
-      for (int i = 0; i < PY; ++i) ry[d][i] = load_piece(ys + py[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < PY; ++i) {
-        const int p = threadIdx.x + kThreads * i;
-        const int64_t j = rj + p / TY::PR, n = n0 + p % TY::PR * VEC;
-        ry[d][i] = load_left<T, WHOLE>(dy + j * a.C_out + n, j < t.end ? a.C_out - n : 0);
-      }
+    for (int i = 0; i < PY; ++i) {
+      const int64_t j = rj + jy + NT / TY::PR * i;
+      const T* const p = dy + j * a.C_out;
+      if constexpr (DMA)
+        load_to_lds(j < t.end ? p + cyr : zero, buf + TX::PIECES + NT * i + 64 * wave);
+      else ry[i] = load_left<T, false>(p + cy, j < t.end ? a.C_out - cy : 0);
     }
     if (rq == 0) {
-      // (read from the next stage but RUN - 1 on, with barriers between)
-      const int to = run == 2 ? 0 : run + 1;
-      s_row[to][threadIdx.x] = row_next;
-      row_next = row_of(rj + 2 * kThreads + threadIdx.x);
+      // (read RUN - 1 stages on at the earliest, with barriers between)
+      s_row[run == 2 ? 0 : run + 1][threadIdx.x] = row_next;
+      row_next = row_of(rj + 2 * NT + threadIdx.x);
     }
     rj += BK;
     if (++rq == RUN) {
@@ -578,73 +965,68 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_dw(WeightArgs a) {
       run = run == 2 ? 0 : run + 1;
     }
   };
-  auto put = [&](int d, int buf) {
-    u32x4_t* sx = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage);
-    u32x4_t* sy = reinterpret_cast<u32x4_t*>(s_buf + buf * kStage + TX::BYTES);
-#pragma unroll
-    for (int i = 0; i < PX; ++i) {
-      const int p = threadIdx.x + kThreads * i;
-      sx[TX::at(p / TX::PR, p % TX::PR)] = rx[d][i];
-    }
-#pragma unroll
-    for (int i = 0; i < PY; ++i) {
-      const int p = threadIdx.x + kThreads * i;
-      sy[TY::at(p / TY::PR, p % TY::PR)] = ry[d][i];
-    }
-  };
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int wr = (wave >> 1) * (BC / 2), wc = (wave & 1) * (BN / 2);
+  const int wr = wave / WC * (BC / WR), wc = wave % WC * (BN / WC);
   const bool bias = a.db && c0 == 0 && wr == 0;    // (uniform over the wave)
-  f32x16 acc[FN][FC], accb[FN];
+  f32x16 acc[FN][FC];
+  float sum[FN];
 #pragma unroll
-  for (int n = 0; n < FN; ++n)
+  for (int n = 0; n < FN; ++n) {
+    sum[n] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      accb[n][i] = 0.0f;
+    for (int m = 0; m < FC; ++m)
 #pragma unroll
-      for (int m = 0; m < FC; ++m) acc[n][m][i] = 0.0f;
-    }
+      for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
+  }
+  const typename TX::template Reader<32, FC> x_of(wr, lane);
+  const typename TY::template Reader<32, FN> dy_of(wc, lane);
+  auto multiply = [&](const u32x4_t* buf) {
+    multiply_stage<T, KB, FC, FN>(
+        acc, [&](int m, int q) { return x_of(buf, m, q); },
+        [&](int n, int q) {
+          const typename Mma<T>::Frag f = dy_of(buf + TX::PIECES, n, q);
+          if (bias) sum[n] = frag_sum(sum[n], f);
+          return f;
+        });
+  };
   const int64_t nk = (t.end - t.begin + BK - 1) / BK;
-#pragma unroll
-  for (int d = 0; d < kDepth; ++d)
-    if (d < nk) request(d);
-  for (int64_t k0 = 0; k0 < nk; k0 += kDepth) {
-#pragma unroll
-    for (int d = 0; d < kDepth; ++d) {
-      if (k0 + d >= nk) break;
-      const int buf = d & 1;
-      put(d, buf);
-      if (k0 + d + kDepth < nk) request(d);
+  if constexpr (DMA) {
+    // (stages past the last one are asked for too, as zeros)
+    auto stage = [&](const u32x4_t* buf, u32x4_t* before) {
+      stage_barrier<(PX + PY) * (kRing - 2)>();
+      request(before);
+      multiply(buf);
+    };
+    request(s_buf0);
+    request(s_buf1);
+    request(s_buf2);
+    for (int64_t s = 0; s < nk; s += kRing) {
+      stage(s_buf0, s_buf3);
+      if (s + 1 < nk) stage(s_buf1, s_buf0);
+      if (s + 2 < nk) stage(s_buf2, s_buf1);
+      if (s + 3 < nk) stage(s_buf3, s_buf2);
+    }
+    stage_barrier<0>();                            // (no load to LDS outlives the workgroup)
+  } else {
+    if (nk) request(nullptr);
+    for (int64_t s = 0; s < nk; ++s) {
       __syncthreads();
-      const u32x4_t* sx = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage);
-      const u32x4_t* sy = reinterpret_cast<const u32x4_t*>(s_buf + buf * kStage + TX::BYTES);
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        typename M::Frag fx[FC], fy[FN];
+      for (int i = 0; i < PX; ++i) s_buf0[TX::at(jx + NT / TX::PR * i, px)] = rx[i];
 #pragma unroll
-        for (int m = 0; m < FC; ++m) fx[m] = TX::frag(sx, wr + 32 * m, s, lane);
-#pragma unroll
-        for (int n = 0; n < FN; ++n) fy[n] = TY::frag(sy, wc + 32 * n, s, lane);
-#pragma unroll
-        for (int n = 0; n < FN; ++n)
-#pragma unroll
-          for (int m = 0; m < FC; ++m) acc[n][m] = M::mma(fy[n], fx[m], acc[n][m]);
-        if (bias) {
-#pragma unroll
-          for (int n = 0; n < FN; ++n) accb[n] = M::mma(fy[n], M::ones(), accb[n]);
-        }
-      }
+      for (int i = 0; i < PY; ++i)
+        s_buf0[TX::PIECES + TY::at(jy + NT / TY::PR * i, py)] = ry[i];
+      __syncthreads();
+      if (s + 1 < nk) request(nullptr);
+      multiply(s_buf0);
     }
   }
-  // every column of the product with ones holds the same sums
-  if (bias && (lane & 31) == 0) {
+  if (bias) {
 #pragma unroll
-    for (int n = 0; n < FN; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int64_t col = n0 + wc + 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-        if (col < a.C_out) a.db[job * a.C_out + col] = accb[n][i];
-      }
+    for (int n = 0; n < FN; ++n) {
+      const float v = sum[n] + __shfl_xor(sum[n], 32, 64);
+      const int col = n0 + wc + 32 * n + lane;
+      if (lane < 32 && col < a.C_out) a.db[job * a.C_out + col] = v;
+    }
   }
   float* out = a.dw + job * a.C_in * a.C_out;
 #pragma unroll
@@ -655,7 +1037,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_dw(WeightArgs a) {
       if (r >= a.C_in) continue;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t c = n0 + wc + 32 * n + 8 * q + 4 * (lane >> 5);
+        const int c = n0 + wc + 32 * n + 8 * q + 4 * (lane >> 5);
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = acc[n][m][4 * q + i];
@@ -719,64 +1101,144 @@ __global__ __launch_bounds__(kThreads) void k_grouped_dw_sum(
   }
 }
 
-// How the weight gradient cuts its groups: chunk = 0 where the groups' own tiles
-// fill the card or there is little to sum, else positions per chunk.
+// How the weight gradient cuts its groups: tiles of dw of 256 x 256, 128 x 128 or
+// 64 x 64, the largest that fill the card; chunk = 0 where the groups' own tiles
+// do or there is little to sum, else positions per chunk.
 struct DwPlan {
-  int64_t chunk, jobs;
+  int tile;
+  int64_t chunk, jobs, tiles;
   size_t bytes;
 };
-DwPlan dw_plan(int dt, int64_t m, int E, int C_in, int C_out) {
-  (void)dt;
-  const int64_t tiles = ((C_in + 127ll) / 128) * ((C_out + 127ll) / 128);
-  const int64_t want = 1024;                       // workgroups: two waves of two a compute unit
-  if (m <= 1024 || E * tiles >= 4 * want) return DwPlan{0, E, 0};
-  int64_t chunks = (want + tiles - 1) / tiles;
-  int64_t chunk = (m + chunks - 1) / chunks;
-  chunk = (chunk + 255) / 256 * 256;
-  const int64_t jobs = m / chunk + (E < m ? E : m);
-  const size_t per = static_cast<size_t>(C_in) * C_out + C_out;
-  return DwPlan{chunk, jobs, static_cast<size_t>(jobs) * per * sizeof(float)};
+DwPlan dw_plan(int64_t m, int E, int C_in, int C_out, bool wide) {
+  const int64_t widest = C_in < C_out ? C_out : C_in, least = C_in < C_out ? C_in : C_out;
+  DwPlan p;
+  p.tile = wide && least > 128 && m > 16384 ? 256 : least > 64 && widest > 64 ? 128 : 64;
+  p.tiles = ((C_in + p.tile - 1ll) / p.tile) * ((C_out + p.tile - 1ll) / p.tile);
+  p.chunk = 0;
+  p.jobs = E;
+  p.bytes = 0;
+  if (m <= 1024) return p;
+  // Rounds of the card's workgroups (one, two or four a compute unit) times a
+  // chunk's positions, and what the chunks' sums cost to write and read: a
+  // position takes about 0.04 us of a 256 x 256 tile, a workgroup 8 us besides
+  // them, the sums 4 MB a us.  Without chunks a workgroup can have twice the mean.
+  const int64_t slots = p.tile == 256 ? 256 : p.tile == 128 ? 512 : 1024;
+  const double pos = p.tile == 256 ? 0.04 : p.tile == 128 ? 0.02 : 0.01, fixed = 8.0;
+  const double per = (static_cast<double>(C_in) * C_out + C_out) * 8.0 / 4e6;
+  const int64_t groups = E < m ? E : m;
+  const double mean = static_cast<double>(m) / groups;
+  const double work = static_cast<double>((groups * p.tiles + slots - 1) / slots);
+  double best = (work < 2.0 ? 2.0 : work) * (mean * pos + fixed);
+  if (groups == 1) best = work * (mean * pos + fixed);
+  for (int rounds = 1; rounds <= 8; ++rounds) {
+    const int64_t chunks = rounds * slots / p.tiles - groups;
+    if (chunks < 1) continue;
+    int64_t chunk = (m + chunks - 1) / chunks;
+    chunk = (chunk + 63) / 64 * 64;
+    const int64_t jobs = m / chunk + groups;
+    const double cost = rounds * (chunk * pos + fixed) + jobs * per;
+    if (cost < best) {
+      best = cost;
+      p.chunk = chunk;
+      p.jobs = jobs;
+    }
+  }
+  if (p.chunk)
+    p.bytes = static_cast<size_t>(p.jobs) * (static_cast<size_t>(C_in) * C_out + C_out) * 4;
+  return p;
 }
 
-// (a shift of the count: groups never have more tiles than this)
+// (groups never have more tiles than this)
 inline int64_t tile_bound(int64_t m, int64_t groups, int64_t BM) {
   return m / BM + (groups < m ? groups : m);
 }
+// Whole aligned 16-byte pieces in rows of C elements from p.
+template <typename T> bool whole_rows(const void* p, int64_t C) {
+  return C % Row<T>::VEC == 0 && aligned_to(p, 16);
+}
 
-template <typename T, typename TO, bool BT, int BM, int BN> int run_tile(GroupedArgs a) {
-  const int64_t tiles = tile_bound(a.m, a.E + 1, BM), ncol = (a.cols + BN - 1) / BN;
-  // longer strips while they leave four workgroups a compute unit
-  int64_t strip = tiles * ncol / 1024;
-  strip = strip < 1 ? 1 : strip > ncol ? ncol : strip;
-  a.strip = static_cast<int>(strip);
-  const int64_t blocks = tiles * ((ncol + strip - 1) / strip);
-  if (blocks > 0x7fffffff) return SPCONV_EINVAL;
-  const bool whole = a.red % Row<T>::VEC == 0 && (BT || a.cols % Row<T>::VEC == 0);
-  if (whole)
-    k_grouped<T, TO, BT, BM, BN, true><<<static_cast<uint32_t>(blocks), kThreads, 0, a.st>>>(a);
-  else
-    k_grouped<T, TO, BT, BM, BN, false><<<static_cast<uint32_t>(blocks), kThreads, 0, a.st>>>(a);
+template <int BM> bool grouped_grid(const GroupedArgs& a, int span, uint32_t* blocks) {
+  const int64_t n = tile_bound(a.m, a.E + 1, BM) * ((a.cols + span - 1) / span);
+  *blocks = static_cast<uint32_t>(n);
+  return n <= 0x7fffffff;
+}
+template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC>
+int run_grouped(const GroupedArgs& a) {
+  uint32_t blocks;
+  if (!grouped_grid<BM>(a, BN, &blocks)) return SPCONV_EINVAL;
+  k_grouped<T, TO, BT, BM, BN, WR, WC><<<blocks, 64 * WR * WC, 0, a.st>>>(a);
   return launched();
 }
-template <typename T, typename TO, bool BT> int run_grouped(const GroupedArgs& a) {
-  if (a.cols <= 64 || a.m <= 64ll * a.E) return run_tile<T, TO, BT, 64, 64>(a);
-  return run_tile<T, TO, BT, 128, 128>(a);
+template <typename T, typename TO, bool BT, int BM, int BN>
+int run_grouped_any(const GroupedArgs& a) {
+  uint32_t blocks;
+  if (!grouped_grid<BM>(a, BN, &blocks)) return SPCONV_EINVAL;
+  k_grouped_any<T, TO, BT, BM, BN><<<blocks, kThreads, 0, a.st>>>(a);
+  return launched();
+}
+template <typename TO, bool BT, int NK> int run_grouped_short(const GroupedArgs& a) {
+  // 256 rows a workgroup; 128 where their fragments leave room for no more than
+  // the waves of one, so that another one multiplies while it stores
+  // (256 -> 1024, 696,416 positions: 663 us against 706; 64 -> 256: 137 against 124)
+  constexpr int WR = NK <= 2 ? 4 : 2, BM = 64 * WR;
+  // all columns, or as many as leave eight workgroups a compute unit
+  const int64_t tiles = tile_bound(a.m, a.E + 1, BM), want = 2048 / tiles + 1;
+  const int ncol = (a.cols + 127) / 128;
+  const int parts = static_cast<int>(want < ncol ? want : ncol);
+  const int span = (ncol + parts - 1) / parts * 128;
+  uint32_t blocks;
+  if (!grouped_grid<BM>(a, span, &blocks)) return SPCONV_EINVAL;
+  if (BT ? a.mask != nullptr : a.relu != 0)
+    k_grouped_short<TO, BT, NK, WR, !BT, BT><<<blocks, 128 * WR, 0, a.st>>>(a, span);
+  else
+    k_grouped_short<TO, BT, NK, WR, false, false><<<blocks, 128 * WR, 0, a.st>>>(a, span);
+  return launched();
+}
+// Which kernel: k_grouped_any where pieces may be cut or unaligned; k_grouped_short
+// for bf16 reductions of at most 256 and more than one column tile, of many rows
+// (256 -> 1024, 696,416 positions: 663 us against 847); else k_grouped with tiles
+// of 256 x 256 where they fill the card twice and waste little of their last
+// columns (bf16 2048 -> 2048, 65,536 positions: 603 us against 692 with 128 x 128,
+// of which two fit a compute unit; fp32, bound by its products, 433 against 341 the
+// other way), 64 x 64 for few rows a group or few columns, 128 x 128 otherwise.
+template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
+  const bool small = a.cols <= 64 || a.m <= 64ll * a.E;
+  if (!whole_rows<T>(a.x, a.red) || !whole_rows<T>(a.w, BT ? a.red : a.cols))
+    return small ? run_grouped_any<T, TO, BT, 64, 64>(a) : run_grouped_any<T, TO, BT, 128, 128>(a);
+  if (small) return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
+  if constexpr (sizeof(T) == 2) {
+    if (a.red <= 256 && a.cols > 128 && a.cols % Row<TO>::VEC == 0 && a.m >= 16384) {
+      const int nk = (a.red + kBK<T, 128> - 1) / kBK<T, 128>;
+      if (nk <= 1) return run_grouped_short<TO, BT, 1>(a);
+      if (nk <= 2) return run_grouped_short<TO, BT, 2>(a);
+      if (nk <= 3) return run_grouped_short<TO, BT, 3>(a);
+      return run_grouped_short<TO, BT, 4>(a);
+    }
+    const int64_t c256 = (a.cols + 255) / 256, c128 = (a.cols + 127) / 128;
+    if (20 * c256 <= 11 * c128 + 1 && a.m / 256 * c256 >= 512)
+      return run_grouped<T, TO, BT, 256, 256, 2, 4>(a);
+  }
+  return run_grouped<T, TO, BT, 128, 128, 2, 2>(a);
 }
 template <bool BT> int run_types(int in_dt, int out_dt, const GroupedArgs& a) {
   if (in_dt == SPCONV_BF16)
-    return out_dt == SPCONV_BF16 ? run_grouped<bf16_t, bf16_t, BT>(a)
-                                 : run_grouped<bf16_t, float, BT>(a);
-  return out_dt == SPCONV_BF16 ? run_grouped<float, bf16_t, BT>(a)
-                               : run_grouped<float, float, BT>(a);
+    return out_dt == SPCONV_BF16 ? by_size<bf16_t, bf16_t, BT>(a) : by_size<bf16_t, float, BT>(a);
+  return out_dt == SPCONV_BF16 ? by_size<float, bf16_t, BT>(a) : by_size<float, float, BT>(a);
 }
 
-template <typename T, int BC, int BN> void run_dw(const WeightArgs& a, int64_t jobs) {
-  const uint32_t blocks = static_cast<uint32_t>(jobs * ((a.C_in + BC - 1) / BC) *
-                                                ((a.C_out + BN - 1) / BN));
-  if (a.C_in % Row<T>::VEC == 0 && a.C_out % Row<T>::VEC == 0)
-    k_grouped_dw<T, BC, BN, true><<<blocks, kThreads, 0, a.st>>>(a);
+template <typename T> void run_dw(const WeightArgs& a, const DwPlan& p) {
+  const uint32_t blocks = static_cast<uint32_t>(p.jobs * p.tiles);
+  const bool dma = whole_rows<T>(a.x, a.C_in) && whole_rows<T>(a.dy, a.C_out);
+  if (p.tile == 256)
+    k_grouped_dw<T, 256, 256, 2, 4, true><<<blocks, 512, 0, a.st>>>(a);
+  else if (p.tile == 128 && dma)
+    k_grouped_dw<T, 128, 128, 2, 2, true><<<blocks, 256, 0, a.st>>>(a);
+  else if (p.tile == 128)
+    k_grouped_dw<T, 128, 128, 2, 2, false><<<blocks, 256, 0, a.st>>>(a);
+  else if (dma)
+    k_grouped_dw<T, 64, 64, 2, 2, true><<<blocks, 256, 0, a.st>>>(a);
   else
-    k_grouped_dw<T, BC, BN, false><<<blocks, kThreads, 0, a.st>>>(a);
+    k_grouped_dw<T, 64, 64, 2, 2, false><<<blocks, 256, 0, a.st>>>(a);
 }
 
 bool sizes_ok(int64_t m, int E, int C_in, int C_out) {
@@ -803,7 +1265,7 @@ extern "C" int spconv_grouped_forward(int in_dt, const void* x, int64_t n_x, con
   if (m == 0) return SPCONV_OK;
   return run_types<false>(in_dt, out_dt,
                           GroupedArgs{x, n_x, w, offsets, rows, bias, nullptr, relu, y, m, E, C_in,
-                                      C_out, 1, static_cast<hipStream_t>(stream)});
+                                      C_out, static_cast<hipStream_t>(stream)});
 }
 
 extern "C" int spconv_grouped_backward_data(int dt, const void* dy, const void* w,
@@ -818,13 +1280,16 @@ extern "C" int spconv_grouped_backward_data(int dt, const void* dy, const void* 
   if (m == 0) return SPCONV_OK;
   return run_types<true>(dt, out_dt,
                          GroupedArgs{dy, m, w, offsets, nullptr, nullptr, mask, 0, dx, m, E, C_out,
-                                     C_in, 1, static_cast<hipStream_t>(stream)});
+                                     C_in, static_cast<hipStream_t>(stream)});
 }
 
 extern "C" int spconv_grouped_backward_weight_workspace(int dt, int64_t m, int E, int C_in,
                                                         int C_out, size_t* bytes) {
   if (!dtype_ok(dt) || !sizes_ok(m, E, C_in, C_out) || !bytes) return SPCONV_EINVAL;
-  *bytes = dw_plan(dt, m, E, C_in, C_out).bytes;
+  // (the pointers are not known yet: enough for either kernel)
+  const size_t a = dw_plan(m, E, C_in, C_out, true).bytes;
+  const size_t b = dw_plan(m, E, C_in, C_out, false).bytes;
+  *bytes = a > b ? a : b;
   return SPCONV_OK;
 }
 
@@ -836,13 +1301,15 @@ extern "C" int spconv_grouped_backward_weight(int dt, const void* x, int64_t n_x
   if (!dtype_ok(dt) || !sizes_ok(m, E, C_in, C_out) || !rows_ok(n_x) || (!rows && n_x < m))
     return SPCONV_EINVAL;
   const size_t e = elem_bytes(dt);
-  const DwPlan plan = dw_plan(dt, m, E, C_in, C_out);
+  const bool wide = dt == SPCONV_BF16
+                        ? whole_rows<bf16_t>(x, C_in) && whole_rows<bf16_t>(dy, C_out)
+                        : whole_rows<float>(x, C_in) && whole_rows<float>(dy, C_out);
+  const DwPlan plan = dw_plan(m, E, C_in, C_out, wide);
   if (!ptr_ok(x, n_x, e) || !ptr_ok(dy, m, e) || !ptr_ok(offsets, 1, 4) || !aligned_to(rows, 4) ||
       !ptr_ok(dw, 1, 4) || !aligned_to(db, 4) ||
       (plan.bytes && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < plan.bytes)))
     return SPCONV_EINVAL;
-  const int64_t tiles = ((C_in + 63ll) / 64) * ((C_out + 63ll) / 64);
-  if (plan.jobs * tiles > 0x7fffffff) return SPCONV_EINVAL;
+  if (plan.jobs * plan.tiles > 0x7fffffff) return SPCONV_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   WeightArgs a{x, n_x, dy, offsets, rows, dw, db, m, plan.chunk, E, C_in, C_out, st};
   const int64_t per = static_cast<int64_t>(C_in) * C_out;
@@ -850,11 +1317,7 @@ extern "C" int spconv_grouped_backward_weight(int dt, const void* x, int64_t n_x
     a.dw = static_cast<float*>(workspace);
     a.db = db ? a.dw + plan.jobs * per : nullptr;
   }
-  const bool small = C_in <= 64 || C_out <= 64;
-  if (dt == SPCONV_BF16)
-    small ? run_dw<bf16_t, 64, 64>(a, plan.jobs) : run_dw<bf16_t, 128, 128>(a, plan.jobs);
-  else
-    small ? run_dw<float, 64, 64>(a, plan.jobs) : run_dw<float, 128, 128>(a, plan.jobs);
+  if (dt == SPCONV_BF16) run_dw<bf16_t>(a, plan); else run_dw<float>(a, plan);
   if (plan.chunk) {
     const dim3 grid(static_cast<uint32_t>((per + 4 * kThreads - 1) / (4 * kThreads)), E);
     k_grouped_dw_sum<<<grid, kThreads, 0, st>>>(a.dw, a.db, offsets, E, m, plan.chunk, per, C_out,

@@ -330,6 +330,59 @@ def test_grouped_large_groups_are_summed_in_chunks(dtype):
         assert torch.equal(gw, again[0]) and torch.equal(gb, again[1])
 
 
+@pytest.mark.parametrize("sizes,ci,co,dtype", [
+    # reductions of one to four stages kept in registers, several column tiles
+    ([9000, 0, 1, 8500, 127], 40, 136, "bf16"), ([17001, 60], 64, 264, "bf16"),
+    ([300, 16500], 128, 520, "bf16"), ([8192, 8193], 168, 200, "bf16"),
+    ([5000, 12000, 77], 256, 392, "bf16"),
+    # tiles of 256 x 256, and the fp32 kernels at the same sizes
+    ([70000, 61000, 300], 264, 144, "bf16"), ([17000, 90], 264, 144, "f32"),
+    ([20000, 513], 200, 328, "bf16")])
+def test_grouped_many_rows(sizes, ci, co, dtype):
+    dt = DT[dtype]
+    odt = torch.float32 if dt == torch.bfloat16 else torch.bfloat16
+    r, off, m, rows, x, w, b = _groups_case(sizes, ci, co, dt, 3, True, 70)
+    offd, rd = torch.from_numpy(off).int().cuda(), rows.int().cuda()
+    dy, mask = r(m, co, dtype=dt), r(m, ci, dtype=dt)
+    plain, mag = ref.grouped(_f64(x), _f64(w), off, rows, _f64(b), False)
+    (dx, dw, db), (mx, mw, mb) = ref.grouped_grad(_f64(x), _f64(dy), _f64(w), off, rows, None)
+    y = spc.grouped_forward(x.cuda(), w.cuda(), offd, rows=rd, bias=b.cuda(), relu=True)
+    _close(y, torch.where(plain < 0, 0.0, plain), mag, ci + 1, "y")
+    y = spc.grouped_forward(x.cuda(), w.cuda(), offd, rows=rd, bias=b.cuda(), out_dtype=odt)
+    _close(y, plain, mag, ci + 1, "y of another type")
+    # the same widths the other way: as an input gradient
+    wt = w.transpose(1, 2).contiguous()
+    back, mag = ref.grouped(_f64(dy), _f64(wt), off, None, None, False)
+    g = spc.grouped_backward_data(dy.cuda(), w.cuda(), offd, mask=mask.cuda())
+    _close(g, torch.where(mask.double() <= 0, 0.0, dx), mx, co, "dx")
+    g = spc.grouped_backward_data(dy.cuda(), w.cuda(), offd, out_dtype=odt)
+    _close(g, dx, mx, co, "dx of another type")
+    fwd_mask = r(m, co, dtype=dt)
+    xs = ref.take(x, rows, m)
+    (dx2, _, _), (mx2, _, _) = ref.grouped_grad(_f64(dy), _f64(xs), _f64(wt), off, None, None)
+    g = spc.grouped_backward_data(xs.cuda(), wt.cuda(), offd, mask=fwd_mask.cuda())
+    _close(g, torch.where(fwd_mask.double() <= 0, 0.0, dx2), mx2, ci, "dx, wide")
+    y = spc.grouped_forward(dy.cuda(), wt.cuda(), offd)
+    _close(y, back, mag, co, "y, narrow")
+    gw, gb = spc.grouped_backward_weight(x.cuda(), dy.cuda(), offd, rows=rd)
+    _close(gw, dw, mw, max(sizes), "dw")
+    _close(gb, db, mb, max(sizes), "db")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_grouped_few_rows(dtype):
+    """Up to a few dozen positions: one, several and all of them in a group, long reductions."""
+    for sizes, ci, co in (([0, 1, 0, 0, 2], 512, 200), ([32], 1030, 64), ([5, 0, 9, 1], 7, 2048),
+                          ([4, 4], 2500, 136), ([33], 96, 64)):
+        r, off, m, rows, x, w, b = _groups_case(sizes, ci, co, DT[dtype], 8, True, 1)
+        offd = torch.from_numpy(off).int().cuda()
+        for relu in (False, True):
+            y = spc.grouped_forward(x.cuda(), w.cuda(), offd, rows=rows.int().cuda(),
+                                    bias=b.cuda(), relu=relu)
+            want, mag = ref.grouped(_f64(x), _f64(w), off, rows, _f64(b), relu)
+            _close(y, want, mag, ci + 1, (sizes, ci, co))
+
+
 def test_grouped_no_rows_and_many_groups():
     for dt in DT.values():
         w = torch.randn(5, 16, 24).to(dt).cuda()
