@@ -41,6 +41,13 @@ template <typename T> __device__ __forceinline__ void store_piece(T* p, u32x4_t 
   __builtin_memcpy(p, &v, 16);
 }
 
+// The same past the caches' replacement order: for an output far larger than the
+// L2 cache, which would otherwise push out what is still to be read.
+template <typename T> __device__ __forceinline__ void store_piece_past(T* p, u32x4_t v) {
+  typedef uint32_t any_t __attribute__((ext_vector_type(4), aligned(2)));
+  __builtin_nontemporal_store(v, reinterpret_cast<any_t*>(p));
+}
+
 __device__ __forceinline__ void unpack(u32x4_t u, float (&v)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(u[i]);

@@ -214,11 +214,11 @@ __device__ __forceinline__ u32x4_t load_left(const T* p, int64_t left) {
     return v;
   }
 }
-template <typename TO>
+template <typename TO, bool PAST = false>
 __device__ __forceinline__ void store_left(TO* p, u32x4_t v, int64_t left) {
   constexpr int VO = Row<TO>::VEC;
   if (left >= VO) {
-    store_piece(p, v);
+    if (PAST) store_piece_past(p, v); else store_piece(p, v);
   } else {
     TO e[VO];
     __builtin_memcpy(e, &v, 16);
@@ -428,7 +428,7 @@ __device__ __forceinline__ void store_tile_rows(
             for (int e = 0; e < VO; ++e) v[e] = z[e] <= 0.0f ? 0.0f : v[e];
             u = pack(v);
           }
-          store_left(y + at[i], u, left[i]);
+          store_left<TO, (BM * BN > 128 * 128)>(y + at[i], u, left[i]);
         }
       }
     }
@@ -646,34 +646,38 @@ __device__ __forceinline__ void store_wave_rows(const f32x16 (&acc)[2][FM], cons
           for (int e = 0; e < VO; ++e) v[e] = z[e] <= 0.0f ? 0.0f : v[e];
           piece[t] = pack(v);
         }
-        if (t < rows) store_piece(y + static_cast<int64_t>(t) * a.cols, piece[t]);
+        if (t < rows) store_piece_past(y + static_cast<int64_t>(t) * a.cols, piece[t]);
       }
     }
   }
 }
 
-// Short reductions of bf16 (NK stages): a workgroup keeps its 64 * WR rows in
+// Short reductions of bf16 (NK stages of 32): a workgroup keeps its 256 rows in
 // registers, as fragments, and takes the columns `span` by 128 at a time.  Only
-// the weights go through LDS, kRing stages of them, all but one on their way while
-// that one is multiplied, and finished tiles leave from the registers: nothing in
-// the loop waits for memory asked for in the same tile.  (k_grouped would read the
-// rows once per 256 columns, wait for memory every stage, and drain and refill for
-// every tile of a few stages.)
-constexpr int short_ring(int nk) { return nk == 3 ? 3 : 4; }
-template <typename TO, bool BT, int NK, int WR, bool RELU, bool MASK>
-__global__ __launch_bounds__(128 * WR, 2) void k_grouped_short(GroupedArgs a, int span) {
+// the weights go through LDS, a ring of 6 or 8 stages of them, all but one on their
+// way while that one is multiplied, and finished tiles leave from the registers.
+// (k_grouped would read the rows once per 256 columns, and drain and refill for
+// every tile of a few stages.)  The ring is as long as that because a wave's loads
+// and stores are counted together and in order: with 4 stages of 64 ahead a stage
+// waited for the stores of the tile before, 669 us instead of 591 for 256 -> 1024
+// at 696,416 positions, and two workgroups of 128 rows a compute unit took 621.
+constexpr int kShortRows = 256;
+constexpr int short_ring(int nk) { return nk == 6 ? 6 : 8; }
+template <typename TO, bool BT, int NK, bool RELU, bool MASK>
+__global__ __launch_bounds__(512, 2) void k_grouped_short(GroupedArgs a, int span) {
   typedef bf16_t T;
   typedef Mma<T> M;
-  constexpr int BM = 64 * WR, BN = 128, NT = 128 * WR, WC = 2, FM = 2, FN = 2;
+  constexpr int BM = kShortRows, BN = 128, NT = 512, WC = 2, FM = 2, FN = 2;
   constexpr int kRing = short_ring(NK), U = kRing / NK;   // tiles until the ring repeats
-  constexpr int KB = 128;
+  constexpr int KB = 64;
   typedef RTile<T, BN, KB> TBr;
   typedef KTile<T, BN, KB> TBk;
   constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, STEPS = BK / M::KS;
   constexpr int PB = TBk::PIECES / NT;
   // (separate arrays, so that the compiler knows which loads a read waits for)
-  __shared__ u32x4_t s_w0[TBk::PIECES], s_w1[TBk::PIECES], s_w2[TBk::PIECES],
-      s_w3[kRing > 3 ? TBk::PIECES : 1];
+  constexpr int NP = TBk::PIECES;
+  __shared__ u32x4_t s_w0[NP], s_w1[NP], s_w2[NP], s_w3[NP], s_w4[NP], s_w5[NP],
+      s_w6[kRing > 6 ? NP : 1], s_w7[kRing > 6 ? NP : 1];
   const T* const x = static_cast<const T*>(a.x);
   Job j;
   if (!grouped_job<TO, BM>(a, span, &j)) return;
@@ -685,12 +689,13 @@ __global__ __launch_bounds__(128 * WR, 2) void k_grouped_short(GroupedArgs a, in
   // A lane's pieces of a weights' stage are those that belong at its place in LDS.
   // Stages past the last one are asked for too (as zeros or as columns of others),
   // so that the number of loads behind a stage's own is known.
-  const int ra0 = threadIdx.x >> 3, ka = ((threadIdx.x & 7) ^ ((ra0 >> 1) & 7)) * VEC;
+  constexpr int PR = TBr::PR;
+  const int ra0 = threadIdx.x / PR, ka = (TBr::at(ra0, threadIdx.x % PR) - ra0 * PR) * VEC;
   const int kb = threadIdx.x / TBk::PR;
   const int nb = (TBk::at(kb, threadIdx.x % TBk::PR) - kb * TBk::PR) * VEC;
   // (columns past the last one are read as others: nothing of them is stored)
   const int own = lane_place(BT ? ra0 * a.red + ka : kb * a.cols + nb);
-  const int next = BT ? NT / 8 * a.red : NT / TBk::PR * a.cols;
+  const int next = BT ? NT / PR * a.red : NT / TBk::PR * a.cols;
   auto request = [&](int k, int n0, u32x4_t* buf) {
     const bool whole = n0 + BN <= a.cols && (k + 1) * BK <= a.red;
     const T* const ws = w + (BT ? static_cast<int64_t>(n0) * a.red + k * BK
@@ -701,7 +706,7 @@ __global__ __launch_bounds__(128 * WR, 2) void k_grouped_short(GroupedArgs a, in
     } else {
 #pragma unroll
       for (int i = 0; i < PB; ++i) {
-        const int n = n0 + (BT ? ra0 + NT / 8 * i : nb);
+        const int n = n0 + (BT ? ra0 + NT / PR * i : nb);
         const int c = k * BK + (BT ? ka : kb + NT / TBk::PR * i);
         load_to_lds(n < a.cols && c < a.red ? ws + (own + i * next) : zero,
                     buf + NT * i + 64 * wave);
@@ -710,7 +715,10 @@ __global__ __launch_bounds__(128 * WR, 2) void k_grouped_short(GroupedArgs a, in
   };
   const std::conditional_t<BT, typename TBr::Reader, typename TBk::template Reader<32, FN>>
       weights_of(wc, lane);
-  auto ring = [&](int r) { return r == 0 ? s_w0 : r == 1 ? s_w1 : r == 2 ? s_w2 : s_w3; };
+  auto ring = [&](int r) {
+    return r < 4 ? (r < 2 ? (r ? s_w1 : s_w0) : (r > 2 ? s_w3 : s_w2))
+                 : (r < 6 ? (r > 4 ? s_w5 : s_w4) : (r > 6 ? s_w7 : s_w6));
+  };
   // A tile starts from its bias: lane i has that of column wc + i, asked for a
   // tile before.
   const float* const b = a.bias ? a.bias + static_cast<int64_t>(j.group) * a.cols : nullptr;
@@ -1177,21 +1185,17 @@ int run_grouped_any(const GroupedArgs& a) {
   return launched();
 }
 template <typename TO, bool BT, int NK> int run_grouped_short(const GroupedArgs& a) {
-  // 256 rows a workgroup; 128 where their fragments leave room for no more than
-  // the waves of one, so that another one multiplies while it stores
-  // (256 -> 1024, 696,416 positions: 663 us against 706; 64 -> 256: 137 against 124)
-  constexpr int WR = NK <= 2 ? 4 : 2, BM = 64 * WR;
   // all columns, or as many as leave eight workgroups a compute unit
-  const int64_t tiles = tile_bound(a.m, a.E + 1, BM), want = 2048 / tiles + 1;
+  const int64_t tiles = tile_bound(a.m, a.E + 1, kShortRows), want = 2048 / tiles + 1;
   const int ncol = (a.cols + 127) / 128;
   const int parts = static_cast<int>(want < ncol ? want : ncol);
   const int span = (ncol + parts - 1) / parts * 128;
   uint32_t blocks;
-  if (!grouped_grid<BM>(a, span, &blocks)) return SPCONV_EINVAL;
+  if (!grouped_grid<kShortRows>(a, span, &blocks)) return SPCONV_EINVAL;
   if (BT ? a.mask != nullptr : a.relu != 0)
-    k_grouped_short<TO, BT, NK, WR, !BT, BT><<<blocks, 128 * WR, 0, a.st>>>(a, span);
+    k_grouped_short<TO, BT, NK, !BT, BT><<<blocks, 512, 0, a.st>>>(a, span);
   else
-    k_grouped_short<TO, BT, NK, WR, false, false><<<blocks, 128 * WR, 0, a.st>>>(a, span);
+    k_grouped_short<TO, BT, NK, false, false><<<blocks, 512, 0, a.st>>>(a, span);
   return launched();
 }
 // Which kernel: k_grouped_any where pieces may be cut or unaligned; k_grouped_short
@@ -1208,11 +1212,10 @@ template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
   if (small) return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
   if constexpr (sizeof(T) == 2) {
     if (a.red <= 256 && a.cols > 128 && a.cols % Row<TO>::VEC == 0 && a.m >= 16384) {
-      const int nk = (a.red + kBK<T, 128> - 1) / kBK<T, 128>;
-      if (nk <= 1) return run_grouped_short<TO, BT, 1>(a);
-      if (nk <= 2) return run_grouped_short<TO, BT, 2>(a);
-      if (nk <= 3) return run_grouped_short<TO, BT, 3>(a);
-      return run_grouped_short<TO, BT, 4>(a);
+      if (a.red <= 64) return run_grouped_short<TO, BT, 2>(a);
+      if (a.red <= 128) return run_grouped_short<TO, BT, 4>(a);
+      if (a.red <= 192) return run_grouped_short<TO, BT, 6>(a);
+      return run_grouped_short<TO, BT, 8>(a);
     }
     const int64_t c256 = (a.cols + 255) / 256, c128 = (a.cols + 127) / 128;
     if (20 * c256 <= 11 * c128 + 1 && a.m / 256 * c256 >= 512)
