@@ -135,61 +135,87 @@ __global__ __launch_bounds__(kThreads) void k_route(
 #pragma unroll
     for (int q = 0; q < kWaves; ++q) s_count[q][e] = 0;
 
-  for (int q = threadIdx.x / LPR; q < nrow; q += G) {   // (a group's lanes stay together)
-    const int64_t r = row0 + q;
-    uint32_t o[NV][VEC];
+  // UR rows of a group at a time, for their chains of lane exchanges to overlap, and
+  // the next ones' logits on their way meanwhile (a group's lanes stay together).
+  constexpr int UR = NV == 1 ? 2 : 1;
+  float next[UR][NV][VEC];
+  auto request = [&](int q0) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = (lane + LPR * j) * VEC;
-      float v[VEC];
+    for (int u = 0; u < UR; ++u)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = 0.0f;
-      if (c < E) load_row<T, TAIL>(logits + r * E, c, E, v);
+      for (int j = 0; j < NV; ++j) {
+        const int q = q0 + G * u, c = (lane + LPR * j) * VEC;
+        if (q < nrow && c < E) load_row<T, TAIL>(logits + (row0 + q) * E, c, E, next[u][j]);
+      }
+  };
+  request(threadIdx.x / LPR);
+  for (int q0 = threadIdx.x / LPR; q0 < nrow; q0 += G * UR) {
+    uint32_t o[UR][NV][VEC];
+    float top[UR], sum[UR];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) o[j][i] = c + i < E ? order_of(v[i]) : 0u;
+    for (int u = 0; u < UR; ++u) {
+      sum[u] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+          o[u][j][i] = (lane + LPR * j) * VEC + i < E ? order_of(next[u][j][i]) : 0u;
     }
-    float top = 0.0f, sum = 0.0f;
+    request(q0 + G * UR);
     for (int s = 0; s < k; ++s) {
-      uint32_t bo = 0, bc = 0xffffffffu;
+      uint32_t bo[UR], bc[UR];
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
+      for (int u = 0; u < UR; ++u) {
+        bo[u] = 0;
+        bc[u] = 0xffffffffu;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          if (o[j][i] > bo) {                      // ascending columns: the lowest of equals
-            bo = o[j][i];
-            bc = (lane + LPR * j) * VEC + i;
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i)
+            if (o[u][j][i] > bo[u]) {              // ascending columns: the lowest of equals
+              bo[u] = o[u][j][i];
+              bc[u] = (lane + LPR * j) * VEC + i;
+            }
+        group_best<LPR>(bo[u], bc[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < UR; ++u) {
+        const bool some = bo[u] > kNone;
+        const float v = value_of(bo[u]);
+        if (s == 0) {
+          top[u] = some ? v : 0.0f;
+          if (!normalize) {
+            // the whole row's sum, before anything is taken out of it
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+              for (int i = 0; i < VEC; ++i)
+                if (o[u][j][i]) sum[u] += expf(value_of(o[u][j][i]) - top[u]);
+            sum[u] = group_sum<LPR>(sum[u]);
           }
-      group_best<LPR>(bo, bc);
-      const bool some = bo > kNone;
-      const float v = value_of(bo);
-      if (s == 0) {
-        top = some ? v : 0.0f;
-        if (!normalize) {
-          // the whole row's sum, before anything is taken out of it
-#pragma unroll
-          for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-              if (o[j][i]) sum += expf(value_of(o[j][i]) - top);
-          sum = group_sum<LPR>(sum);
         }
-      }
-      const float w = some ? expf(v - top) : 0.0f;
-      if (normalize) sum += w;
-      if (lane == s % LPR) {
-        s_expert[q * k + s] = static_cast<int16_t>(some ? static_cast<int32_t>(bc) : -1);
-        s_weight[q * k + s] = w;
-      }
-      // take it out
+        const float w = some ? expf(v - top[u]) : 0.0f;
+        if (normalize) sum[u] += w;
+        const int q = q0 + G * u;
+        if (lane == s % LPR && q < nrow) {
+          s_expert[q * k + s] = static_cast<int16_t>(some ? static_cast<int32_t>(bc[u]) : -1);
+          s_weight[q * k + s] = w;
+        }
+        // take it out
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          if (static_cast<uint32_t>((lane + LPR * j) * VEC + i) == bc) o[j][i] = 0u;
+          for (int i = 0; i < VEC; ++i)
+            if (static_cast<uint32_t>((lane + LPR * j) * VEC + i) == bc[u]) o[u][j][i] = 0u;
+      }
     }
     // (each lane divides the slots it wrote)
-    for (int s = lane; s < k; s += LPR)
-      if (s_expert[q * k + s] >= 0) s_weight[q * k + s] /= sum;
+#pragma unroll
+    for (int u = 0; u < UR; ++u) {
+      const int q = q0 + G * u;
+      for (int s = lane; s < k && q < nrow; s += LPR)
+        if (s_expert[q * k + s] >= 0) s_weight[q * k + s] /= sum[u];
+    }
   }
   __syncthreads();
   const int npair = nrow * k, wave = threadIdx.x >> 6, wl = threadIdx.x & 63;
@@ -432,17 +458,19 @@ template <typename T, int LPR, int NV> void run(const Bwd& a) {
     k_route_bwd<T, LPR, NV, false><<<blocks, kThreads, 0, a.st>>>(
         a.dweights, l, a.experts, a.weights, a.n, a.E, a.k, a.normalize, d);
 }
-// The fewest lanes whose registers hold the row, one piece a lane up to a wave.
+// Up to four pieces a lane, then more lanes: a step of the exchange between lanes
+// costs a wave the same for 4 rows as for 16 (64 fp32 logits, 348,208 rows: four
+// lanes a row 31 us, sixteen with a piece each 48).
 template <typename T, typename A> void by_width(const A& a) {
   const int pieces = (a.E + Row<T>::VEC - 1) / Row<T>::VEC;
   if (pieces <= 1) return run<T, 1, 1>(a);
-  if (pieces <= 2) return run<T, 2, 1>(a);
-  if (pieces <= 4) return run<T, 4, 1>(a);
-  if (pieces <= 8) return run<T, 8, 1>(a);
-  if (pieces <= 16) return run<T, 16, 1>(a);
-  if (pieces <= 32) return run<T, 32, 1>(a);
-  if (pieces <= 64) return run<T, 64, 1>(a);
-  if (pieces <= 128) return run<T, 64, 2>(a);
+  if (pieces <= 2) return run<T, 1, 2>(a);
+  if (pieces <= 4) return run<T, 1, 4>(a);
+  if (pieces <= 8) return run<T, 2, 4>(a);
+  if (pieces <= 16) return run<T, 4, 4>(a);
+  if (pieces <= 32) return run<T, 8, 4>(a);
+  if (pieces <= 64) return run<T, 16, 4>(a);
+  if (pieces <= 128) return run<T, 32, 4>(a);
   if constexpr (Row<T>::VEC == 4) run<T, 64, 4>(a);
 }
 
