@@ -454,7 +454,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped(GroupedArgs a) {
   // (the first one also takes the finished tile; separate arrays, so that the
   // compiler knows which loads a read waits for)
   constexpr int kOut = BM * BN * static_cast<int>(sizeof(TO)) / 16;
-  constexpr int NP0 = kOut > NP && BM * BN <= 128 * 128 ? (kOut > 2 * NP ? 2 * NP : kOut) : NP;
+  constexpr int NP0 = kOut > NP && BM == 64 ? kOut : NP;
   __shared__ u32x4_t s_buf0[NP0], s_buf1[NP], s_buf2[NP], s_buf3[NP];
   __shared__ __attribute__((aligned(16))) float s_bias[BN];
   const T* const x = static_cast<const T*>(a.x);
@@ -1054,106 +1054,123 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped_dw(WeightArgs a) {
     }
 }
 
-// The chunks' sums of a group, in ascending order: dw | db of one group as a
-// row of C_in * C_out + C_out values, four a lane.
+// The chunks' sums of a group: kThreads / RUNS lanes side by side with four values
+// each, RUNS of them down the chunks, every RUNS-th one each, then those in order.
+// The first workgroup of a group also adds up the bias gradient.  (Eight runs
+// where few values have many chunks: 29 us of a gradient of 64 x 256 became 9.)
+template <int RUNS>
 __global__ __launch_bounds__(kThreads) void k_grouped_dw_sum(
     const float* __restrict__ part, const float* __restrict__ part_db,
     const int32_t* __restrict__ offsets, int E, int64_t m, int64_t chunk, int64_t per, int C_out,
     float* __restrict__ dw, float* __restrict__ db) {
-  __shared__ int64_t s_first, s_count;
-  const int e = blockIdx.y;
-  if (threadIdx.x < 64) {
-    // chunks before group e, and its own
-    int64_t before = 0, own = 0;
-    for (int g = threadIdx.x; g <= e; g += 64) {
-      int64_t b = offsets[g], f = offsets[g + 1];
-      b = b < 0 ? 0 : b > m ? m : b;
-      f = f < b ? b : f > m ? m : f;
-      const int64_t c = (f - b + chunk - 1) / chunk;
-      if (g < e) before += c; else own = c;
-    }
+  constexpr int kLanes = kThreads / RUNS;
+  __shared__ f32x4_t s_sum[RUNS][kLanes];
+  const int e = blockIdx.y, lane = threadIdx.x % kLanes, run = threadIdx.x / kLanes;
+  // chunks before group e, and its own (every wave finds them)
+  int64_t first = 0, count = 0;
+  for (int g = threadIdx.x & 63; g <= e; g += 64) {
+    int64_t b = offsets[g], f = offsets[g + 1];
+    b = b < 0 ? 0 : b > m ? m : b;
+    f = f < b ? b : f > m ? m : f;
+    const int64_t c = (f - b + chunk - 1) / chunk;
+    if (g < e) first += c; else count = c;
+  }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      before += __shfl_xor(before, d, 64);
-      own += __shfl_xor(own, d, 64);
-    }
-    if (threadIdx.x == 0) {
-      s_first = before;
-      s_count = own;
-    }
+  for (int d = 1; d < 64; d *= 2) {
+    first += __shfl_xor(first, d, 64);
+    count += __shfl_xor(count, d, 64);
   }
-  __syncthreads();
-  const int64_t first = s_first, count = s_count;
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
-  if (i < per) {
+  auto add = [&](const float* p, int64_t width, int64_t i, float* out) {
     f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (i + 4 <= per) {
+    if (i + 4 <= width) {
 #pragma unroll 4
-      for (int64_t c = 0; c < count; ++c)
-        a += __builtin_bit_cast(f32x4_t, load_piece(part + (first + c) * per + i));
-      store_piece(dw + e * per + i, __builtin_bit_cast(u32x4_t, a));
+      for (int64_t c = run; c < count; c += RUNS)
+        a += __builtin_bit_cast(f32x4_t, load_piece(p + (first + c) * width + i));
     } else {
-      for (int64_t j = i; j < per; ++j) {
-        float s = 0.0f;
-        for (int64_t c = 0; c < count; ++c) s += part[(first + c) * per + j];
-        dw[e * per + j] = s;
-      }
+      for (int64_t c = run; c < count; c += RUNS)
+        for (int q = 0; q < 4 && i + q < width; ++q) a[q] += p[(first + c) * width + i + q];
     }
-  }
-  if (db && blockIdx.x == 0) {
-    for (int n = threadIdx.x; n < C_out; n += kThreads) {
-      float s = 0.0f;
-      for (int64_t c = 0; c < count; ++c) s += part_db[(first + c) * C_out + n];
-      db[static_cast<int64_t>(e) * C_out + n] = s;
+    if constexpr (RUNS > 1) {
+      s_sum[run][lane] = a;
+      __syncthreads();
     }
-  }
+    if (run == 0 && i < width) {
+#pragma unroll
+      for (int q = 1; q < RUNS; ++q) a += s_sum[q][lane];
+      store_left(out + e * width + i, __builtin_bit_cast(u32x4_t, a), width - i);
+    }
+    if constexpr (RUNS > 1) __syncthreads();
+  };
+  add(part, per, (static_cast<int64_t>(blockIdx.x) * kLanes + lane) * 4, dw);
+  if (db && blockIdx.x == 0)
+    for (int64_t c = 0; c < C_out; c += kLanes * 4) add(part_db, C_out, c + lane * 4, db);
 }
 
-// How the weight gradient cuts its groups: tiles of dw of 256 x 256, 128 x 128 or
-// 64 x 64, the largest that fill the card; chunk = 0 where the groups' own tiles
-// do or there is little to sum, else positions per chunk.
+// How the weight gradient is cut: tiles of dw of 64, 128 or (bf16, whole pieces)
+// 256 squared, and the positions of a group into chunks (chunk = 0: each group is
+// one, and its sums go straight to dw).
 struct DwPlan {
   int tile;
   int64_t chunk, jobs, tiles;
   size_t bytes;
 };
-DwPlan dw_plan(int64_t m, int E, int C_in, int C_out, bool wide) {
-  const int64_t widest = C_in < C_out ? C_out : C_in, least = C_in < C_out ? C_in : C_out;
-  DwPlan p;
-  p.tile = wide && least > 128 && m > 16384 ? 256 : least > 64 && widest > 64 ? 128 : 64;
-  p.tiles = ((C_in + p.tile - 1ll) / p.tile) * ((C_out + p.tile - 1ll) / p.tile);
-  p.chunk = 0;
-  p.jobs = E;
-  p.bytes = 0;
-  if (m <= 1024) return p;
-  // Rounds of the card's workgroups (one, two or four a compute unit) times a
-  // chunk's positions, and what the chunks' sums cost to write and read: a
-  // position takes about 0.04 us of a 256 x 256 tile, a workgroup 8 us besides
-  // them, the sums 4 MB a us.  Without chunks a workgroup can have twice the mean.
-  const int64_t slots = p.tile == 256 ? 256 : p.tile == 128 ? 512 : 1024;
-  const double pos = p.tile == 256 ? 0.04 : p.tile == 128 ? 0.02 : 0.01, fixed = 8.0;
-  const double per = (static_cast<double>(C_in) * C_out + C_out) * 8.0 / 4e6;
-  const int64_t groups = E < m ? E : m;
-  const double mean = static_cast<double>(m) / groups;
-  const double work = static_cast<double>((groups * p.tiles + slots - 1) / slots);
-  double best = (work < 2.0 ? 2.0 : work) * (mean * pos + fixed);
-  if (groups == 1) best = work * (mean * pos + fixed);
-  for (int rounds = 1; rounds <= 8; ++rounds) {
-    const int64_t chunks = rounds * slots / p.tiles - groups;
-    if (chunks < 1) continue;
-    int64_t chunk = (m + chunks - 1) / chunks;
-    chunk = (chunk + 63) / 64 * 64;
-    const int64_t jobs = m / chunk + groups;
-    const double cost = rounds * (chunk * pos + fixed) + jobs * per;
-    if (cost < best) {
-      best = cost;
-      p.chunk = chunk;
-      p.jobs = jobs;
+// The estimate it is chosen by, in us.  A stage of a tile (128 bytes: 16 or 32
+// positions) takes `alone` with one workgroup a compute unit and `full` with as
+// many as fit; a workgroup 3 us besides its stages; the chunks' sums are written
+// and read at 4 MB a us.  A group may have three times the mean.  (Measured at
+// 1,000 to 696,416 positions, 64 x 256 to 2048 x 2048: within 15 % of the best of
+// all tiles and chunks tried.)
+double dw_cost(bool f32, int64_t m, int64_t groups, double values, int tile, double tiles,
+               int64_t chunk) {
+  const int t = tile == 64 ? 0 : tile == 128 ? 1 : 2;
+  static const double alone[2][3] = {{0.63, 0.98, 1.27}, {0.75, 1.6, 4.0}};
+  static const double full[2][3] = {{0.8, 1.2, 1.5}, {1.35, 2.2, 4.2}};
+  const double stage = f32 ? 16.0 : 32.0, slots = t == 0 ? 1024.0 : t == 1 ? 512.0 : 256.0;
+  const double mean = static_cast<double>(m) / groups, longest = groups > 1 ? 3.0 * mean : mean;
+  const double jobs = chunk ? static_cast<double>(m) / chunk + groups : groups;
+  const double rounds = jobs * tiles / slots, fill = rounds < 1.0 ? rounds : 1.0;
+  const double us = alone[f32][t] + (full[f32][t] - alone[f32][t]) * fill;
+  const double length = chunk && chunk < longest ? static_cast<double>(chunk) : longest;
+  const double unit = length / stage * us + 3.0, even = mean / stage * us + 3.0;
+  if (!chunk) return rounds * even > unit ? rounds * even : unit;
+  const double whole = static_cast<double>(static_cast<int64_t>(rounds)) + (rounds > 3.0 ? 0.5 : 1.0);
+  return unit * whole + 4.0 + jobs * values * 8.0 / 4e6;
+}
+DwPlan dw_plan(int dt, int64_t m, int E, int C_in, int C_out, bool wide) {
+  const bool f32 = dt == SPCONV_F32;
+  const int64_t groups = m < 1 ? 1 : E < m ? E : m;
+  const double values = static_cast<double>(C_in) * C_out + C_out;
+  const int64_t least = C_in < C_out ? C_in : C_out, widest = C_in < C_out ? C_out : C_in;
+  DwPlan best{64, 0, E, 0, 0};
+  double cost = 0.0;
+  auto consider = [&](int tile, int64_t tiles, int64_t chunk) {
+    const double c = dw_cost(f32, m, groups, values, tile, static_cast<double>(tiles), chunk);
+    if (best.tiles && !(c < cost)) return;
+    cost = c;
+    best.tile = tile;
+    best.tiles = tiles;
+    best.chunk = chunk;
+  };
+  for (int tile = 64; tile <= 256; tile *= 2) {
+    if (tile == 128 && widest <= 64) break;
+    if (tile == 256 && (f32 || !wide || least <= 128)) break;
+    const int64_t tiles = ((C_in + tile - 1ll) / tile) * ((C_out + tile - 1ll) / tile);
+    consider(tile, tiles, 0);
+    for (int64_t chunk = 64; chunk < m; chunk *= 2) consider(tile, tiles, chunk);
+    // and what fills one to four rounds of the card
+    const int64_t slots = tile == 64 ? 1024 : tile == 128 ? 512 : 256;
+    for (int rounds = 1; rounds <= 4; ++rounds) {
+      const int64_t chunks = rounds * slots / tiles - groups;
+      const int64_t chunk = chunks > 0 ? ((m + chunks - 1) / chunks + 63) / 64 * 64 : 0;
+      // (one less than a whole number of rounds, by the estimate's rounding up)
+      if (chunk && chunk < m) consider(tile, tiles, chunk + 64);
     }
   }
-  if (p.chunk)
-    p.bytes = static_cast<size_t>(p.jobs) * (static_cast<size_t>(C_in) * C_out + C_out) * 4;
-  return p;
+  if (best.chunk) {
+    best.jobs = m / best.chunk + groups;
+    best.bytes = static_cast<size_t>(best.jobs) * (static_cast<size_t>(C_in) * C_out + C_out) * 4;
+  }
+  return best;
 }
 
 // (groups never have more tiles than this)
@@ -1200,16 +1217,21 @@ template <typename TO, bool BT, int NK> int run_grouped_short(const GroupedArgs&
 }
 // Which kernel: k_grouped_any where pieces may be cut or unaligned; k_grouped_short
 // for bf16 reductions of at most 256 and more than one column tile, of many rows
-// (256 -> 1024, 696,416 positions: 663 us against 847); else k_grouped with tiles
-// of 256 x 256 where they fill the card twice and waste little of their last
-// columns (bf16 2048 -> 2048, 65,536 positions: 603 us against 692 with 128 x 128,
-// of which two fit a compute unit; fp32, bound by its products, 433 against 341 the
-// other way), 64 x 64 for few rows a group or few columns, 128 x 128 otherwise.
+// (256 -> 1024, 696,416 positions: 570 us against 847); else k_grouped.  Its tiles
+// are 64 x 64 for fp32, whose products bound it and hide everything else best with
+// many waves (512 -> 512, 65,536 positions: 365 us against 404 with 128 x 128), for
+// few columns, and for bf16 where 128 x 128 would not fill the card twice (512 ->
+// 512, 8,000 positions: 20 us against 26); 256 x 256 where they do and waste little
+// of their last columns (2048 -> 2048, 65,536 positions: 603 us against 692).
 template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
-  const bool small = a.cols <= 64 || a.m <= 64ll * a.E;
-  if (!whole_rows<T>(a.x, a.red) || !whole_rows<T>(a.w, BT ? a.red : a.cols))
-    return small ? run_grouped_any<T, TO, BT, 64, 64>(a) : run_grouped_any<T, TO, BT, 128, 128>(a);
-  if (small) return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
+  const int64_t c256 = (a.cols + 255) / 256, c128 = (a.cols + 127) / 128;
+  const bool small = sizeof(T) == 4 || a.cols <= 64 || a.m <= 64ll * a.E ||
+                     tile_bound(a.m, a.E, 128) * c128 < 1024;
+  if (!whole_rows<T>(a.x, a.red) || !whole_rows<T>(a.w, BT ? a.red : a.cols)) {
+    if constexpr (sizeof(T) == 2)
+      if (!small) return run_grouped_any<T, TO, BT, 128, 128>(a);
+    return run_grouped_any<T, TO, BT, 64, 64>(a);
+  }
   if constexpr (sizeof(T) == 2) {
     if (a.red <= 256 && a.cols > 128 && a.cols % Row<TO>::VEC == 0 && a.m >= 16384) {
       if (a.red <= 64) return run_grouped_short<TO, BT, 2>(a);
@@ -1217,11 +1239,13 @@ template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
       if (a.red <= 192) return run_grouped_short<TO, BT, 6>(a);
       return run_grouped_short<TO, BT, 8>(a);
     }
-    const int64_t c256 = (a.cols + 255) / 256, c128 = (a.cols + 127) / 128;
-    if (20 * c256 <= 11 * c128 + 1 && a.m / 256 * c256 >= 512)
-      return run_grouped<T, TO, BT, 256, 256, 2, 4>(a);
+    if (!small) {
+      if (20 * c256 <= 11 * c128 + 1 && a.m / 256 * c256 >= 512)
+        return run_grouped<T, TO, BT, 256, 256, 2, 4>(a);
+      return run_grouped<T, TO, BT, 128, 128, 2, 2>(a);
+    }
   }
-  return run_grouped<T, TO, BT, 128, 128, 2, 2>(a);
+  return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
 }
 template <bool BT> int run_types(int in_dt, int out_dt, const GroupedArgs& a) {
   if (in_dt == SPCONV_BF16)
@@ -1232,9 +1256,13 @@ template <bool BT> int run_types(int in_dt, int out_dt, const GroupedArgs& a) {
 template <typename T> void run_dw(const WeightArgs& a, const DwPlan& p) {
   const uint32_t blocks = static_cast<uint32_t>(p.jobs * p.tiles);
   const bool dma = whole_rows<T>(a.x, a.C_in) && whole_rows<T>(a.dy, a.C_out);
-  if (p.tile == 256)
-    k_grouped_dw<T, 256, 256, 2, 4, true><<<blocks, 512, 0, a.st>>>(a);
-  else if (p.tile == 128 && dma)
+  if constexpr (sizeof(T) == 2) {
+    if (p.tile == 256) {
+      k_grouped_dw<T, 256, 256, 2, 4, true><<<blocks, 512, 0, a.st>>>(a);
+      return;
+    }
+  }
+  if (p.tile == 128 && dma)
     k_grouped_dw<T, 128, 128, 2, 2, true><<<blocks, 256, 0, a.st>>>(a);
   else if (p.tile == 128)
     k_grouped_dw<T, 128, 128, 2, 2, false><<<blocks, 256, 0, a.st>>>(a);
@@ -1290,8 +1318,8 @@ extern "C" int spconv_grouped_backward_weight_workspace(int dt, int64_t m, int E
                                                         int C_out, size_t* bytes) {
   if (!dtype_ok(dt) || !sizes_ok(m, E, C_in, C_out) || !bytes) return SPCONV_EINVAL;
   // (the pointers are not known yet: enough for either kernel)
-  const size_t a = dw_plan(m, E, C_in, C_out, true).bytes;
-  const size_t b = dw_plan(m, E, C_in, C_out, false).bytes;
+  const size_t a = dw_plan(dt, m, E, C_in, C_out, true).bytes;
+  const size_t b = dw_plan(dt, m, E, C_in, C_out, false).bytes;
   *bytes = a > b ? a : b;
   return SPCONV_OK;
 }
@@ -1307,7 +1335,7 @@ extern "C" int spconv_grouped_backward_weight(int dt, const void* x, int64_t n_x
   const bool wide = dt == SPCONV_BF16
                         ? whole_rows<bf16_t>(x, C_in) && whole_rows<bf16_t>(dy, C_out)
                         : whole_rows<float>(x, C_in) && whole_rows<float>(dy, C_out);
-  const DwPlan plan = dw_plan(m, E, C_in, C_out, wide);
+  const DwPlan plan = dw_plan(dt, m, E, C_in, C_out, wide);
   if (!ptr_ok(x, n_x, e) || !ptr_ok(dy, m, e) || !ptr_ok(offsets, 1, 4) || !aligned_to(rows, 4) ||
       !ptr_ok(dw, 1, 4) || !aligned_to(db, 4) ||
       (plan.bytes && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < plan.bytes)))
@@ -1322,9 +1350,14 @@ extern "C" int spconv_grouped_backward_weight(int dt, const void* x, int64_t n_x
   }
   if (dt == SPCONV_BF16) run_dw<bf16_t>(a, plan); else run_dw<float>(a, plan);
   if (plan.chunk) {
-    const dim3 grid(static_cast<uint32_t>((per + 4 * kThreads - 1) / (4 * kThreads)), E);
-    k_grouped_dw_sum<<<grid, kThreads, 0, st>>>(a.dw, a.db, offsets, E, m, plan.chunk, per, C_out,
-                                               dw, db);
+    const uint32_t wide_grid = static_cast<uint32_t>((per + 4 * kThreads - 1) / (4 * kThreads));
+    const dim3 many(static_cast<uint32_t>((per + kThreads / 2 - 1) / (kThreads / 2)), E);
+    if (static_cast<int64_t>(wide_grid) * E < 1024 && plan.jobs > 4ll * E)
+      k_grouped_dw_sum<8><<<many, kThreads, 0, st>>>(a.dw, a.db, offsets, E, m, plan.chunk, per,
+                                                     C_out, dw, db);
+    else
+      k_grouped_dw_sum<1><<<dim3(wide_grid, E), kThreads, 0, st>>>(
+          a.dw, a.db, offsets, E, m, plan.chunk, per, C_out, dw, db);
   }
   return launched();
 }
