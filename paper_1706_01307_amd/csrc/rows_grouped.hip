@@ -864,6 +864,95 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_any(GroupedArgs a) {
   store_tile_rows<TO, BM, BN, 2, 2, NP * 16>(s_buf, acc, s_bias, a, j, n0);
 }
 
+// Few positions in all (a row at a time through its experts): the weights' bytes,
+// once, and the time to the last of them are all there is.  A workgroup of 16 waves
+// takes up to 4 positions of a group and 64 bytes of columns, 4 lanes side by side;
+// its 256 slices of the reduction run down the weights' rows on the vector ALU, 8
+// loads of a slice in flight, and are added over the lanes, then the waves, in
+// order.  (The tiles' chain of stages took 48 us for one fp32 position of 2048 ->
+// 512, this 7.8.)
+constexpr int kFewThreads = 1024;
+// v of lane i + D within 16 lanes (rotating), D = 4 or 8
+template <int D> __device__ __forceinline__ float row_rotate(float v) {
+  return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_update_dpp(
+      0, static_cast<int>(__float_as_uint(v)), 0x120 | D, 0xf, 0xf, true)));
+}
+template <typename T, typename TO>
+__global__ __launch_bounds__(kFewThreads) void k_grouped_few(GroupedArgs a) {
+  constexpr int VEC = Row<T>::VEC, R = 4, CL = 4, NC = CL * VEC, KS = kFewThreads / CL;
+  constexpr int KC = 2048, UN = 8;                 // of the reduction in LDS; loads in flight
+  constexpr int NW = kFewThreads / 64;
+  __shared__ float s_x[R][KC];
+  __shared__ float s_sum[NW][R][NC];
+  const T* const x = static_cast<const T*>(a.x);
+  Job j;
+  if (!grouped_job<TO, R>(a, NC, &j)) return;
+  const T* const w = static_cast<const T*>(a.w) + static_cast<int64_t>(j.group) * a.red * a.cols;
+  const int slice = threadIdx.x / CL, c = j.n0 + threadIdx.x % CL * VEC;
+  float acc[R][VEC];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[r][i] = 0.0f;
+  const int sr = threadIdx.x / (kFewThreads / R);  // the row a lane stages
+  const int64_t src = source_row(a, j, sr);
+  for (int k0 = 0; k0 < a.red; k0 += KC) {
+    const int kc = a.red - k0 < KC ? a.red - k0 : KC;
+    __syncthreads();
+    for (int k = threadIdx.x % (kFewThreads / R); k < kc; k += kFewThreads / R)
+      s_x[sr][k] = src >= 0 ? Row<T>::get(x[src * a.red + k0 + k]) : 0.0f;
+    __syncthreads();
+    for (int k1 = slice; k1 < kc; k1 += KS * UN) {
+      u32x4_t u[UN];
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        const int k = k1 + KS * i;
+        u[i] = load_piece(k < kc && c < a.cols ? w + static_cast<int64_t>(k0 + k) * a.cols + c
+                                               : reinterpret_cast<const T*>(&g_zeros));
+      }
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        const int k = k1 + KS * i;
+        if (k >= kc) break;
+        float v[VEC];
+        unpack(u[i], v);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[r][e] = fmaf(s_x[r][k], v[e], acc[r][e]);
+      }
+    }
+  }
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float v = acc[r][e];
+      v += row_rotate<8>(v);
+      v += row_rotate<4>(v);
+      const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                      false);
+      v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+      const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                      false);
+      v = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+      if (lane < CL) s_sum[wave][r][lane * VEC + e] = v;
+    }
+  __syncthreads();
+  TO* const y = static_cast<TO*>(a.y);
+  if (threadIdx.x < R * NC) {
+    const int r = threadIdx.x / NC, col = j.n0 + threadIdx.x % NC;
+    if (r >= j.nrow || col >= a.cols) return;
+    float z = 0.0f;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) z += s_sum[q][r][threadIdx.x % NC];
+    if (a.bias) z += a.bias[static_cast<int64_t>(j.group) * a.cols + col];
+    if (a.relu && z < 0.0f) z = 0.0f;
+    y[(j.begin + r) * a.cols + col] = Row<TO>::put(z);
+  }
+}
+
 // Weight gradient of a BC x BN tile of one group, over a chunk of its
 // positions: dw[c][n] = sum_j x[row j][c] dy[j][n].  Both operands are staged
 // with the positions as the reduction's rows.  Chunk `job` leaves its sums as
@@ -1215,7 +1304,20 @@ template <typename TO, bool BT, int NK> int run_grouped_short(const GroupedArgs&
     k_grouped_short<TO, BT, NK, false, false><<<blocks, 512, 0, a.st>>>(a, span);
   return launched();
 }
-// Which kernel: k_grouped_any where pieces may be cut or unaligned; k_grouped_short
+// Whether k_grouped_few is the faster for at most 32 positions of whole pieces, by
+// an estimate of both in us: tiles take 0.2 (bf16) or 0.34 a stage however few rows
+// they have; the few kernel's workgroups, above 64 of them, take turns.  (One
+// position, 2048 -> 512: bf16 17.2 and 9.7 us, fp32 48 and 7.8; four of as many
+// groups, 512 -> 2048: bf16 8.3 and 14.6.)
+inline bool few_is_faster(const GroupedArgs& a, size_t bytes) {
+  const int64_t piece = 16 / static_cast<int64_t>(bytes);
+  if (a.m > 32 || a.cols % piece) return false;
+  const double tiles = 5.0 + (bytes == 2 ? 0.2 / 32 : 0.34 / 16) * a.red;
+  const double blocks = static_cast<double>(tile_bound(a.m, a.E, 4)) * a.cols / (4 * piece);
+  const double k = a.red / 2048.0, over = blocks > 64 ? (blocks - 64) / 192 : 0.0;
+  return 6.4 + 2.5 * k + over * (4.0 + 10.0 * k) < tiles;
+}
+// Which kernel: k_grouped_few by the estimate above; k_grouped_any where pieces may be cut or unaligned; k_grouped_short
 // for bf16 reductions of at most 256 and more than one column tile, of many rows
 // (256 -> 1024, 696,416 positions: 570 us against 847); else k_grouped.  Its tiles
 // are 64 x 64 for fp32, whose products bound it and hide everything else best with
@@ -1224,6 +1326,13 @@ template <typename TO, bool BT, int NK> int run_grouped_short(const GroupedArgs&
 // 512, 8,000 positions: 20 us against 26); 256 x 256 where they do and waste little
 // of their last columns (2048 -> 2048, 65,536 positions: 603 us against 692).
 template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
+  if constexpr (!BT) {
+    uint32_t blocks;
+    if (few_is_faster(a, sizeof(T)) && grouped_grid<4>(a, 4 * Row<T>::VEC, &blocks)) {
+      k_grouped_few<T, TO><<<blocks, kFewThreads, 0, a.st>>>(a);
+      return launched();
+    }
+  }
   const int64_t c256 = (a.cols + 255) / 256, c128 = (a.cols + 127) / 128;
   const bool small = sizeof(T) == 4 || a.cols <= 64 || a.m <= 64ll * a.E ||
                      tile_bound(a.m, a.E, 128) * c128 < 1024;
