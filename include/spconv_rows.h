@@ -33,7 +33,9 @@
  * Indices. offsets, rows and pos are read on the device.  Entries out of range
  *          are never followed (each entry point says what they count as).
  * Errors.  EINVAL for a bad dtype, size, flag, NULL, misaligned or too small
- *          argument, found on the host before any work is enqueued; EHIP.
+ *          argument, or for more rows than one launch holds (2^32 threads: beyond
+ *          100 GB of features), found on the host before any work is enqueued;
+ *          EHIP.
  */
 #ifndef SPCONV_ROWS_H
 #define SPCONV_ROWS_H
@@ -73,7 +75,7 @@ int spconv_layer_norm_backward(int dt, const void* dy, const void* x, const floa
                                float* dbeta, int64_t n, int C, void* workspace,
                                size_t workspace_bytes, void* stream);
 
-/* Dropout of `count` elements in flat order:
+/* Dropout of `count` < 2^34 elements in flat order:
  *   y[i] = residual[i] + (u(i) >= round(p * 2^32) ? x[i] / (1 - p) : 0)
  * where u(i) is word i % 4 of Philox4x32 with 7 rounds (Salmon, Moraes, Dror
  * and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) for the

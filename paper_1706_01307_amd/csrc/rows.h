@@ -174,6 +174,8 @@ inline bool ptr_ok(const void* p, int64_t count, size_t bytes) {
   return (p || count == 0) && aligned_to(p, bytes);
 }
 inline bool rows_ok(int64_t n) { return n >= 0 && n < 0x80000000ll; }
+// A launch holds fewer than 2^32 threads.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks < (1ll << 32) / threads; }
 inline int launched() { return hipGetLastError() == hipSuccess ? SPCONV_OK : SPCONV_EHIP; }
 
 }  // namespace spc

@@ -1,5 +1,7 @@
 // Weighted sum of a row's expert outputs, and its gradients.  Both are bound by
 // memory bandwidth: every row of y (and of dy) is touched once, in whole rows.
+#include <type_traits>
+
 #include "rows.h"
 
 namespace spc {
@@ -140,14 +142,17 @@ struct Fwd {
   int k, C;
   hipStream_t st;
 };
-template <typename T, int LPR, int K, bool TAIL> void fwd_run(const Fwd& a) {
-  const uint32_t bx = static_cast<uint32_t>((a.n + kThreads / LPR - 1) / (kThreads / LPR));
+template <typename T, int LPR, int K, bool TAIL> int fwd_run(const Fwd& a) {
+  const int64_t blocks = (a.n + kThreads / LPR - 1) / (kThreads / LPR);
+  if (!grid_fits(blocks, kThreads)) return SPCONV_EINVAL;
+  const uint32_t bx = static_cast<uint32_t>(blocks);
   // few rows: their columns over more workgroups
   const int64_t strips = (a.C + LPR * Row<T>::VEC - 1ll) / (LPR * Row<T>::VEC);
   const uint32_t by = bx >= 256 ? 1 : static_cast<uint32_t>(strips < 64 ? strips : 64);
   k_combine_fwd<T, LPR, K, TAIL><<<dim3(bx, by), kThreads, 0, a.st>>>(
       static_cast<const T*>(a.y), a.m, a.pos, a.weights, static_cast<const T*>(a.res),
       static_cast<T*>(a.out), a.n, a.k, a.C);
+  return launched();
 }
 struct Bwd {
   const void *dout, *y;
@@ -160,41 +165,44 @@ struct Bwd {
   int k, C;
   hipStream_t st;
 };
-template <typename T, int LPR, int K, bool TAIL> void bwd_run(const Bwd& a) {
-  const uint32_t bx = static_cast<uint32_t>((a.n + kThreads / LPR - 1) / (kThreads / LPR));
+template <typename T, int LPR, int K, bool TAIL> int bwd_run(const Bwd& a) {
+  const int64_t blocks = (a.n + kThreads / LPR - 1) / (kThreads / LPR);
+  if (!grid_fits(blocks + 64, kThreads)) return SPCONV_EINVAL;
+  const uint32_t bx = static_cast<uint32_t>(blocks);
   // the tail is empty, or what closed experts left: a few workgroups
   const uint32_t bz = a.count && a.m ? 64 : 0;
-  if (bx + bz == 0) return;
+  if (bx + bz == 0) return SPCONV_OK;
   k_combine_bwd<T, LPR, K, TAIL><<<bx + bz, kThreads, 0, a.st>>>(
       static_cast<const T*>(a.dout), static_cast<const T*>(a.y), a.pos, a.weights, a.count,
       static_cast<T*>(a.dy), a.dweights, a.m, a.n, a.k, a.C, bx);
+  return launched();
 }
 
 // LPR: the lanes a row fills, up to a wave.  Slots: 1, 2 and 4 known to the
 // compiler, others one at a time.
-template <typename T, int LPR, bool TAIL, typename A> void by_slots(const A& a) {
+template <typename T, int LPR, bool TAIL, typename A> int by_slots(const A& a) {
   constexpr bool kFwd = __is_same(A, Fwd);
   auto go = [&](auto kc) {
-    if constexpr (kFwd) fwd_run<T, LPR, kc.value, TAIL>(a); else bwd_run<T, LPR, kc.value, TAIL>(a);
+    if constexpr (kFwd) return fwd_run<T, LPR, kc.value, TAIL>(a);
+    else return bwd_run<T, LPR, kc.value, TAIL>(a);
   };
   if (a.k == 1) return go(std::integral_constant<int, 1>{});
   if (a.k == 2) return go(std::integral_constant<int, 2>{});
   if (a.k == 4) return go(std::integral_constant<int, 4>{});
-  go(std::integral_constant<int, 0>{});
+  return go(std::integral_constant<int, 0>{});
 }
-template <typename T, bool TAIL, typename A> void by_width(const A& a) {
+template <typename T, bool TAIL, typename A> int by_width(const A& a) {
   const int64_t pieces = (a.C + Row<T>::VEC - 1ll) / Row<T>::VEC;
   if (pieces <= 4) return by_slots<T, 4, TAIL>(a);
   if (pieces <= 8) return by_slots<T, 8, TAIL>(a);
   if (pieces <= 16) return by_slots<T, 16, TAIL>(a);
   if (pieces <= 32) return by_slots<T, 32, TAIL>(a);
-  by_slots<T, 64, TAIL>(a);
+  return by_slots<T, 64, TAIL>(a);
 }
-template <typename A> void by_type(int dt, const A& a) {
+template <typename A> int by_type(int dt, const A& a) {
   if (dt == SPCONV_BF16)
-    a.C % 8 ? by_width<bf16_t, true>(a) : by_width<bf16_t, false>(a);
-  else
-    a.C % 4 ? by_width<float, true>(a) : by_width<float, false>(a);
+    return a.C % 8 ? by_width<bf16_t, true>(a) : by_width<bf16_t, false>(a);
+  return a.C % 4 ? by_width<float, true>(a) : by_width<float, false>(a);
 }
 
 bool sizes_ok(int dt, int64_t m, int64_t n, int k, int C) {
@@ -216,8 +224,8 @@ extern "C" int spconv_combine_forward(int dt, const void* y, int64_t m, const in
       !aligned_to(residual, e) || !ptr_ok(out, n, e))
     return SPCONV_EINVAL;
   if (n == 0) return SPCONV_OK;
-  by_type(dt, Fwd{y, m, pos, weights, residual, out, n, k, C, static_cast<hipStream_t>(stream)});
-  return launched();
+  return by_type(dt, Fwd{y, m, pos, weights, residual, out, n, k, C,
+                         static_cast<hipStream_t>(stream)});
 }
 
 extern "C" int spconv_combine_backward(int dt, const void* dout, const void* y, const int32_t* pos,
@@ -231,7 +239,6 @@ extern "C" int spconv_combine_backward(int dt, const void* dout, const void* y, 
       !aligned_to(dweights, 4))
     return SPCONV_EINVAL;
   if (n == 0 && m == 0) return SPCONV_OK;
-  by_type(dt, Bwd{dout, y, pos, weights, count, dy, dweights, m, n, k, C,
-                  static_cast<hipStream_t>(stream)});
-  return launched();
+  return by_type(dt, Bwd{dout, y, pos, weights, count, dy, dweights, m, n, k, C,
+                         static_cast<hipStream_t>(stream)});
 }

@@ -88,8 +88,8 @@ using namespace spc;
 extern "C" int spconv_dropout_forward(int dt, const void* x, const void* residual, double p,
                                       uint64_t seed, uint64_t offset, const uint64_t* step, void* y,
                                       int64_t count, void* stream) {
-  // (2^40 elements: the grid's limit)
-  if (!dtype_ok(dt) || !(p >= 0.0 && p < 1.0) || count < 0 || count > (1ll << 40) ||
+  // (2^34 elements: what one launch holds)
+  if (!dtype_ok(dt) || !(p >= 0.0 && p < 1.0) || count < 0 || count >= (1ll << 34) ||
       !ptr_ok(x, count, elem_bytes(dt)) || !ptr_ok(y, count, elem_bytes(dt)) ||
       !aligned_to(residual, elem_bytes(dt)) || !aligned_to(step, 8))
     return SPCONV_EINVAL;

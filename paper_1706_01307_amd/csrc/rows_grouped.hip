@@ -1274,7 +1274,7 @@ template <typename T> bool whole_rows(const void* p, int64_t C) {
 template <int BM> bool grouped_grid(const GroupedArgs& a, int span, uint32_t* blocks) {
   const int64_t n = tile_bound(a.m, a.E + 1, BM) * ((a.cols + span - 1) / span);
   *blocks = static_cast<uint32_t>(n);
-  return n <= 0x7fffffff;
+  return grid_fits(n, 1024);                       // (the largest workgroup)
 }
 template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC>
 int run_grouped(const GroupedArgs& a) {
@@ -1449,7 +1449,7 @@ extern "C" int spconv_grouped_backward_weight(int dt, const void* x, int64_t n_x
       !ptr_ok(dw, 1, 4) || !aligned_to(db, 4) ||
       (plan.bytes && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < plan.bytes)))
     return SPCONV_EINVAL;
-  if (plan.jobs * plan.tiles > 0x7fffffff) return SPCONV_EINVAL;
+  if (!grid_fits(plan.jobs * plan.tiles, 512)) return SPCONV_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   WeightArgs a{x, n_x, dy, offsets, rows, dw, db, m, plan.chunk, E, C_in, C_out, st};
   const int64_t per = static_cast<int64_t>(C_in) * C_out;

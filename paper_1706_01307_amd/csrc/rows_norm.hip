@@ -332,11 +332,10 @@ __global__ __launch_bounds__(1024) void k_norm_parts(const float* __restrict__ p
   }
 }
 
-// Workgroups of the gradient, each with a part of its own: four a compute
-// unit, fewer where the parts (8 C bytes) would be more than a few per cent of
-// the rows' own bytes.
-int norm_parts(int64_t n, int C) {
-  (void)C;
+// Workgroups of the gradient, each with a part (8 C bytes) of its own: four a
+// compute unit, and at least 32 rows each, so that the parts stay a few per cent
+// of the rows' own bytes.
+int norm_parts(int64_t n) {
   const int64_t p = (n + 31) / 32;
   return static_cast<int>(p < 1 ? 1 : p > 1024 ? 1024 : p);
 }
@@ -351,9 +350,11 @@ struct NormFwd {
   int C;
   hipStream_t st;
 };
-template <typename T, int LPR, int NV, int UR> void run_fwd(const NormFwd& a) {
+template <typename T, int LPR, int NV, int UR> int run_fwd(const NormFwd& a) {
   constexpr int64_t rows = kThreads / LPR * UR;
-  const dim3 grid(static_cast<uint32_t>((a.n + rows - 1) / rows));
+  const int64_t blocks = (a.n + rows - 1) / rows;
+  if (!grid_fits(blocks, kThreads)) return SPCONV_EINVAL;
+  const dim3 grid(static_cast<uint32_t>(blocks));
   const T* x = static_cast<const T*>(a.x);
   T* y = static_cast<T*>(a.y);
   if (a.C % Row<T>::VEC == 0)
@@ -362,8 +363,9 @@ template <typename T, int LPR, int NV, int UR> void run_fwd(const NormFwd& a) {
   else
     k_norm_fwd<T, LPR, NV, UR, true><<<grid, kThreads, 0, a.st>>>(x, a.gamma, a.beta, a.eps, y,
                                                                  a.mean, a.rstd, a.n, a.C);
+  return launched();
 }
-template <typename T> void norm_fwd(const NormFwd& a) {
+template <typename T> int norm_fwd(const NormFwd& a) {
   const int64_t pieces = (a.C + Row<T>::VEC - 1) / Row<T>::VEC;
   if (pieces <= 4) return run_fwd<T, 4, 1, 4>(a);
   if (pieces <= 8) return run_fwd<T, 8, 1, 4>(a);
@@ -374,9 +376,11 @@ template <typename T> void norm_fwd(const NormFwd& a) {
   if (pieces <= 256) return run_fwd<T, 64, 4, 1>(a);
   if (pieces <= 512) return run_fwd<T, 256, 2, 1>(a);
   if (pieces <= 1024) return run_fwd<T, 256, 4, 1>(a);
+  if (!grid_fits(a.n, kThreads)) return SPCONV_EINVAL;
   k_norm_fwd_wide<T><<<static_cast<uint32_t>(a.n), kThreads, 0, a.st>>>(
       static_cast<const T*>(a.x), a.gamma, a.beta, a.eps, static_cast<T*>(a.y), a.mean, a.rstd,
       a.C);
+  return launched();
 }
 
 struct NormBwd {
@@ -389,8 +393,10 @@ struct NormBwd {
   int C;
   hipStream_t st;
 };
-template <typename T, int LPR, int NV, int UR> void run_bwd(const NormBwd& a) {
+template <typename T, int LPR, int NV, int UR> int run_bwd(const NormBwd& a) {
   constexpr int64_t rows = kThreads / LPR * UR;
+  const int64_t blocks = (a.n + rows - 1) / rows;
+  if (!grid_fits(blocks, kThreads)) return SPCONV_EINVAL;
   const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x);
   T* dx = static_cast<T*>(a.dx);
   const bool tail = a.C % Row<T>::VEC != 0;
@@ -403,7 +409,7 @@ template <typename T, int LPR, int NV, int UR> void run_bwd(const NormBwd& a) {
       k_norm_bwd<T, LPR, NV, UR, false, true><<<grid, kThreads, 0, a.st>>>(
           dy, x, a.mean, a.rstd, a.gamma, dx, a.part, a.n, a.C);
   } else {
-    const dim3 grid(static_cast<uint32_t>((a.n + rows - 1) / rows));
+    const dim3 grid(static_cast<uint32_t>(blocks));
     if (tail)
       k_norm_bwd<T, LPR, NV, UR, true, false><<<grid, kThreads, 0, a.st>>>(
           dy, x, a.mean, a.rstd, a.gamma, dx, nullptr, a.n, a.C);
@@ -411,8 +417,9 @@ template <typename T, int LPR, int NV, int UR> void run_bwd(const NormBwd& a) {
       k_norm_bwd<T, LPR, NV, UR, false, false><<<grid, kThreads, 0, a.st>>>(
           dy, x, a.mean, a.rstd, a.gamma, dx, nullptr, a.n, a.C);
   }
+  return launched();
 }
-template <typename T> void norm_bwd(const NormBwd& a) {
+template <typename T> int norm_bwd(const NormBwd& a) {
   const int64_t pieces = (a.C + Row<T>::VEC - 1) / Row<T>::VEC;
   if (pieces <= 4) return run_bwd<T, 4, 1, 2>(a);
   if (pieces <= 8) return run_bwd<T, 8, 1, 2>(a);
@@ -424,12 +431,14 @@ template <typename T> void norm_bwd(const NormBwd& a) {
   if (pieces <= 512) return run_bwd<T, 256, 2, 1>(a);
   if (pieces <= 1024) return run_bwd<T, 256, 4, 1>(a);
   const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x);
+  if (!grid_fits(a.n, kThreads)) return SPCONV_EINVAL;
   if (a.n)
     k_norm_bwd_wide<T><<<static_cast<uint32_t>(a.n), kThreads, 0, a.st>>>(
         dy, x, a.mean, a.rstd, a.gamma, static_cast<T*>(a.dx), a.C);
   if (a.part)
     k_norm_cols<T><<<dim3(a.nparts, static_cast<uint32_t>((a.C + kThreads - 1ll) / kThreads)),
                      kThreads, 0, a.st>>>(dy, x, a.mean, a.rstd, a.part, a.n, a.C);
+  return launched();
 }
 
 bool norm_sizes_ok(int64_t n, int C) { return rows_ok(n) && C >= 1 && C <= 0x7fffff00; }
@@ -449,13 +458,12 @@ extern "C" int spconv_layer_norm_forward(int dt, const void* x, const float* gam
     return SPCONV_EINVAL;
   if (n == 0) return SPCONV_OK;
   const NormFwd a{x, gamma, beta, eps, y, mean, rstd, n, C, static_cast<hipStream_t>(stream)};
-  if (dt == SPCONV_BF16) norm_fwd<bf16_t>(a); else norm_fwd<float>(a);
-  return launched();
+  return dt == SPCONV_BF16 ? norm_fwd<bf16_t>(a) : norm_fwd<float>(a);
 }
 
 extern "C" int spconv_layer_norm_backward_workspace(int64_t n, int C, size_t* bytes) {
   if (!norm_sizes_ok(n, C) || !bytes) return SPCONV_EINVAL;
-  *bytes = static_cast<size_t>(norm_parts(n, C)) * 2 * C * sizeof(float);
+  *bytes = static_cast<size_t>(norm_parts(n)) * 2 * C * sizeof(float);
   return SPCONV_OK;
 }
 
@@ -470,7 +478,7 @@ extern "C" int spconv_layer_norm_backward(int dt, const void* dy, const void* x,
   if (!ptr_ok(dy, n, e) || !ptr_ok(x, n, e) || !ptr_ok(dx, n, e) || !ptr_ok(mean, n, 4) ||
       !ptr_ok(rstd, n, 4))
     return SPCONV_EINVAL;
-  const int nparts = norm_parts(n, C);
+  const int nparts = norm_parts(n);
   if (dgamma && (!workspace || !aligned_to(workspace, 16) ||
                  workspace_bytes < static_cast<size_t>(nparts) * 2 * C * sizeof(float)))
     return SPCONV_EINVAL;
@@ -478,7 +486,8 @@ extern "C" int spconv_layer_norm_backward(int dt, const void* dy, const void* x,
   hipStream_t st = static_cast<hipStream_t>(stream);
   float* part = dgamma ? static_cast<float*>(workspace) : nullptr;
   const NormBwd a{dy, x, mean, rstd, gamma, dx, part, nparts, n, C, st};
-  if (dt == SPCONV_BF16) norm_bwd<bf16_t>(a); else norm_bwd<float>(a);
+  const int status = dt == SPCONV_BF16 ? norm_bwd<bf16_t>(a) : norm_bwd<float>(a);
+  if (status != SPCONV_OK) return status;
   if (dgamma)
     k_norm_parts<<<static_cast<uint32_t>((2ll * C + 15) / 16), 1024, 0, st>>>(part, nparts, dgamma,
                                                                             dbeta, C);

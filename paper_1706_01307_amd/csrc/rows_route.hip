@@ -418,7 +418,7 @@ struct Fwd {
   int32_t *offsets, *rows, *pos, *counts;
   hipStream_t st;
 };
-template <typename T, int LPR, int NV> void run(const Fwd& a) {
+template <typename T, int LPR, int NV> int run(const Fwd& a) {
   const int rb = rows_per_block(a.n, a.E, a.k);
   const int nblk = a.n ? static_cast<int>((a.n + rb - 1) / rb) : 1;
   const T* l = static_cast<const T*>(a.logits);
@@ -436,6 +436,7 @@ template <typename T, int LPR, int NV> void run(const Fwd& a) {
     k_route_place<<<nblk, kThreads, 0, a.st>>>(a.experts, a.counts, totals, a.n, a.E, a.k, rb,
                                               a.offsets, a.rows, a.pos);
   }
+  return launched();
 }
 struct Bwd {
   const float* dweights;
@@ -447,8 +448,10 @@ struct Bwd {
   void* dlogits;
   hipStream_t st;
 };
-template <typename T, int LPR, int NV> void run(const Bwd& a) {
-  const uint32_t blocks = static_cast<uint32_t>((a.n + kThreads / LPR - 1) / (kThreads / LPR));
+template <typename T, int LPR, int NV> int run(const Bwd& a) {
+  const int64_t want = (a.n + kThreads / LPR - 1) / (kThreads / LPR);
+  if (!grid_fits(want, kThreads)) return SPCONV_EINVAL;
+  const uint32_t blocks = static_cast<uint32_t>(want);
   const T* l = static_cast<const T*>(a.logits);
   T* d = static_cast<T*>(a.dlogits);
   if (a.E % Row<T>::VEC)
@@ -457,11 +460,12 @@ template <typename T, int LPR, int NV> void run(const Bwd& a) {
   else
     k_route_bwd<T, LPR, NV, false><<<blocks, kThreads, 0, a.st>>>(
         a.dweights, l, a.experts, a.weights, a.n, a.E, a.k, a.normalize, d);
+  return launched();
 }
 // Up to four pieces a lane, then more lanes: a step of the exchange between lanes
 // costs a wave the same for 4 rows as for 16 (64 fp32 logits, 348,208 rows: four
 // lanes a row 31 us, sixteen with a piece each 48).
-template <typename T, typename A> void by_width(const A& a) {
+template <typename T, typename A> int by_width(const A& a) {
   const int pieces = (a.E + Row<T>::VEC - 1) / Row<T>::VEC;
   if (pieces <= 1) return run<T, 1, 1>(a);
   if (pieces <= 2) return run<T, 1, 2>(a);
@@ -471,7 +475,8 @@ template <typename T, typename A> void by_width(const A& a) {
   if (pieces <= 32) return run<T, 8, 4>(a);
   if (pieces <= 64) return run<T, 16, 4>(a);
   if (pieces <= 128) return run<T, 32, 4>(a);
-  if constexpr (Row<T>::VEC == 4) run<T, 64, 4>(a);
+  if constexpr (Row<T>::VEC == 4) return run<T, 64, 4>(a);
+  return SPCONV_EINVAL;                            // (not reached: E <= kMaxE)
 }
 
 bool sizes_ok(int64_t n, int E, int k) {
@@ -505,8 +510,7 @@ extern "C" int spconv_route_forward(int dt, const void* logits, int64_t n, int E
   // (no rows: one workgroup without rows writes the offsets)
   const Fwd a{logits, n, E, k, normalize, experts, weights, offsets, rows, pos,
               static_cast<int32_t*>(workspace), static_cast<hipStream_t>(stream)};
-  if (dt == SPCONV_BF16) by_width<bf16_t>(a); else by_width<float>(a);
-  return launched();
+  return dt == SPCONV_BF16 ? by_width<bf16_t>(a) : by_width<float>(a);
 }
 
 extern "C" int spconv_route_backward(int dt, const float* dweights, const void* logits,
@@ -519,6 +523,5 @@ extern "C" int spconv_route_backward(int dt, const float* dweights, const void* 
   if (n == 0) return SPCONV_OK;
   const Bwd a{dweights, logits, experts, weights, n, E, k, normalize, dlogits,
               static_cast<hipStream_t>(stream)};
-  if (dt == SPCONV_BF16) by_width<bf16_t>(a); else by_width<float>(a);
-  return launched();
+  return dt == SPCONV_BF16 ? by_width<bf16_t>(a) : by_width<float>(a);
 }

@@ -87,6 +87,8 @@ def _given(t, name, dtypes, shape, dims=0):
 def _result(out, shape, dtype, like):
     """The output tensor: `out`, which must fit as it is, or a new one beside `like`."""
     if out is None:
+        if like.dtype == dtype and like.shape == shape:
+            return torch.empty_like(like)          # (the quicker of the two)
         return torch.empty(shape, dtype=dtype, device=like.device)
     if (not isinstance(out, torch.Tensor) or out.device != like.device or out.dtype != dtype or
             out.shape != shape or not out.is_contiguous()):

@@ -61,7 +61,7 @@ def test_layer_norm_refusals():
 def test_dropout_refusals():
     _refused("spconv_dropout_forward", [0, P, P, 0.5, 1, 2, P, P, 8, None], [
         {0: 2}, {1: None}, {1: ODD}, {2: ODD}, {3: -0.1}, {3: 1.0}, {3: float("nan")},
-        {6: ctypes.c_void_p(4100)}, {7: None}, {7: ODD}, {8: -1}])
+        {6: ctypes.c_void_p(4100)}, {7: None}, {7: ODD}, {8: -1}, {8: 2 ** 34}])
     _refused("spconv_dropout_backward", [0, P, 0.5, 1, 2, None, P, 8, None], [
         {0: 2}, {1: None}, {2: 1.0}, {6: None}, {7: -1}])
 

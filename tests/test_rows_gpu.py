@@ -125,6 +125,15 @@ def test_layer_norm_constant_and_nonfinite_rows():
     assert torch.isnan(y[1]).all() and torch.isfinite(y[0]).all() and torch.isfinite(y[2]).all()
 
 
+def test_layer_norm_without_rows():
+    x = torch.empty(0, 24, device="cuda")
+    y, mean, rstd = spc.layer_norm_forward(x)
+    assert y.shape == (0, 24) and mean.shape == rstd.shape == (0,)
+    dx, dg, db = spc.layer_norm_backward(x, x, mean, rstd, torch.ones(24, device="cuda"))
+    assert dx.shape == (0, 24) and not dg.any() and not db.any()
+    assert spc.dropout_forward(x, 0.5, 1).shape == (0, 24)
+
+
 # ---------------------------------------------------------------------------
 # Dropout
 # ---------------------------------------------------------------------------
