@@ -1317,14 +1317,15 @@ inline bool few_is_faster(const GroupedArgs& a, size_t bytes) {
   const double k = a.red / 2048.0, over = blocks > 64 ? (blocks - 64) / 192 : 0.0;
   return 6.4 + 2.5 * k + over * (4.0 + 10.0 * k) < tiles;
 }
-// Which kernel: k_grouped_few by the estimate above; k_grouped_any where pieces may be cut or unaligned; k_grouped_short
-// for bf16 reductions of at most 256 and more than one column tile, of many rows
-// (256 -> 1024, 696,416 positions: 570 us against 847); else k_grouped.  Its tiles
-// are 64 x 64 for fp32, whose products bound it and hide everything else best with
-// many waves (512 -> 512, 65,536 positions: 365 us against 404 with 128 x 128), for
-// few columns, and for bf16 where 128 x 128 would not fill the card twice (512 ->
-// 512, 8,000 positions: 20 us against 26); 256 x 256 where they do and waste little
-// of their last columns (2048 -> 2048, 65,536 positions: 603 us against 692).
+// Which kernel: k_grouped_few by the estimate above; k_grouped_any where pieces may
+// be cut or unaligned; k_grouped_short for bf16 reductions of at most 256 and more
+// than one column tile, of many rows (256 -> 1024, 696,416 positions: 570 us against
+// 847); else k_grouped.  Its tiles are 64 x 64 for few columns and where 128 x 128
+// would not fill the card twice (bf16 512 -> 512, 8,000 positions: 20 us against
+// 26), for fp32 four times or without wasting columns (fp32 144 -> 80, 492,252
+// positions: 236 us against 268, but 80 -> 144 300 against 285; 1024 -> 1024, 65,536:
+// 1,170 against 1,290); for bf16 256 x 256 where they fill it twice and waste little
+// (2048 -> 2048, 65,536: 603 us against 692).
 template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
   if constexpr (!BT) {
     uint32_t blocks;
@@ -1334,12 +1335,12 @@ template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
     }
   }
   const int64_t c256 = (a.cols + 255) / 256, c128 = (a.cols + 127) / 128;
-  const bool small = sizeof(T) == 4 || a.cols <= 64 || a.m <= 64ll * a.E ||
-                     tile_bound(a.m, a.E, 128) * c128 < 1024;
+  const int64_t c64 = (a.cols + 63) / 64, tiles = tile_bound(a.m, a.E, 128) * c128;
+  const bool waste = c64 % 2 && c64 > 2 && c64 < 16;   // of the last 128 columns
+  const bool small = a.cols <= 64 || a.m <= 64ll * a.E ||
+                     (sizeof(T) == 2 ? tiles < 1024 : tiles < 2048 || waste);
   if (!whole_rows<T>(a.x, a.red) || !whole_rows<T>(a.w, BT ? a.red : a.cols)) {
-    if constexpr (sizeof(T) == 2)
-      if (!small) return run_grouped_any<T, TO, BT, 128, 128>(a);
-    return run_grouped_any<T, TO, BT, 64, 64>(a);
+    return small ? run_grouped_any<T, TO, BT, 64, 64>(a) : run_grouped_any<T, TO, BT, 128, 128>(a);
   }
   if constexpr (sizeof(T) == 2) {
     if (a.red <= 256 && a.cols > 128 && a.cols % Row<TO>::VEC == 0 && a.m >= 16384) {
@@ -1348,13 +1349,11 @@ template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
       if (a.red <= 192) return run_grouped_short<TO, BT, 6>(a);
       return run_grouped_short<TO, BT, 8>(a);
     }
-    if (!small) {
-      if (20 * c256 <= 11 * c128 + 1 && a.m / 256 * c256 >= 512)
-        return run_grouped<T, TO, BT, 256, 256, 2, 4>(a);
-      return run_grouped<T, TO, BT, 128, 128, 2, 2>(a);
-    }
+    if (!small && 20 * c256 <= 11 * c128 + 1 && a.m / 256 * c256 >= 512)
+      return run_grouped<T, TO, BT, 256, 256, 2, 4>(a);
   }
-  return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
+  if (small) return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
+  return run_grouped<T, TO, BT, 128, 128, 2, 2>(a);
 }
 template <bool BT> int run_types(int in_dt, int out_dt, const GroupedArgs& a) {
   if (in_dt == SPCONV_BF16)
