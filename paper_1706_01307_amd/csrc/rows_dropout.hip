@@ -5,6 +5,7 @@
 // counter by rounds of two 32 x 32 -> 64 bit products.  Seven rounds are the
 // fewest its authors found to pass their whole battery of tests.
 #include <cmath>
+#include <type_traits>
 
 #include "rows.h"
 
@@ -97,14 +98,15 @@ extern "C" int spconv_dropout_forward(int dt, const void* x, const void* residua
   // up to 2^32 itself, which drops everything
   const uint64_t threshold = static_cast<uint64_t>(std::nearbyint(p * 4294967296.0));
   const float scale = static_cast<float>(1.0 / (1.0 - p));
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dt == SPCONV_BF16) {
-    if (residual) run<bf16_t, true>(x, residual, threshold, scale, seed, offset, step, y, count, st);
-    else run<bf16_t, false>(x, nullptr, threshold, scale, seed, offset, step, y, count, st);
-  } else {
-    if (residual) run<float, true>(x, residual, threshold, scale, seed, offset, step, y, count, st);
-    else run<float, false>(x, nullptr, threshold, scale, seed, offset, step, y, count, st);
-  }
+  const auto go = [&](auto* type, auto res) {
+    run<std::remove_pointer_t<decltype(type)>, res.value>(x, residual, threshold, scale, seed,
+                                                          offset, step, y, count,
+                                                          static_cast<hipStream_t>(stream));
+  };
+  bf16_t* const b = nullptr;
+  float* const f = nullptr;
+  if (dt == SPCONV_BF16) residual ? go(b, std::true_type{}) : go(b, std::false_type{});
+  else residual ? go(f, std::true_type{}) : go(f, std::false_type{});
   return launched();
 }
 

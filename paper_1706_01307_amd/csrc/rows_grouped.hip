@@ -1222,7 +1222,7 @@ double dw_cost(bool f32, int64_t m, int64_t groups, double values, int tile, dou
   const double length = chunk && chunk < longest ? static_cast<double>(chunk) : longest;
   const double unit = length / stage * us + 3.0, even = mean / stage * us + 3.0;
   if (!chunk) return rounds * even > unit ? rounds * even : unit;
-  const double whole = static_cast<double>(static_cast<int64_t>(rounds)) + (rounds > 3.0 ? 0.5 : 1.0);
+  const double whole = static_cast<int64_t>(rounds) + (rounds > 3.0 ? 0.5 : 1.0);
   return unit * whole + 4.0 + jobs * values * 8.0 / 4e6;
 }
 DwPlan dw_plan(int dt, int64_t m, int E, int C_in, int C_out, bool wide) {
@@ -1271,22 +1271,23 @@ template <typename T> bool whole_rows(const void* p, int64_t C) {
   return C % Row<T>::VEC == 0 && aligned_to(p, 16);
 }
 
-template <int BM> bool grouped_grid(const GroupedArgs& a, int span, uint32_t* blocks) {
+template <int BM>
+bool grouped_grid(const GroupedArgs& a, int span, int threads, uint32_t* blocks) {
   const int64_t n = tile_bound(a.m, a.E + 1, BM) * ((a.cols + span - 1) / span);
   *blocks = static_cast<uint32_t>(n);
-  return grid_fits(n, 1024);                       // (the largest workgroup)
+  return grid_fits(n, threads);
 }
 template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC>
 int run_grouped(const GroupedArgs& a) {
   uint32_t blocks;
-  if (!grouped_grid<BM>(a, BN, &blocks)) return SPCONV_EINVAL;
+  if (!grouped_grid<BM>(a, BN, 64 * WR * WC, &blocks)) return SPCONV_EINVAL;
   k_grouped<T, TO, BT, BM, BN, WR, WC><<<blocks, 64 * WR * WC, 0, a.st>>>(a);
   return launched();
 }
 template <typename T, typename TO, bool BT, int BM, int BN>
 int run_grouped_any(const GroupedArgs& a) {
   uint32_t blocks;
-  if (!grouped_grid<BM>(a, BN, &blocks)) return SPCONV_EINVAL;
+  if (!grouped_grid<BM>(a, BN, kThreads, &blocks)) return SPCONV_EINVAL;
   k_grouped_any<T, TO, BT, BM, BN><<<blocks, kThreads, 0, a.st>>>(a);
   return launched();
 }
@@ -1297,7 +1298,7 @@ template <typename TO, bool BT, int NK> int run_grouped_short(const GroupedArgs&
   const int parts = static_cast<int>(want < ncol ? want : ncol);
   const int span = (ncol + parts - 1) / parts * 128;
   uint32_t blocks;
-  if (!grouped_grid<kShortRows>(a, span, &blocks)) return SPCONV_EINVAL;
+  if (!grouped_grid<kShortRows>(a, span, 512, &blocks)) return SPCONV_EINVAL;
   if (BT ? a.mask != nullptr : a.relu != 0)
     k_grouped_short<TO, BT, NK, !BT, BT><<<blocks, 512, 0, a.st>>>(a, span);
   else
@@ -1329,7 +1330,7 @@ inline bool few_is_faster(const GroupedArgs& a, size_t bytes) {
 template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
   if constexpr (!BT) {
     uint32_t blocks;
-    if (few_is_faster(a, sizeof(T)) && grouped_grid<4>(a, 4 * Row<T>::VEC, &blocks)) {
+    if (few_is_faster(a, sizeof(T)) && grouped_grid<4>(a, 4 * Row<T>::VEC, kFewThreads, &blocks)) {
       k_grouped_few<T, TO><<<blocks, kFewThreads, 0, a.st>>>(a);
       return launched();
     }
