@@ -349,89 +349,99 @@ __device__ __forceinline__ void put4(bf16_t* d, const float (&v)[4]) {
 }
 
 // The finished tile of a workgroup of WR x WC waves, FM x FN blocks each, leaves
-// through LDS as whole rows, in parts that fit `lds` (BYTES): FNP column and FMP
-// row blocks of every wave at a time.  A barrier before and within each part.
-template <typename TO, int BM, int BN, int WR, int WC, int BYTES>
+// through LDS as whole rows, in parts that fit `lds` (BYTES) and are up to four
+// pieces a lane: FNP column and FMP row blocks of every wave at a time.  A barrier before and within each part; its
+// mask (MASK) is asked for while the part before is finished.
+// WHOLE: rows are of whole pieces.
+template <typename TO, bool MASK, bool RELU, bool WHOLE, int BM, int BN, int WR, int WC, int BYTES>
 __device__ __forceinline__ void store_tile_rows(
     u32x4_t* lds, const f32x16 (&acc)[BN / WC / 32][BM / WR / 32], const float* s_bias,
     const GroupedArgs& a, const Job& j, int n0) {
   constexpr int FM = BM / WR / 32, FN = BN / WC / 32, VO = Row<TO>::VEC;
   constexpr int TOB = static_cast<int>(sizeof(TO));
-  constexpr int FNP = BM * BN * TOB <= BYTES ? FN : 1;
+  constexpr int NT = 64 * WR * WC, ROOM = BYTES < 64 * NT ? BYTES : 64 * NT;
+  constexpr int FNP = BM * BN * TOB <= ROOM ? FN : 1;
   constexpr int CW = WC * 32 * FNP;                // columns of a part
-  constexpr int FMP = BM * CW * TOB <= BYTES ? FM : BM * CW * TOB <= 2 * BYTES ? FM / 2 : FM / 4;
+  constexpr int FMP = BM * CW * TOB <= ROOM ? FM : BM * CW * TOB <= 2 * ROOM ? FM / 2 : FM / 4;
   constexpr int RW = WR * 32 * FMP;                // rows of a part
-  static_assert(FMP >= 1 && RW * CW * TOB <= BYTES, "a part fits the buffer");
-  constexpr int NT = 64 * WR * WC, PR = CW / VO, NPC = RW * PR / NT;
-  constexpr int NB = NPC < 4 ? NPC : 4;            // pieces a lane stores together
+  constexpr int PR = CW / VO, NPC = RW * PR / NT;  // pieces of a row, pieces a lane stores
+  constexpr int MP = FM / FMP, PARTS = FN / FNP * MP;
+  static_assert(FMP >= 1 && RW * CW * TOB <= ROOM && NPC * NT == RW * PR, "whole parts that fit");
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
   const int wrow = wave / WC, wcol = wave % WC;
   TO* const y = static_cast<TO*>(a.y);
-  const TO* const mask = static_cast<const TO*>(a.mask);
+  // where a part's piece i of this lane belongs, and the elements left of its row
+  auto place = [&](int part, int i, int64_t* at) {
+    const int p = threadIdx.x + NT * i, lr = p / PR;
+    const int r = lr / (32 * FMP) * (BM / WR) + 32 * (part % MP * FMP) + lr % (32 * FMP);
+    const int col = n0 + WC * 32 * (part / MP * FNP) + p % PR * VO;
+    *at = (j.begin + r) * a.cols + col;
+    return r < j.nrow ? a.cols - col : 0;
+  };
+  u32x4_t g[2][NPC];
+  auto ask = [&](int part) {
 #pragma unroll
-  for (int np = 0; np < FN; np += FNP)
+    for (int i = 0; i < NPC; ++i) {
+      int64_t at;
+      const int left = place(part, i, &at);
+      g[part & 1][i] = load_left<TO, WHOLE>(static_cast<const TO*>(a.mask) + at, left);
+    }
+  };
+  if constexpr (MASK) ask(0);
 #pragma unroll
-    for (int mp = 0; mp < FM; mp += FMP) {
-      __syncthreads();
-      auto write = [&](auto relu) {
+  for (int part = 0; part < PARTS; ++part) {
+    if constexpr (MASK) {
+      if (part + 1 < PARTS) ask(part + 1);
+    }
+    __syncthreads();
 #pragma unroll
-        for (int f = 0; f < FNP; ++f)
+    for (int f = 0; f < FNP; ++f)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            // 4 adjacent columns of one row in every four registers of a lane
-            const int c = col_of<WC>(wcol, f) + 8 * q + 4 * h;
-            const float4 b = *reinterpret_cast<const float4*>(s_bias + WC * 32 * np + c);
-            const float bias[4] = {b.x, b.y, b.z, b.w};
+      for (int q = 0; q < 4; ++q) {
+        // 4 adjacent columns of one row in every four registers of a lane
+        const int c = col_of<WC>(wcol, f) + 8 * q + 4 * h, np = part / MP * FNP;
+        const float4 b = *reinterpret_cast<const float4*>(s_bias + WC * 32 * np + c);
+        const float bias[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int m = 0; m < FMP; ++m) {
-              const int r = wrow * 32 * FMP + 32 * m + (lane & 31);
-              float v[4];
+        for (int m = 0; m < FMP; ++m) {
+          const int r = wrow * 32 * FMP + 32 * m + (lane & 31);
+          float v[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                v[i] = acc[np + f][mp + m][4 * q + i] + bias[i];
-                if (relu.value) v[i] = v[i] < 0.0f ? 0.0f : v[i];
-              }
-              put4(reinterpret_cast<TO*>(lds + out_at<TO, CW>(r, c / VO)) + c % VO, v);
-            }
+          for (int i = 0; i < 4; ++i) {
+            v[i] = acc[np + f][part % MP * FMP + m][4 * q + i] + bias[i];
+            if (RELU) v[i] = v[i] < 0.0f ? 0.0f : v[i];
           }
-      };
-      if (a.relu) write(std::true_type{}); else write(std::false_type{});
-      __syncthreads();
-      for (int p0 = threadIdx.x; p0 < RW * PR; p0 += NT * NB) {
-        int64_t at[NB];
-        int left[NB];
-        u32x4_t g[NB];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-          const int p = p0 + NT * i, lr = p / PR;
-          const int r = lr / (32 * FMP) * (BM / WR) + 32 * mp + lr % (32 * FMP);
-          const int col = n0 + WC * 32 * np + p % PR * VO;
-          left[i] = r < j.nrow ? a.cols - col : 0;
-          at[i] = (j.begin + r) * a.cols + col;
-        }
-        if (mask) {
-#pragma unroll
-          for (int i = 0; i < NB; ++i)
-            g[i] = left[i] >= VO || left[i] <= 0 ? load_left<TO, true>(mask + at[i], left[i])
-                                                 : load_left<TO, false>(mask + at[i], left[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-          if (left[i] <= 0) continue;
-          const int p = p0 + NT * i;
-          u32x4_t u = lds[out_at<TO, CW>(p / PR, p % PR)];
-          if (mask) {
-            float v[VO], z[VO];
-            unpack(u, v);
-            unpack(g[i], z);
-#pragma unroll
-            for (int e = 0; e < VO; ++e) v[e] = z[e] <= 0.0f ? 0.0f : v[e];
-            u = pack(v);
-          }
-          store_left<TO, (BM * BN > 128 * 128)>(y + at[i], u, left[i]);
+          put4(reinterpret_cast<TO*>(lds + out_at<TO, CW>(r, c / VO)) + c % VO, v);
         }
       }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NPC; ++i) {
+      int64_t at;
+      const int left = place(part, i, &at), p = threadIdx.x + NT * i;
+      if (left <= 0) continue;
+      u32x4_t u = lds[out_at<TO, CW>(p / PR, p % PR)];
+      if constexpr (MASK) {
+        float v[VO], z[VO];
+        unpack(u, v);
+        unpack(g[part & 1][i], z);
+#pragma unroll
+        for (int e = 0; e < VO; ++e) v[e] = z[e] <= 0.0f ? 0.0f : v[e];
+        u = pack(v);
+      }
+      store_left<TO, (BM * BN > 128 * 128)>(y + at, u, left);
     }
+  }
+}
+// The forward (BT false) has a ReLU and no mask, the input gradient a mask.
+template <typename TO, bool BT, bool WHOLE, int BM, int BN, int WR, int WC, int BYTES>
+__device__ __forceinline__ void store_tile(
+    u32x4_t* lds, const f32x16 (&acc)[BN / WC / 32][BM / WR / 32], const float* s_bias,
+    const GroupedArgs& a, const Job& j, int n0) {
+  if (BT ? a.mask != nullptr : a.relu != 0)
+    store_tile_rows<TO, BT, !BT, WHOLE, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
+  else
+    store_tile_rows<TO, false, false, WHOLE, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
 }
 
 // Rows x weights: BT false: w[e] is [red][cols] (the forward), BT true: w[e] is
@@ -548,7 +558,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped(GroupedArgs a) {
     if (s + 3 < nk) stage(s_buf3, s_buf2);
   }
   stage_barrier<0>();                              // (no load is on its way to s_buf0)
-  store_tile_rows<TO, BM, BN, WR, WC, NP0 * 16>(s_buf0, acc, s_bias, a, j, j.n0);
+  store_tile<TO, BT, true, BM, BN, WR, WC, NP0 * 16>(s_buf0, acc, s_bias, a, j, j.n0);
 }
 
 // 4 x 4 exchange among the four lanes of a quad: lane i's v[j] becomes lane j's
@@ -861,7 +871,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_any(GroupedArgs a) {
         acc, [&](int m, int q) { return rows_of(s_buf, m, q); },
         [&](int n, int q) { return weights_of(s_buf + TA::PIECES, BT ? 2 * n : n, q); });
   }
-  store_tile_rows<TO, BM, BN, 2, 2, NP * 16>(s_buf, acc, s_bias, a, j, n0);
+  store_tile<TO, BT, false, BM, BN, 2, 2, NP * 16>(s_buf, acc, s_bias, a, j, n0);
 }
 
 // Few positions in all (a row at a time through its experts): the weights' bytes,
