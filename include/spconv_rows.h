@@ -34,7 +34,8 @@
  *          are never followed (each entry point says what they count as).
  * Errors.  EINVAL for a bad dtype, size, flag, NULL, misaligned or too small
  *          argument, or for more rows than one launch holds (2^32 threads: beyond
- *          100 GB of features), found on the host before any work is enqueued;
+ *          100 GB of features; layer norm adds up dgamma and dbeta of at most
+ *          16,776,960 columns), found on the host before any work is enqueued;
  *          EHIP.
  */
 #ifndef SPCONV_ROWS_H

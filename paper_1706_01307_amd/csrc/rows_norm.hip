@@ -3,7 +3,10 @@
 // One pass over the rows: a row lives in the registers of a group of lanes
 // between its statistics and its output, so that memory is read and written
 // once; the group's sums go over the vector ALU's lane permutations.  Both
-// directions are bound by memory bandwidth.
+// directions are bound by memory bandwidth: 902,504 bf16 rows of 64 take 40 us
+// forwards (6.0 TB/s; a large copy reaches 5.1, less of it from the last-level
+// cache) and 62 + 4 us backwards (5.7 TB/s), 87,052 fp32 rows of 145 backwards
+// 31 + 4 us (5.0 TB/s).
 #include <cmath>
 
 #include "rows.h"
@@ -24,6 +27,8 @@ template <int LPR> struct RowSum {
   }
 };
 
+// y = (x - mean) rstd gamma + beta with rstd = 1 / sqrt(mean of (x - mean)^2 + eps),
+// the squares taken of x - mean (the difference of two large sums would cancel).
 // A group of LPR lanes holds a row of at most LPR * NV * VEC elements: NV
 // pieces of 16 bytes a lane.  The group takes UR rows at a time, their loads in
 // flight together.
@@ -141,7 +146,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd_wide(
   }
 }
 
-// The gradient, rows held as above.  With PARAM, a lane keeps its columns' sums
+// The gradient, rows held as above: with z = (x - mean) rstd and d = gamma dy,
+// dx = rstd (d - mean of d - z mean of d z).  With PARAM, a lane keeps its columns' sums
 // of dy z and dy over the rows its group takes (every gridDim.x * G-th batch of
 // UR rows); the groups' sums are added through LDS in group order and leave as
 // the workgroup's row of `part` ([2][C]; dgamma and dbeta themselves where one
@@ -479,6 +485,9 @@ extern "C" int spconv_layer_norm_backward(int dt, const void* dy, const void* x,
       !ptr_ok(rstd, n, 4))
     return SPCONV_EINVAL;
   const int nparts = norm_parts(n);
+  // k_norm_cols: a column of workgroups per part, at most 65,535 rows of them
+  if (dgamma && (C > 65535 * kThreads || !grid_fits(nparts * (C / kThreads + 1ll), kThreads)))
+    return SPCONV_EINVAL;
   if (dgamma && (!workspace || !aligned_to(workspace, 16) ||
                  workspace_bytes < static_cast<size_t>(nparts) * 2 * C * sizeof(float)))
     return SPCONV_EINVAL;

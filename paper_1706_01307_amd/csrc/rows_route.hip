@@ -8,6 +8,10 @@
 //   k_route_place  every pair's position: its expert's start + its
 //                  workgroup's start + its rank.
 // Where one workgroup has every row, the first launch does it all.
+//
+// 348,208 rows of 64 fp32 logits to 2 each: 30 + 4 + 5 us, where the bytes alone
+// would take 20: k_route is bound by the k dependent searches of a row (compares and
+// lane exchanges on the vector ALU), the other two are short.
 #include <cmath>
 
 #include "rows.h"

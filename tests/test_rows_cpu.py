@@ -58,6 +58,12 @@ def test_layer_norm_refusals():
     assert lib.spconv_layer_norm_backward_workspace(4, 8, ctypes.byref(n)) == 0 and n.value >= 64
 
 
+def test_layer_norm_refuses_more_columns_than_its_sums_launch():
+    good = [0, P, P, P, P, P, P, P, P, 4, 8, P, 2 ** 62, None]
+    _refused("spconv_layer_norm_backward", good, [
+        {10: 65535 * 256 + 1}, {10: 2 ** 31 - 256}, {9: 2 ** 31 - 1, 10: 65535 * 256}])
+
+
 def test_dropout_refusals():
     _refused("spconv_dropout_forward", [0, P, P, 0.5, 1, 2, P, P, 8, None], [
         {0: 2}, {1: None}, {1: ODD}, {2: ODD}, {3: -0.1}, {3: 1.0}, {3: float("nan")},
