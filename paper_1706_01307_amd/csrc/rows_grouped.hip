@@ -350,10 +350,12 @@ __device__ __forceinline__ void put4(bf16_t* d, const float (&v)[4]) {
 
 // The finished tile of a workgroup of WR x WC waves, FM x FN blocks each, leaves
 // through LDS as whole rows, in parts that fit `lds` (BYTES) and are up to four
-// pieces a lane: FNP column and FMP row blocks of every wave at a time.  A barrier before and within each part; its
-// mask (MASK) is asked for while the part before is finished.
-// WHOLE: rows are of whole pieces.
-template <typename TO, bool MASK, bool RELU, bool WHOLE, int BM, int BN, int WR, int WC,
+// pieces a lane: FNP column and FMP row blocks of every wave at a time.  A barrier
+// before and within each part; its mask (MASK) is asked for while the part before is
+// finished (65,536 x 512 -> 2048 bf16, backwards: 261 us; when a part needs it, 314),
+// unless the last pieces of its rows may be cut (WHOLE false): those loads wait for
+// one another.
+template <typename TO, bool MASK, bool WHOLE, bool RELU, int BM, int BN, int WR, int WC,
           int BYTES>
 __device__ __forceinline__ void store_tile_rows(
     u32x4_t* lds, const f32x16 (&acc)[BN / WC / 32][BM / WR / 32], const float* s_bias,
@@ -388,10 +390,10 @@ __device__ __forceinline__ void store_tile_rows(
       g[part & 1][i] = load_left<TO, WHOLE>(static_cast<const TO*>(a.mask) + at, left);
     }
   };
-  if constexpr (MASK) ask(0);
+  if constexpr (MASK && WHOLE) ask(0);
 #pragma unroll
   for (int part = 0; part < PARTS; ++part) {
-    if constexpr (MASK) {
+    if constexpr (MASK && WHOLE) {
       if (part + 1 < PARTS) ask(part + 1);
     }
     __syncthreads();
@@ -415,6 +417,7 @@ __device__ __forceinline__ void store_tile_rows(
           put4(reinterpret_cast<TO*>(lds + out_at<TO, CW>(r, c / VO)) + c % VO, v);
         }
       }
+    if constexpr (MASK && !WHOLE) ask(part);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NPC; ++i) {
@@ -435,14 +438,18 @@ __device__ __forceinline__ void store_tile_rows(
   }
 }
 // The forward (BT false) has a ReLU and no mask, the input gradient a mask.
-template <typename TO, bool BT, bool WHOLE, int BM, int BN, int WR, int WC, int BYTES>
+template <typename TO, bool BT, int BM, int BN, int WR, int WC, int BYTES>
 __device__ __forceinline__ void store_tile(
     u32x4_t* lds, const f32x16 (&acc)[BN / WC / 32][BM / WR / 32], const float* s_bias,
     const GroupedArgs& a, const Job& j, int n0) {
-  if (BT ? a.mask != nullptr : a.relu != 0)
-    store_tile_rows<TO, BT, !BT, WHOLE, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
+  if (BT && a.mask && a.cols % Row<TO>::VEC == 0)
+    store_tile_rows<TO, BT, true, false, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
+  else if (BT && a.mask)
+    store_tile_rows<TO, BT, false, false, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
+  else if (!BT && a.relu)
+    store_tile_rows<TO, false, true, !BT, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
   else
-    store_tile_rows<TO, false, false, WHOLE, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
+    store_tile_rows<TO, false, true, false, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
 }
 
 // Rows x weights: BT false: w[e] is [red][cols] (the forward), BT true: w[e] is
@@ -564,7 +571,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped(GroupedArgs a) {
     if (s + 3 < nk) stage(s_buf3, s_buf2);
   }
   stage_barrier<0>();                              // (no load is on its way to s_buf0)
-  store_tile<TO, BT, true, BM, BN, WR, WC, NP0 * 16>(s_buf0, acc, s_bias, a, j, j.n0);
+  store_tile<TO, BT, BM, BN, WR, WC, NP0 * 16>(s_buf0, acc, s_bias, a, j, j.n0);
 }
 
 // 4 x 4 exchange among the four lanes of a quad: lane i's v[j] becomes lane j's
@@ -880,7 +887,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_any(GroupedArgs a) {
         acc, [&](int m, int q) { return rows_of(s_buf, m, q); },
         [&](int n, int q) { return weights_of(s_buf + TA::PIECES, BT ? 2 * n : n, q); });
   }
-  store_tile<TO, BT, false, BM, BN, 2, 2, NP * 16>(s_buf, acc, s_bias, a, j, n0);
+  store_tile<TO, BT, BM, BN, 2, 2, NP * 16>(s_buf, acc, s_bias, a, j, n0);
 }
 
 // Few positions in all (a row at a time through its experts): the weights' bytes,
