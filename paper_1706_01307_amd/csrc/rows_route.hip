@@ -4,7 +4,8 @@
 //
 //   k_route        a group of lanes per row picks the experts; the workgroup
 //                  ranks its own pairs per expert and leaves its counts;
-//   k_route_scan   per expert, the counts' running sums over the workgroups;
+//   k_route_scan   per expert, the counts' running sums over the workgroups (few
+//                  counts are left to k_route_place);
 //   k_route_place  every pair's position: its expert's start + its
 //                  workgroup's start + its rank.
 // Where one workgroup has every row, the first launch does it all.
@@ -24,6 +25,10 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kMaxE = SPCONV_ROUTE_MAX_EXPERTS;
 constexpr int kMaxK = SPCONV_ROUTE_MAX_SLOTS;
 constexpr int kPairs = 2048;           // pairs a workgroup ranks at most
+// Counts that k_route_place adds up itself, rather than in a launch of k_route_scan
+// (30,000 rows to 2 of 16, 7,504 counts: 20.2 -> 17.7 us; captured 16.7 either way, and
+// 17.4 -> 21.2 with 15,008).
+constexpr int kSumCounts = 8192;
 
 // Rows a workgroup takes: a power of two, at most 256 (one row a lane).
 __host__ __device__ inline int rows_per_block(int64_t n, int E, int k) {
@@ -319,20 +324,52 @@ __global__ __launch_bounds__(1024) void k_route_scan(int32_t* __restrict__ count
   if (threadIdx.x == 0) totals[blockIdx.x] = carry;
 }
 
+// SUM: `counts` are k_route's, and every workgroup adds up those before its own and
+// all of them, four experts a wave in turn; else they are k_route_scan's running sums.
+template <bool SUM>
 __global__ __launch_bounds__(kThreads) void k_route_place(
-    const int32_t* __restrict__ experts, const int32_t* __restrict__ starts,
+    const int32_t* __restrict__ experts, const int32_t* __restrict__ counts,
     const int32_t* __restrict__ totals, int64_t n, int E, int k, int rows_blk,
     int32_t* __restrict__ offsets, int32_t* __restrict__ rows, int32_t* __restrict__ pos) {
-  __shared__ int32_t s_start[kMaxE], s_wave[kWaves];
-  for (int e = threadIdx.x; e < E; e += kThreads) s_start[e] = totals[e];
+  __shared__ int32_t s_start[kMaxE], s_before[SUM ? kMaxE : 1], s_wave[kWaves];
+  const int nblk = gridDim.x, blk = blockIdx.x;
+  if constexpr (SUM) {
+    constexpr int N = 4;                           // experts whose loads are in flight together
+    for (int e0 = (threadIdx.x >> 6) * N; e0 < E; e0 += kWaves * N) {
+      int32_t before[N] = {}, all[N] = {};
+      for (int b = threadIdx.x & 63; b < nblk; b += 64)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int e = e0 + i < E ? e0 + i : E - 1;
+          const int32_t v = counts[static_cast<int64_t>(e) * nblk + b];
+          all[i] += v;
+          before[i] += b < blk ? v : 0;
+        }
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          all[i] += __shfl_xor(all[i], d, 64);
+          before[i] += __shfl_xor(before[i], d, 64);
+        }
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if ((threadIdx.x & 63) == i && e0 + i < E) {
+          s_start[e0 + i] = all[i];
+          s_before[e0 + i] = before[i];
+        }
+    }
+  } else {
+    for (int e = threadIdx.x; e < E; e += kThreads) s_start[e] = totals[e];
+  }
   const int32_t total = block_scan(s_start, E, s_wave);
-  if (blockIdx.x == 0) {
+  if (blk == 0) {
     for (int e = threadIdx.x; e < E; e += kThreads) offsets[e] = s_start[e];
     if (threadIdx.x == 0) offsets[E] = total;
     __syncthreads();
   }
   for (int e = threadIdx.x; e < E; e += kThreads)
-    s_start[e] += starts[static_cast<int64_t>(e) * gridDim.x + blockIdx.x];
+    s_start[e] += SUM ? s_before[e] : counts[static_cast<int64_t>(e) * nblk + blk];
   __syncthreads();
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows_blk;
   const int64_t end = (row0 + rows_blk < n ? row0 + rows_blk : n) * k;
@@ -436,9 +473,14 @@ template <typename T, int LPR, int NV> int run(const Fwd& a) {
                                                            a.pos, a.counts);
   if (nblk > 1) {
     int32_t* totals = a.counts + static_cast<int64_t>(nblk) * a.E;
-    k_route_scan<<<a.E, 1024, 0, a.st>>>(a.counts, nblk, totals);
-    k_route_place<<<nblk, kThreads, 0, a.st>>>(a.experts, a.counts, totals, a.n, a.E, a.k, rb,
-                                              a.offsets, a.rows, a.pos);
+    if (static_cast<int64_t>(nblk) * a.E <= kSumCounts) {
+      k_route_place<true><<<nblk, kThreads, 0, a.st>>>(a.experts, a.counts, nullptr, a.n, a.E, a.k,
+                                                      rb, a.offsets, a.rows, a.pos);
+    } else {
+      k_route_scan<<<a.E, 1024, 0, a.st>>>(a.counts, nblk, totals);
+      k_route_place<false><<<nblk, kThreads, 0, a.st>>>(a.experts, a.counts, totals, a.n, a.E, a.k,
+                                                       rb, a.offsets, a.rows, a.pos);
+    }
   }
   return launched();
 }
