@@ -437,35 +437,85 @@ __device__ __forceinline__ void store_tile_rows(
     }
   }
 }
+// Small fp32 tiles leave from the registers, 32 bytes of a row by two lanes: without
+// room for them in LDS a compute unit holds four workgroups rather than three (fp32 512
+// -> 512, 8,000 positions: 53 us against 57; bf16 256 -> 64 to fp32, 348,208: 50 against
+// 54).
+template <bool MASK, bool WHOLE, bool RELU, int FM, int FN, int WR, int WC>
+__device__ __forceinline__ void store_tile_direct(const f32x16 (&acc)[FN][FM], const float* s_bias,
+                                                  const GroupedArgs& a, const Job& j, int n0) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
+  float* const y = static_cast<float*>(a.y);
+#pragma unroll
+  for (int m = 0; m < FM; ++m) {
+    const int r = wave / WC * FM * 32 + 32 * m + (lane & 31);
+    const int64_t row = (j.begin + r) * a.cols + n0;
+#pragma unroll
+    for (int n = 0; n < FN; ++n) {
+      const int c0 = col_of<WC>(wave % WC, n) + 4 * h;
+      u32x4_t g[4];
+      if constexpr (MASK) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          g[q] = load_left<float, WHOLE>(static_cast<const float*>(a.mask) + row + c0 + 8 * q,
+                                         r < j.nrow ? a.cols - n0 - c0 - 8 * q : 0);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = c0 + 8 * q, left = r < j.nrow ? a.cols - n0 - c : 0;
+        if (left <= 0) continue;
+        const float4 b = *reinterpret_cast<const float4*>(s_bias + c);
+        const float bias[4] = {b.x, b.y, b.z, b.w};
+        float v[4], z[4];
+        if constexpr (MASK) unpack(g[q], z);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = acc[n][m][4 * q + i] + bias[i];
+          if (RELU) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+          if (MASK) v[i] = z[i] <= 0.0f ? 0.0f : v[i];
+        }
+        store_left(y + row + c, pack(v), left);
+      }
+    }
+  }
+}
 // The forward (BT false) has a ReLU and no mask, the input gradient a mask.
-template <typename TO, bool BT, int BM, int BN, int WR, int WC, int BYTES>
+template <typename TO, bool BT, bool DIRECT, int BM, int BN, int WR, int WC, int BYTES>
 __device__ __forceinline__ void store_tile(
     u32x4_t* lds, const f32x16 (&acc)[BN / WC / 32][BM / WR / 32], const float* s_bias,
     const GroupedArgs& a, const Job& j, int n0) {
-  if (BT && a.mask && a.cols % Row<TO>::VEC == 0)
-    store_tile_rows<TO, BT, true, false, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
-  else if (BT && a.mask)
-    store_tile_rows<TO, BT, false, false, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
-  else if (!BT && a.relu)
-    store_tile_rows<TO, false, true, !BT, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
-  else
-    store_tile_rows<TO, false, true, false, BM, BN, WR, WC, BYTES>(lds, acc, s_bias, a, j, n0);
+  auto store = [&](auto mask, auto whole, auto relu) {
+    if constexpr (DIRECT)
+      store_tile_direct<mask.value, whole.value, relu.value, BM / WR / 32, BN / WC / 32, WR, WC>(
+          acc, s_bias, a, j, n0);
+    else
+      store_tile_rows<TO, mask.value, whole.value, relu.value, BM, BN, WR, WC, BYTES>(
+          lds, acc, s_bias, a, j, n0);
+  };
+  constexpr std::true_type yes;
+  constexpr std::false_type no;
+  constexpr std::bool_constant<BT> masks;
+  constexpr std::bool_constant<!BT> relus;
+  if (BT && a.mask && a.cols % Row<TO>::VEC == 0) store(masks, yes, no);
+  else if (BT && a.mask) store(masks, no, no);
+  else if (!BT && a.relu) store(no, yes, relus);
+  else store(no, yes, no);
 }
 
 // Rows x weights: BT false: w[e] is [red][cols] (the forward), BT true: w[e] is
 // [cols][red] (the input gradient).  A workgroup of WR x WC waves takes a tile of
 // BM positions by BN columns, in stages of 64 bytes of the reduction through a
-// ring of four LDS buffers: three stages are on their way while one is multiplied,
-// one barrier a stage.  Sums stay in fp32 and are rounded once, after bias and ReLU
+// ring of three or four LDS buffers: two or three stages are on their way while one is
+// multiplied, one barrier a stage.  Sums stay in fp32 and are rounded once, after bias and ReLU
 // or mask.  Whole 16-byte pieces at aligned addresses only (k_grouped_any takes the
 // others).  Bound by LDS and matrix cores in turn: a 256 x 256 bf16 stage keeps the
 // LDS about as long as the matrix cores, and a short reduction starts and ends cold.
 // 65,536 x 2048 -> 2048 bf16: 603 us, 912 TFLOP/s (a large library product 1,175);
 // 696,416 x 1024 -> 256 with a mask, backwards: 581 us, 628; 65,536 x 1024 -> 1024
-// fp32: 1,170 us, 117 TFLOP/s (154).
-template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC>
+// fp32: 1,160 us, 118 TFLOP/s (154).
+template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC, int kRing>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped(GroupedArgs a) {
-  constexpr int KB = 64, kRing = 4;
+  constexpr int KB = 64;
   typedef RTile<T, BM, KB> TA;
   typedef RTile<T, BN, KB> TBr;
   typedef KTile<T, BN, KB> TBk;
@@ -477,8 +527,9 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped(GroupedArgs a) {
   // (the first one also takes the finished tile; separate arrays, so that the
   // compiler knows which loads a read waits for)
   constexpr int kOut = BM * BN * static_cast<int>(sizeof(TO)) / 16;
-  constexpr int NP0 = kOut > NP && BM == 64 ? kOut : NP;
-  __shared__ u32x4_t s_buf0[NP0], s_buf1[NP], s_buf2[NP], s_buf3[NP];
+  constexpr bool kDirect = sizeof(TO) == 4 && BM == 64;
+  constexpr int NP0 = kOut > NP && BM == 64 && !kDirect ? kOut : NP;
+  __shared__ u32x4_t s_buf0[NP0], s_buf1[NP], s_buf2[NP], s_buf3[kRing == 4 ? NP : 1];
   __shared__ __attribute__((aligned(16))) float s_bias[BN];
   const T* const x = static_cast<const T*>(a.x);
   Job j;
@@ -563,15 +614,23 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped(GroupedArgs a) {
   };
   request(s_buf0);
   request(s_buf1);
-  request(s_buf2);
-  for (int s = 0; s < nk; s += kRing) {
-    stage(s_buf0, s_buf3);
-    if (s + 1 < nk) stage(s_buf1, s_buf0);
-    if (s + 2 < nk) stage(s_buf2, s_buf1);
-    if (s + 3 < nk) stage(s_buf3, s_buf2);
+  if constexpr (kRing == 4) {
+    request(s_buf2);
+    for (int s = 0; s < nk; s += kRing) {
+      stage(s_buf0, s_buf3);
+      if (s + 1 < nk) stage(s_buf1, s_buf0);
+      if (s + 2 < nk) stage(s_buf2, s_buf1);
+      if (s + 3 < nk) stage(s_buf3, s_buf2);
+    }
+  } else {
+    for (int s = 0; s < nk; s += kRing) {
+      stage(s_buf0, s_buf2);
+      if (s + 1 < nk) stage(s_buf1, s_buf0);
+      if (s + 2 < nk) stage(s_buf2, s_buf1);
+    }
   }
   stage_barrier<0>();                              // (no load is on its way to s_buf0)
-  store_tile<TO, BT, BM, BN, WR, WC, NP0 * 16>(s_buf0, acc, s_bias, a, j, j.n0);
+  store_tile<TO, BT, kDirect, BM, BN, WR, WC, NP0 * 16>(s_buf0, acc, s_bias, a, j, j.n0);
 }
 
 // 4 x 4 exchange among the four lanes of a quad: lane i's v[j] becomes lane j's
@@ -887,7 +946,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_grouped_any(GroupedArgs a) {
         acc, [&](int m, int q) { return rows_of(s_buf, m, q); },
         [&](int n, int q) { return weights_of(s_buf + TA::PIECES, BT ? 2 * n : n, q); });
   }
-  store_tile<TO, BT, BM, BN, 2, 2, NP * 16>(s_buf, acc, s_bias, a, j, n0);
+  store_tile<TO, BT, false, BM, BN, 2, 2, NP * 16>(s_buf, acc, s_bias, a, j, n0);
 }
 
 // Few positions in all (a row at a time through its experts): the weights' bytes,
@@ -1306,11 +1365,11 @@ bool grouped_grid(const GroupedArgs& a, int span, int threads, uint32_t* blocks)
   *blocks = static_cast<uint32_t>(n);
   return grid_fits(n, threads);
 }
-template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC>
+template <typename T, typename TO, bool BT, int BM, int BN, int WR, int WC, int RING = 4>
 int run_grouped(const GroupedArgs& a) {
   uint32_t blocks;
   if (!grouped_grid<BM>(a, BN, 64 * WR * WC, &blocks)) return SPCONV_EINVAL;
-  k_grouped<T, TO, BT, BM, BN, WR, WC><<<blocks, 64 * WR * WC, 0, a.st>>>(a);
+  k_grouped<T, TO, BT, BM, BN, WR, WC, RING><<<blocks, 64 * WR * WC, 0, a.st>>>(a);
   return launched();
 }
 template <typename T, typename TO, bool BT, int BM, int BN>
@@ -1351,11 +1410,15 @@ inline bool few_is_faster(const GroupedArgs& a, size_t bytes) {
 // be cut or unaligned; k_grouped_short for bf16 reductions of at most 256 and more
 // than one column tile, of many rows (256 -> 1024, 696,416 positions: 570 us against
 // 847); else k_grouped.  Its tiles are 64 x 64 for few columns and where 128 x 128
-// would not fill the card twice (bf16 512 -> 512, 8,000 positions: 20 us against
-// 26), for fp32 four times or without wasting columns (fp32 144 -> 80, 492,252
-// positions: 236 us against 268, but 80 -> 144 300 against 285; 1024 -> 1024, 65,536:
-// 1,170 against 1,290); for bf16 256 x 256 where they fill it twice and waste little
-// (2048 -> 2048, 65,536: 603 us against 692).
+// would not fill the card twice (bf16 512 -> 512, 8,000 positions: 20 us against 26),
+// for fp32 four times or without wasting columns (80 -> 144, 492,252 positions: 235
+// us against 300 of 128 x 128; 1024 -> 1024, 65,536: 1,250 against 1,160); for bf16
+// 256 x 256 where they fill it twice and waste little (2048 -> 2048, 65,536: 603 us
+// against 692).  64 x 64 tiles have a ring of four stages while the card holds all of
+// them, four a compute unit, at once (bf16 256 -> 1024, 2,000 positions: 13 us, a
+// ring of three 17), else of three, for six a compute unit to hide one another's
+// beginnings and ends (fp32 64 -> 64, 300,000: 43 us against 47; bf16 512 -> 512,
+// 8,000 of 8 groups: 16 against 18).
 template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
   if constexpr (!BT) {
     uint32_t blocks;
@@ -1382,6 +1445,8 @@ template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
     if (!small && 20 * c256 <= 11 * c128 + 1 && a.m / 256 * c256 >= 512)
       return run_grouped<T, TO, BT, 256, 256, 2, 4>(a);
   }
+  if (small && tile_bound(a.m, a.E, 64) * c64 > 1024)
+    return run_grouped<T, TO, BT, 64, 64, 2, 2, 3>(a);
   if (small) return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
   return run_grouped<T, TO, BT, 128, 128, 2, 2>(a);
 }
