@@ -1071,11 +1071,13 @@ __device__ __forceinline__ float frag_sum(float s, f32x4_t f) {
   return s;
 }
 
-// DMA: whole 16-byte pieces at aligned addresses, straight to LDS, through
-// a ring of four buffers as k_grouped's; else through registers, one buffer.
+// DMA: whole 16-byte pieces at aligned addresses, straight to LDS, through a ring of
+// four buffers as k_grouped's, of three for tiles below 256, so that one workgroup
+// more fits a compute unit (fp32 512 x 512 of 8 groups, 65,536 positions: 450 -> 408
+// us); else through registers, one buffer.
 template <typename T, int BC, int BN, int WR, int WC, bool DMA>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped_dw(WeightArgs a) {
-  constexpr int KB = DMA ? 64 : 128, kRing = 4;
+  constexpr int KB = DMA ? 64 : 128, kRing = BC == 256 ? 4 : 3;
   typedef KTile<T, BC, KB> TX;
   typedef KTile<T, BN, KB> TY;
   constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = 64 * WR * WC;
@@ -1083,7 +1085,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped_dw(WeightArgs a) {
   constexpr int PX = TX::PIECES / NT, PY = TY::PIECES / NT, NP = TX::PIECES + TY::PIECES;
   static_assert(NT % 256 == 0, "a lane's pieces of a stage have one place in their rows");
   constexpr int NR = DMA ? NP : 1;
-  __shared__ u32x4_t s_buf0[NP], s_buf1[NR], s_buf2[NR], s_buf3[NR];
+  __shared__ u32x4_t s_buf0[NP], s_buf1[NR], s_buf2[NR], s_buf3[kRing == 4 ? NR : 1];
   // The row numbers of NT positions at a time, three such runs: the one being
   // requested, the next one, and the one a slower wave may still read.
   __shared__ int32_t s_row[3][NT];
@@ -1183,12 +1185,20 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped_dw(WeightArgs a) {
     };
     request(s_buf0);
     request(s_buf1);
-    request(s_buf2);
-    for (int64_t s = 0; s < nk; s += kRing) {
-      stage(s_buf0, s_buf3);
-      if (s + 1 < nk) stage(s_buf1, s_buf0);
-      if (s + 2 < nk) stage(s_buf2, s_buf1);
-      if (s + 3 < nk) stage(s_buf3, s_buf2);
+    if constexpr (kRing == 4) {
+      request(s_buf2);
+      for (int64_t s = 0; s < nk; s += kRing) {
+        stage(s_buf0, s_buf3);
+        if (s + 1 < nk) stage(s_buf1, s_buf0);
+        if (s + 2 < nk) stage(s_buf2, s_buf1);
+        if (s + 3 < nk) stage(s_buf3, s_buf2);
+      }
+    } else {
+      for (int64_t s = 0; s < nk; s += kRing) {
+        stage(s_buf0, s_buf2);
+        if (s + 1 < nk) stage(s_buf1, s_buf0);
+        if (s + 2 < nk) stage(s_buf2, s_buf1);
+      }
     }
     stage_barrier<0>();                            // (no load to LDS outlives the workgroup)
   } else {
@@ -1292,8 +1302,10 @@ struct DwPlan {
   size_t bytes;
 };
 // The estimate it is chosen by, in us.  A stage of a tile (128 bytes: 16 or 32
-// positions) takes `alone` with one workgroup a compute unit and `full` with as
-// many as fit; a workgroup 3 us besides its stages; the chunks' sums are written
+// positions) takes `alone` with one workgroup a compute unit and `full` with four,
+// two or (256) one, which `slots` counts (another one or two fit and even out the
+// rest; counted too they were slower as often as faster); a workgroup 3 us besides
+// its stages; the chunks' sums are written
 // and read at 4 MB a us.  A group may have three times the mean.  (Measured at
 // 1,000 to 696,416 positions, 64 x 256 to 2048 x 2048: within 15 % of the best of
 // all tiles and chunks tried.)
