@@ -26,8 +26,8 @@ constexpr int kMaxE = SPCONV_ROUTE_MAX_EXPERTS;
 constexpr int kMaxK = SPCONV_ROUTE_MAX_SLOTS;
 constexpr int kPairs = 2048;           // pairs a workgroup ranks at most
 // Counts that k_route_place adds up itself, rather than in a launch of k_route_scan
-// (30,000 rows to 2 of 16, 7,504 counts: 20.2 -> 17.7 us; captured 16.7 either way, and
-// 17.4 -> 21.2 with 15,008).
+// (30,000 rows to 2 of 16, 7,504 counts: 20.2 -> 17.8 us, captured 16.7 -> 15.0; with
+// 15,008 counts and four loads a lane in flight, captured 17.4 -> 21.2).
 constexpr int kSumCounts = 8192;
 
 // Rows a workgroup takes: a power of two, at most 256 (one row a lane).
@@ -334,17 +334,26 @@ __global__ __launch_bounds__(kThreads) void k_route_place(
   __shared__ int32_t s_start[kMaxE], s_before[SUM ? kMaxE : 1], s_wave[kWaves];
   const int nblk = gridDim.x, blk = blockIdx.x;
   if constexpr (SUM) {
-    constexpr int N = 4;                           // experts whose loads are in flight together
+    constexpr int N = 4, U = 4;                    // experts, counts of each, in flight together
     for (int e0 = (threadIdx.x >> 6) * N; e0 < E; e0 += kWaves * N) {
       int32_t before[N] = {}, all[N] = {};
-      for (int b = threadIdx.x & 63; b < nblk; b += 64)
+      for (int b0 = threadIdx.x & 63; b0 < nblk; b0 += 64 * U) {
+        int32_t v[U][N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int e = e0 + i < E ? e0 + i : E - 1;
-          const int32_t v = counts[static_cast<int64_t>(e) * nblk + b];
-          all[i] += v;
-          before[i] += b < blk ? v : 0;
-        }
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const int e = e0 + i < E ? e0 + i : E - 1, b = b0 + 64 * u;
+            v[u][i] = counts[static_cast<int64_t>(e) * nblk + (b < nblk ? b : b0)];
+          }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            all[i] += b0 + 64 * u < nblk ? v[u][i] : 0;
+            before[i] += b0 + 64 * u < blk ? v[u][i] : 0;
+          }
+      }
 #pragma unroll
       for (int d = 1; d < 64; d *= 2)
 #pragma unroll
