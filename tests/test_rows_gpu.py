@@ -379,6 +379,23 @@ def test_grouped_many_rows(sizes, ci, co, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes,ci,co", [
+    ([300, 0, 77], 133, 72), ([40000, 9000], 66, 72), ([9000, 12000], 390, 264),
+    ([66000, 66001], 261, 264), ([66000, 66001], 256, 264)])
+def test_grouped_masks_of_cut_and_whole_rows(sizes, ci, co, dtype):
+    """The input gradient's mask in tiles of every size, with results of either type."""
+    r, off, m, _, _, w, _ = _groups_case(sizes, ci, co, DT[dtype], 11, False, 3)
+    dy = r(m, co, dtype=DT[dtype])
+    want, mag = ref.grouped(_f64(dy), _f64(w.transpose(1, 2).contiguous()), off, None, None, False)
+    offd, dyd, wd = torch.from_numpy(off).int().cuda(), dy.cuda(), w.cuda()
+    for odt in DT.values():
+        mask = r(m, ci, dtype=odt)
+        mask[m // 2, 0], mask[m - 4, ci - 1] = math.nan, -0.0
+        g = spc.grouped_backward_data(dyd, wd, offd, mask=mask.cuda(), out_dtype=odt)
+        _close(g, torch.where(mask.double() <= 0, 0.0, want), mag, co, (sizes, ci, co, odt))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_grouped_few_rows(dtype):
     """Up to a few dozen positions: one, several and all of them in a group, long reductions."""
     for sizes, ci, co in (([0, 1, 0, 0, 2], 512, 200), ([32], 1030, 64), ([5, 0, 9, 1], 7, 2048),
