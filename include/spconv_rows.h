@@ -139,7 +139,8 @@ int spconv_route_backward(int dt, const float* dweights, const void* logits,
  *   x        [n_x][C_in]
  *   w        [E][C_in][C_out]
  *   offsets  int32 [E+1], ascending within [0, m]; values outside are moved
- *            into that range, and a descending pair is an empty group
+ *            into that range, and one below those before it counts as the largest
+ *            of them: a descending pair is an empty group, and no position has two
  *   rows     int32 [m] or NULL (position j reads row j); an entry outside
  *            [0, n_x) reads a row of zeros
  *   bias     fp32 [E][C_out] or NULL

@@ -26,45 +26,100 @@ struct Tile {
   int index;                   // which of the group's tiles
 };
 
+// The positions [begin, end) of a group.
+struct Span {
+  int32_t begin, end;
+};
+__device__ __forceinline__ int32_t clamp_offset(int32_t v, int64_t m) {
+  return v < 0 ? 0 : v > m ? static_cast<int32_t>(m) : v;
+}
+// Those of group e0 + lane, the positions behind the last group as group E
+// (WITH_TAIL), none from there on.  Offsets are moved into [0, m], and one below
+// those before it counts as the largest of them: whatever they hold, groups do not
+// overlap, and so have no more tiles or chunks than a launch and its workspace are
+// sized for.  `top` is the largest offset up to e0's, for the next 64 groups then.
+// The whole wave calls it; offsets that ascend cost one comparison.
+template <bool WITH_TAIL>
+__device__ __forceinline__ Span group_span(const int32_t* __restrict__ offsets, int E, int64_t m,
+                                           int e0, int32_t* top) {
+  const int lane = threadIdx.x & 63, e = e0 + lane;
+  Span s{*top, *top};
+  if (e < E + (WITH_TAIL ? 1 : 0)) {
+    const int32_t a = offsets[e], b = offsets[e < E ? e + 1 : e];   // (both on their way)
+    s.begin = clamp_offset(a, m);
+    s.end = clamp_offset(e < E ? b : static_cast<int32_t>(m), m);
+  }
+  if (__ballot(s.begin < *top || s.end < s.begin)) {
+    s.begin = s.begin < *top ? *top : s.begin;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int32_t o = __shfl_up(s.begin, d, 64);
+      if (lane >= d && o > s.begin) s.begin = o;
+    }
+    s.end = s.end < s.begin ? s.begin : s.end;
+  }
+  *top = __builtin_amdgcn_readlane(s.end, 63);
+  return s;
+}
+// op over the lanes of a wave; all of them get it.
+template <typename Op> __device__ __forceinline__ uint32_t wave_reduce(uint32_t v, Op op) {
+  v = op(v, lane_other<1>(v));
+  v = op(v, lane_other<2>(v));
+  v = op(v, lane_other<4>(v));
+  v = op(v, lane_other<8>(v));
+  const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = op(p[0], p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return op(q[0], q[1]);
+}
+// A lane's part, of NT, of the largest offset up to group e's.
+template <int NT>
+__device__ __forceinline__ uint32_t part_top(const int32_t* __restrict__ offsets, int64_t m, int e) {
+  uint32_t top = 0;
+#pragma unroll 8
+  for (int g = threadIdx.x; g <= e; g += NT) {
+    const uint32_t o = static_cast<uint32_t>(clamp_offset(offsets[g], m));
+    top = o > top ? o : top;
+  }
+  return top;
+}
+
 // Tile t of the groups cut into tiles of BM positions, the positions behind
 // the last group as group E (WITH_TAIL).  Every wave of the workgroup calls it
-// and gets the same answer.  Offsets are moved into [0, m]; a group never
-// reaches beyond them.
+// and gets the same answer.
 template <bool WITH_TAIL>
 __device__ __forceinline__ Tile find_tile(const int32_t* __restrict__ offsets, int E, int64_t m,
                                           int64_t BM, int64_t t) {
   const int lane = threadIdx.x & 63;
   const int groups = E + (WITH_TAIL ? 1 : 0);
   int64_t before = 0;
+  int32_t top = 0;
   for (int e0 = 0; e0 < groups; e0 += 64) {
-    const int e = e0 + lane;
-    int64_t a = 0, b = 0;
-    if (e < groups) {
-      a = offsets[e];
-      b = e < E ? offsets[e + 1] : m;
-      a = a < 0 ? 0 : a > m ? m : a;
-      b = b < 0 ? 0 : b > m ? m : b;
-    }
-    const int64_t len = b > a ? b - a : 0;
-    const int tiles = static_cast<int>((len + BM - 1) / BM);
-    int sum = tiles;
+    const Span s = group_span<WITH_TAIL>(offsets, E, m, e0, &top);
+    const int tiles = static_cast<int>((static_cast<int64_t>(s.end) - s.begin + BM - 1) / BM);
+    // (the running sum only where the tile is among these groups')
+    const bool last = e0 + 64 >= groups;
+    const uint32_t all = last ? 0 : wave_reduce(static_cast<uint32_t>(tiles),
+                                                [](uint32_t u, uint32_t v) { return u + v; });
+    if (last || before + all > t) {
+      int sum = tiles;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int o = __shfl_up(sum, d, 64);
-      if (lane >= d) sum += o;
-    }
-    const uint64_t hit = __ballot(before + sum > t);
-    if (hit) {
+      for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(sum, d, 64);
+        if (lane >= d) sum += o;
+      }
+      const uint64_t hit = __ballot(before + sum > t);
+      if (!hit) break;
       const int src = __ffsll(static_cast<unsigned long long>(hit)) - 1;
       Tile r;
       r.group = e0 + src;
-      r.index = static_cast<int>(t - before) - (__shfl(sum, src, 64) - __shfl(tiles, src, 64));
-      const int64_t ga = __shfl(a, src, 64), gb = __shfl(b, src, 64);
-      r.begin = ga + static_cast<int64_t>(r.index) * BM;
-      r.end = r.begin + BM < gb ? r.begin + BM : gb;
+      r.index = static_cast<int>(t - before) - __builtin_amdgcn_readlane(sum - tiles, src);
+      const int64_t end = __builtin_amdgcn_readlane(s.end, src);
+      r.begin = __builtin_amdgcn_readlane(s.begin, src) + static_cast<int64_t>(r.index) * BM;
+      r.end = r.begin + BM < end ? r.begin + BM : end;
       return r;
     }
-    before += __shfl(sum, 63, 64);
+    before += all;
   }
   return Tile{-1, 0, 0, 0};
 }
@@ -1099,10 +1154,9 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped_dw(WeightArgs a) {
     t = find_tile<false>(a.offsets, a.E, a.m, a.chunk, job);
     if (t.group < 0) return;
   } else {
-    int64_t b = a.offsets[job], e = a.offsets[job + 1];
-    b = b < 0 ? 0 : b > a.m ? a.m : b;
-    e = e < b ? b : e > a.m ? a.m : e;
-    t = Tile{static_cast<int>(job), b, e, 0};
+    const int32_t begin = clamp_offset(a.offsets[job], a.m);
+    const int32_t end = clamp_offset(a.offsets[job + 1], a.m);
+    t = Tile{static_cast<int>(job), begin, end < begin ? begin : end, 0};
   }
   constexpr int RUN = NT / BK;                     // stages of a run
   auto row_of = [&](int64_t j) {
@@ -1110,10 +1164,33 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_grouped_dw(WeightArgs a) {
   };
   int64_t rj = t.begin;                            // the next stage to request
   int rq = 0, run = 0;                             // its place in its run, its run (mod 3)
-  s_row[0][threadIdx.x] = row_of(rj + threadIdx.x);
-  int32_t row_next = row_of(rj + NT + threadIdx.x);
-  __syncthreads();
+  int32_t row_next = 0;
+  auto first_rows = [&] {
+    s_row[0][threadIdx.x] = row_of(rj + threadIdx.x);
+    row_next = row_of(rj + NT + threadIdx.x);
+  };
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  first_rows();
+  if (!a.chunk && t.end > t.begin) {               // (uniform, as below)
+    // The group's own offset is meant to be the largest up to it: found out while the
+    // row numbers come, and mended where it is not (group_span).
+    const auto larger = [](uint32_t u, uint32_t v) { return u > v ? u : v; };
+    uint32_t top = wave_reduce(part_top<NT>(a.offsets, a.m, t.group), larger);
+    __shared__ uint32_t s_top[NT / 64];
+    if (lane == 0) s_top[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NT / 64; ++q) top = larger(top, s_top[q]);
+    top = __builtin_amdgcn_readfirstlane(top);     // (known to the compiler as uniform)
+    if (top > t.begin) {
+      rj = t.begin = top;
+      if (t.end < t.begin) t.end = t.begin;
+      first_rows();
+      __syncthreads();
+    }
+  } else {
+    __syncthreads();
+  }
   // a lane's first row of a stage and its column there, per operand: the place
   // in LDS that a lane's piece goes to is its own (DMA) or its piece's
   const int jx = threadIdx.x / TX::PR, px = threadIdx.x % TX::PR;
@@ -1255,12 +1332,12 @@ __global__ __launch_bounds__(kThreads) void k_grouped_dw_sum(
   const int e = blockIdx.y, lane = threadIdx.x % kLanes, run = threadIdx.x / kLanes;
   // chunks before group e, and its own (every wave finds them)
   int64_t first = 0, count = 0;
-  for (int g = threadIdx.x & 63; g <= e; g += 64) {
-    int64_t b = offsets[g], f = offsets[g + 1];
-    b = b < 0 ? 0 : b > m ? m : b;
-    f = f < b ? b : f > m ? m : f;
-    const int64_t c = (f - b + chunk - 1) / chunk;
-    if (g < e) first += c; else count = c;
+  int32_t top = 0;
+  for (int e0 = 0; e0 <= e; e0 += 64) {
+    const Span s = group_span<false>(offsets, E, m, e0, &top);
+    const int64_t c = (s.end - s.begin + chunk - 1) / chunk;
+    const int g = e0 + static_cast<int>(threadIdx.x & 63);
+    if (g < e) first += c; else if (g == e) count = c;
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
