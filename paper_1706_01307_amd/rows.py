@@ -263,6 +263,8 @@ def route_backward(dweights, logits, experts, weights, normalize=True, *, out=No
 # ---------------------------------------------------------------------------
 def _groups(w, offsets, dtype):
     w = _given(w, "w", (dtype,), None, 3)
+    for size in w.shape:
+        _i32(size)
     return w, _given(offsets, "offsets", _INT, (w.shape[0] + 1,))
 
 
@@ -323,7 +325,8 @@ def grouped_backward_weight(x, dy, offsets, *, rows=None, bias=True):
     x = _given(x, "x", _CODE, None, 2)
     dy = _given(dy, "dy", (x.dtype,), None, 2)
     offsets = _given(offsets, "offsets", _INT, None, 1)
-    E, ci, co, m = offsets.shape[0] - 1, x.shape[1], dy.shape[1], dy.shape[0]
+    E, ci, co = _i32(offsets.shape[0] - 1), _i32(x.shape[1]), _i32(dy.shape[1])
+    m = dy.shape[0]
     if rows is not None:
         rows = _given(rows, "rows", _INT, (m,))
     elif x.shape[0] != m:

@@ -61,3 +61,20 @@ def test_groups_do_not_overlap(E, m, ci, co, kind, dtype):
     _close(gb, db, mb, int(np.diff(cut).max()), "db")
     again = spc.grouped_backward_weight(xd, dyd, offd)
     assert torch.equal(gw, again[0]) and torch.equal(gb, again[1])
+
+
+def test_sizes_past_32_bits_are_refused():
+    """A width of 2^32 + 8 is not taken for one of 8 (tensors without elements)."""
+    wide = 2 ** 32 + 8
+
+    def empty(*shape):
+        return torch.empty(shape, device="cuda")
+    off0, off1 = (torch.zeros(e, dtype=torch.int32, device="cuda") for e in (1, 2))
+    for call in (lambda: spc.grouped_forward(empty(0, wide), empty(0, wide, 4), off0),
+                 lambda: spc.grouped_forward(empty(0, 8), empty(0, 8, wide), off0),
+                 lambda: spc.grouped_backward_data(empty(0, wide), empty(0, 8, wide), off0),
+                 lambda: spc.grouped_backward_data(empty(0, 4), empty(0, wide, 4), off0),
+                 lambda: spc.grouped_backward_weight(empty(0, wide), empty(0, 4), off1),
+                 lambda: spc.grouped_backward_weight(empty(0, 8), empty(0, wide), off1)):
+        with pytest.raises(ValueError):
+            call()
