@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "rows.h"
+#include "rows_plan.h"
 
 namespace spc {
 namespace {
@@ -74,7 +75,8 @@ template <typename Op> __device__ __forceinline__ uint32_t wave_reduce(uint32_t 
 }
 // A lane's part, of NT, of the largest offset up to group e's.
 template <int NT>
-__device__ __forceinline__ uint32_t part_top(const int32_t* __restrict__ offsets, int64_t m, int e) {
+__device__ __forceinline__ uint32_t part_top(const int32_t* __restrict__ offsets, int64_t m,
+                                             int e) {
   uint32_t top = 0;
 #pragma unroll 8
   for (int g = threadIdx.x; g <= e; g += NT) {
@@ -800,7 +802,6 @@ __device__ __forceinline__ void store_wave_rows(const f32x16 (&acc)[2][FM], cons
 // at 696,416 positions, and two workgroups of 128 rows a compute unit took 621.
 // (570 to 630 us from card to card, 580 to 640 TFLOP/s: the 1.4 GB of outputs alone
 // would take 210 at the fastest stores, and wait for the products of their tile.)
-constexpr int kShortRows = 256;
 constexpr int short_ring(int nk) { return nk == 6 ? 6 : 8; }
 template <typename TO, bool BT, int NK, bool RELU, bool MASK>
 __global__ __launch_bounds__(512, 2) void k_grouped_short(GroupedArgs a, int span) {
@@ -1370,79 +1371,6 @@ __global__ __launch_bounds__(kThreads) void k_grouped_dw_sum(
     for (int64_t c = 0; c < C_out; c += kLanes * 4) add(part_db, C_out, c + lane * 4, db);
 }
 
-// How the weight gradient is cut: tiles of dw of 64, 128 or (bf16, whole pieces)
-// 256 squared, and the positions of a group into chunks (chunk = 0: each group is
-// one, and its sums go straight to dw).
-struct DwPlan {
-  int tile;
-  int64_t chunk, jobs, tiles;
-  size_t bytes;
-};
-// The estimate it is chosen by, in us.  A stage of a tile (128 bytes: 16 or 32
-// positions) takes `alone` with one workgroup a compute unit and `full` with four,
-// two or (256) one, which `slots` counts (another one or two fit and even out the
-// rest; counted too they were slower as often as faster); a workgroup 3 us besides
-// its stages; the chunks' sums are written
-// and read at 4 MB a us.  A group may have three times the mean.  (Measured at
-// 1,000 to 696,416 positions, 64 x 256 to 2048 x 2048: within 15 % of the best of
-// all tiles and chunks tried.)
-double dw_cost(bool f32, int64_t m, int64_t groups, double values, int tile, double tiles,
-               int64_t chunk) {
-  const int t = tile == 64 ? 0 : tile == 128 ? 1 : 2;
-  static const double alone[2][3] = {{0.63, 0.98, 1.27}, {0.75, 1.6, 4.0}};
-  static const double full[2][3] = {{0.8, 1.2, 1.5}, {1.35, 2.2, 4.2}};
-  const double stage = f32 ? 16.0 : 32.0, slots = t == 0 ? 1024.0 : t == 1 ? 512.0 : 256.0;
-  const double mean = static_cast<double>(m) / groups, longest = groups > 1 ? 3.0 * mean : mean;
-  const double jobs = chunk ? static_cast<double>(m) / chunk + groups : groups;
-  const double rounds = jobs * tiles / slots, fill = rounds < 1.0 ? rounds : 1.0;
-  const double us = alone[f32][t] + (full[f32][t] - alone[f32][t]) * fill;
-  const double length = chunk && chunk < longest ? static_cast<double>(chunk) : longest;
-  const double unit = length / stage * us + 3.0, even = mean / stage * us + 3.0;
-  if (!chunk) return rounds * even > unit ? rounds * even : unit;
-  const double whole = static_cast<int64_t>(rounds) + (rounds > 3.0 ? 0.5 : 1.0);
-  return unit * whole + 4.0 + jobs * values * 8.0 / 4e6;
-}
-DwPlan dw_plan(int dt, int64_t m, int E, int C_in, int C_out, bool wide) {
-  const bool f32 = dt == SPCONV_F32;
-  const int64_t groups = m < 1 ? 1 : E < m ? E : m;
-  const double values = static_cast<double>(C_in) * C_out + C_out;
-  const int64_t least = C_in < C_out ? C_in : C_out, widest = C_in < C_out ? C_out : C_in;
-  DwPlan best{64, 0, E, 0, 0};
-  double cost = 0.0;
-  auto consider = [&](int tile, int64_t tiles, int64_t chunk) {
-    const double c = dw_cost(f32, m, groups, values, tile, static_cast<double>(tiles), chunk);
-    if (best.tiles && !(c < cost)) return;
-    cost = c;
-    best.tile = tile;
-    best.tiles = tiles;
-    best.chunk = chunk;
-  };
-  for (int tile = 64; tile <= 256; tile *= 2) {
-    if (tile == 128 && widest <= 64) break;
-    if (tile == 256 && (f32 || !wide || least <= 128)) break;
-    const int64_t tiles = ((C_in + tile - 1ll) / tile) * ((C_out + tile - 1ll) / tile);
-    consider(tile, tiles, 0);
-    for (int64_t chunk = 64; chunk < m; chunk *= 2) consider(tile, tiles, chunk);
-    // and what fills one to four rounds of the card
-    const int64_t slots = tile == 64 ? 1024 : tile == 128 ? 512 : 256;
-    for (int rounds = 1; rounds <= 4; ++rounds) {
-      const int64_t chunks = rounds * slots / tiles - groups;
-      const int64_t chunk = chunks > 0 ? ((m + chunks - 1) / chunks + 63) / 64 * 64 : 0;
-      // (one less than a whole number of rounds, by the estimate's rounding up)
-      if (chunk && chunk < m) consider(tile, tiles, chunk + 64);
-    }
-  }
-  if (best.chunk) {
-    best.jobs = m / best.chunk + groups;
-    best.bytes = static_cast<size_t>(best.jobs) * (static_cast<size_t>(C_in) * C_out + C_out) * 4;
-  }
-  return best;
-}
-
-// (groups never have more tiles than this)
-inline int64_t tile_bound(int64_t m, int64_t groups, int64_t BM) {
-  return m / BM + (groups < m ? groups : m);
-}
 // Whole aligned 16-byte pieces in rows of C elements from p.
 template <typename T> bool whole_rows(const void* p, int64_t C) {
   return C % Row<T>::VEC == 0 && aligned_to(p, 16);
@@ -1482,62 +1410,35 @@ template <typename TO, bool BT, int NK> int run_grouped_short(const GroupedArgs&
     k_grouped_short<TO, BT, NK, false, false><<<blocks, 512, 0, a.st>>>(a, span);
   return launched();
 }
-// Whether k_grouped_few is the faster for at most 32 positions of whole pieces, by
-// an estimate of both in us: tiles take 0.2 (bf16) or 0.34 a stage however few rows
-// they have; the few kernel's workgroups, above 64 of them, take turns.  (One
-// position, 2048 -> 512: bf16 17.2 and 9.7 us, fp32 48 and 7.8; four of as many
-// groups, 512 -> 2048: bf16 8.3 and 14.6.)
-inline bool few_is_faster(const GroupedArgs& a, size_t bytes) {
-  const int64_t piece = 16 / static_cast<int64_t>(bytes);
-  if (a.m > 32 || a.cols % piece) return false;
-  const double tiles = 5.0 + (bytes == 2 ? 0.2 / 32 : 0.34 / 16) * a.red;
-  const double blocks = static_cast<double>(tile_bound(a.m, a.E, 4)) * a.cols / (4 * piece);
-  const double k = a.red / 2048.0, over = blocks > 64 ? (blocks - 64) / 192 : 0.0;
-  return 6.4 + 2.5 * k + over * (4.0 + 10.0 * k) < tiles;
-}
-// Which kernel: k_grouped_few by the estimate above; k_grouped_any where pieces may
-// be cut or unaligned; k_grouped_short for bf16 reductions of at most 256 and more
-// than one column tile, of many rows (256 -> 1024, 696,416 positions: 570 us against
-// 847); else k_grouped.  Its tiles are 64 x 64 for few columns and where 128 x 128
-// would not fill the card twice (bf16 512 -> 512, 8,000 positions: 20 us against 26),
-// for fp32 four times or without wasting columns (80 -> 144, 492,252 positions: 235
-// us against 300 of 128 x 128; 1024 -> 1024, 65,536: 1,250 against 1,160); for bf16
-// 256 x 256 where they fill it twice and waste little (2048 -> 2048, 65,536: 603 us
-// against 692).  64 x 64 tiles have a ring of four stages while the card holds all of
-// them, four a compute unit, at once (bf16 256 -> 1024, 2,000 positions: 13 us, a
-// ring of three 17), else of three, for six a compute unit to hide one another's
-// beginnings and ends (fp32 64 -> 64, 300,000: 43 us against 47; bf16 512 -> 512,
-// 8,000 of 8 groups: 16 against 18).
+// The kernel that grouped_plan says.
 template <typename T, typename TO, bool BT> int by_size(const GroupedArgs& a) {
+  const bool whole = whole_rows<T>(a.x, a.red) && whole_rows<T>(a.w, BT ? a.red : a.cols);
+  const GroupedPlan p = grouped_plan(Row<T>::VEC == 4 ? SPCONV_F32 : SPCONV_BF16,
+                                     Row<TO>::VEC == 4 ? SPCONV_F32 : SPCONV_BF16, BT, a.m, a.E,
+                                     a.red, a.cols, whole);
   if constexpr (!BT) {
-    uint32_t blocks;
-    if (few_is_faster(a, sizeof(T)) && grouped_grid<4>(a, 4 * Row<T>::VEC, kFewThreads, &blocks)) {
+    if (p.kernel == GroupedKernel::kFew) {
+      uint32_t blocks;
+      if (!grouped_grid<4>(a, 4 * Row<T>::VEC, kFewThreads, &blocks)) return SPCONV_EINVAL;
       k_grouped_few<T, TO><<<blocks, kFewThreads, 0, a.st>>>(a);
       return launched();
     }
   }
-  const int64_t c256 = (a.cols + 255) / 256, c128 = (a.cols + 127) / 128;
-  const int64_t c64 = (a.cols + 63) / 64, tiles = tile_bound(a.m, a.E, 128) * c128;
-  const bool waste = c64 % 2 && c64 > 2 && c64 < 16;   // of the last 128 columns
-  const bool small = a.cols <= 64 || a.m <= 64ll * a.E ||
-                     (sizeof(T) == 2 ? tiles < 1024 : tiles < 2048 || waste);
-  if (!whole_rows<T>(a.x, a.red) || !whole_rows<T>(a.w, BT ? a.red : a.cols)) {
-    return small ? run_grouped_any<T, TO, BT, 64, 64>(a) : run_grouped_any<T, TO, BT, 128, 128>(a);
-  }
+  if (p.kernel == GroupedKernel::kAny)
+    return p.tile == 64 ? run_grouped_any<T, TO, BT, 64, 64>(a)
+                        : run_grouped_any<T, TO, BT, 128, 128>(a);
   if constexpr (sizeof(T) == 2) {
-    if (a.red <= 256 && a.cols > 128 && a.cols % Row<TO>::VEC == 0 && a.m >= 16384) {
-      if (a.red <= 64) return run_grouped_short<TO, BT, 2>(a);
-      if (a.red <= 128) return run_grouped_short<TO, BT, 4>(a);
-      if (a.red <= 192) return run_grouped_short<TO, BT, 6>(a);
+    if (p.kernel == GroupedKernel::kShort) {
+      if (p.ring == 2) return run_grouped_short<TO, BT, 2>(a);
+      if (p.ring == 4) return run_grouped_short<TO, BT, 4>(a);
+      if (p.ring == 6) return run_grouped_short<TO, BT, 6>(a);
       return run_grouped_short<TO, BT, 8>(a);
     }
-    if (!small && 20 * c256 <= 11 * c128 + 1 && a.m / 256 * c256 >= 512)
-      return run_grouped<T, TO, BT, 256, 256, 2, 4>(a);
+    if (p.tile == 256) return run_grouped<T, TO, BT, 256, 256, 2, 4>(a);
   }
-  if (small && tile_bound(a.m, a.E, 64) * c64 > 1024)
-    return run_grouped<T, TO, BT, 64, 64, 2, 2, 3>(a);
-  if (small) return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
-  return run_grouped<T, TO, BT, 128, 128, 2, 2>(a);
+  if (p.tile == 128) return run_grouped<T, TO, BT, 128, 128, 2, 2>(a);
+  if (p.ring == 3) return run_grouped<T, TO, BT, 64, 64, 2, 2, 3>(a);
+  return run_grouped<T, TO, BT, 64, 64, 2, 2>(a);
 }
 template <bool BT> int run_types(int in_dt, int out_dt, const GroupedArgs& a) {
   if (in_dt == SPCONV_BF16)
@@ -1642,14 +1543,15 @@ extern "C" int spconv_grouped_backward_weight(int dt, const void* x, int64_t n_x
   }
   if (dt == SPCONV_BF16) run_dw<bf16_t>(a, plan); else run_dw<float>(a, plan);
   if (plan.chunk) {
-    const uint32_t wide_grid = static_cast<uint32_t>((per + 4 * kThreads - 1) / (4 * kThreads));
-    const dim3 many(static_cast<uint32_t>((per + kThreads / 2 - 1) / (kThreads / 2)), E);
-    if (static_cast<int64_t>(wide_grid) * E < 1024 && plan.jobs > 4ll * E)
-      k_grouped_dw_sum<8><<<many, kThreads, 0, st>>>(a.dw, a.db, offsets, E, m, plan.chunk, per,
+    if (dw_sum_runs(plan, E, per) == 8) {
+      const dim3 grid(static_cast<uint32_t>((per + kThreads / 2 - 1) / (kThreads / 2)), E);
+      k_grouped_dw_sum<8><<<grid, kThreads, 0, st>>>(a.dw, a.db, offsets, E, m, plan.chunk, per,
                                                      C_out, dw, db);
-    else
-      k_grouped_dw_sum<1><<<dim3(wide_grid, E), kThreads, 0, st>>>(
-          a.dw, a.db, offsets, E, m, plan.chunk, per, C_out, dw, db);
+    } else {
+      const dim3 grid(static_cast<uint32_t>((per + 4 * kThreads - 1) / (4 * kThreads)), E);
+      k_grouped_dw_sum<1><<<grid, kThreads, 0, st>>>(a.dw, a.db, offsets, E, m, plan.chunk, per,
+                                                     C_out, dw, db);
+    }
   }
   return launched();
 }
