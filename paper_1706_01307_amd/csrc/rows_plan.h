@@ -43,9 +43,14 @@ inline bool few_is_faster(bool f32, int64_t m, int E, int red, int cols) {
 }
 
 // Which kernel: k_grouped_few by the estimate above; k_grouped_any where pieces may
-// be cut or unaligned; k_grouped_short for bf16 reductions of at most 256 and more
-// than one column tile, of many rows (256 -> 1024, 696,416 positions: 570 us against
-// 847); else k_grouped.  Its tiles are 64 x 64 for few columns and where 128 x 128
+// be cut or unaligned; k_grouped_short for bf16 reductions of at most 256 with at least
+// 2^28 results of more than 256 columns, in groups of a workgroup's rows on average,
+// fp32 results of whole 128-byte lines (256 -> 1024 of 16 groups, us of it and of the
+// tiles: 700,000 positions 586 and 690, 524,288 433 and 492, 262,144 232 and 229, 65,536
+// 118 and 70; 64 -> 256, 700,000: 100 and 100; 256 -> 256, 262,144: 122 and 80; 256 ->
+// 1024 of 256 groups, 16,384: 79 and 47; 128 -> 384, 700,000: 179 and 291; to fp32 245
+// and 354, but 40 -> 264, 1,016,800, to fp32 671 and 358; 256 -> 768, 349,525: 263 and
+// 240); else k_grouped.  Its tiles are 64 x 64 for few columns and where 128 x 128
 // would not fill the card twice (bf16 512 -> 512, 8,000 positions: 20 us against 26),
 // for fp32 four times or without wasting columns (80 -> 144, 492,252 positions: 235
 // us against 300 of 128 x 128; 1024 -> 1024, 65,536: 1,250 against 1,160); for bf16
@@ -67,7 +72,8 @@ inline GroupedPlan grouped_plan(int in_dt, int out_dt, bool backward, int64_t m,
   const bool small = cols <= 64 || m <= 64ll * E || (f32 ? tiles < 2048 || waste : tiles < 1024);
   if (!whole) return {GroupedKernel::kAny, small ? 64 : 128, 1};
   if (!f32) {
-    if (red <= 256 && cols > 128 && cols % (out_dt == SPCONV_F32 ? 4 : 8) == 0 && m >= 16384)
+    if (red <= 256 && cols > 256 && cols % (out_dt == SPCONV_F32 ? 32 : 8) == 0 && m >= 16384 &&
+        m >= 256ll * E && m * cols >= 1ll << 28)
       return {GroupedKernel::kShort, kShortRows,
               red <= 64 ? 2 : red <= 128 ? 4 : red <= 192 ? 6 : 8};
     if (!small && 20 * c256 <= 11 * c128 + 1 && m / 256 * c256 >= 512)

@@ -18,10 +18,12 @@ _PRODUCTS = [
     ("bf16", [5000, 0, 3301], 296, 1928, (TILES, 128, 4)),
     ("f32", [12000, 0, 5001], 152, 1928, (TILES, 128, 4)),
     ("bf16", [30000, 0, 14100], 296, 720, (TILES, 256, 4)),
-    ("bf16", [9000, 0, 7601], 40, 392, (SHORT, 256, 2)),
-    ("bf16", [9000, 0, 7601], 104, 392, (SHORT, 256, 4)),
-    ("bf16", [9000, 0, 7601], 168, 392, (SHORT, 256, 6)),
-    ("bf16", [9000, 0, 7601], 232, 392, (SHORT, 256, 8))]
+    # (reductions kept in registers: at least 2^28 results)
+    ("bf16", [299000, 0, 195001], 40, 544, (SHORT, 256, 2)),
+    ("bf16", [299000, 0, 195001], 104, 544, (SHORT, 256, 4)),
+    ("bf16", [299000, 0, 195001], 168, 544, (SHORT, 256, 6)),
+    ("bf16", [299000, 0, 195001], 232, 544, (SHORT, 256, 8)),
+    ("bf16", [299000, 0, 218001], 256, 520, (SHORT, 256, 8))]
 PRODUCTS = [(dt, backward, sizes, red, cols, plan)
             for dtypes, sizes, red, cols, plan in _PRODUCTS for dt in dtypes.split()
             for backward in ((False,) if plan[0] == FEW else (False, True))]

@@ -39,32 +39,54 @@ def _ids(case):
                                      else "")).rstrip("-")
 
 
+def _check(got, x, w, off, bias, finish, terms, what):
+    """Every position of `got` against finish(64-bit product, its positions), some rows at a time
+    on the device; x: the rows read, float64 on the device."""
+    E, m = len(off) - 1, len(x)
+    for e, a, b in ref.groups(off, m) + [(E, int(off[-1]), m)]:
+        for p in range(a, b, 50000):
+            q = min(p + 50000, b)
+            if e == E:                              # behind the last group
+                assert not got[p:q].any(), what
+                continue
+            want, mag = x[p:q] @ w[e], x[p:q].abs() @ w[e].abs()
+            if bias is not None:
+                want, mag = want + bias[e], mag + bias[e].abs()
+            want = finish(want, slice(p, q))
+            bound = (terms + 32) * ref.U * mag + 1e-36
+            if got.dtype == torch.bfloat16:
+                bound += ref.BF16 * want.abs()
+            bad = ~((got[p:q].double() - want).abs() <= bound)
+            assert not bool(bad.any()), (what, e, p, int(bad.sum()))
+
+
 @pytest.mark.parametrize("case", v.PRODUCTS, ids=_ids)
 def test_products(case):
     dtype, backward, sizes, red, cols, _ = case
     dt, r = DT[dtype], _gen(red + cols)
     off, offd, m, n_x, rows = _case(sizes, red)
     E = len(sizes)
-    w = r(E, red, cols, std=1 / math.sqrt(red), dtype=dt)
+    w = r(E, red, cols, std=1 / math.sqrt(red), dtype=dt).cuda()
+    w64 = w.double()
     if backward:
-        x = r(m, red, dtype=dt)
-        want, mag = ref.grouped(_f64(x), _f64(w), off, None, None, False)
-        wt = w.transpose(1, 2).contiguous().cuda()
+        x = r(m, red, dtype=dt).cuda()
+        x64, wt = x.double(), w.transpose(1, 2).contiguous()
         for odt in DT.values():
-            g = spc.grouped_backward_data(x.cuda(), wt, offd, out_dtype=odt)
-            _close(g, want, mag, red, "dx")
-            mask = r(m, cols, dtype=odt)
+            g = spc.grouped_backward_data(x, wt, offd, out_dtype=odt)
+            _check(g, x64, w64, off, None, lambda t, s: t, red, "dx")
+            mask = torch.randn(m, cols, device="cuda").to(odt)
             mask[m // 2, 0], mask[m - 4, cols - 1] = math.nan, -0.0
-            g = spc.grouped_backward_data(x.cuda(), wt, offd, mask=mask.cuda(), out_dtype=odt)
-            _close(g, torch.where(mask.double() <= 0, 0.0, want), mag, red, "dx with a mask")
+            g = spc.grouped_backward_data(x, wt, offd, mask=mask, out_dtype=odt)
+            _check(g, x64, w64, off, None, lambda t, s: torch.where(mask[s] <= 0, 0.0, t), red,
+                   "dx with a mask")
         return
-    x, b = r(n_x, red, dtype=dt), r(E, cols)
-    want, mag = ref.grouped(_f64(x), _f64(w), off, rows, _f64(b), False)
-    xd, wd, rd = x.cuda(), w.cuda(), rows.int().cuda()
+    x, b = r(n_x, red, dtype=dt), r(E, cols).cuda()
+    x64, b64 = ref.take(x.double(), rows, m).cuda(), b.double()
+    x, rows = x.cuda(), rows.int().cuda()
     for odt in DT.values():
         for relu in (False, True):
-            y = spc.grouped_forward(xd, wd, offd, rows=rd, bias=b.cuda(), relu=relu, out_dtype=odt)
-            _close(y, torch.where(want < 0, 0.0, want) if relu else want, mag, red + 1, "y")
+            y = spc.grouped_forward(x, w, offd, rows=rows, bias=b, relu=relu, out_dtype=odt)
+            _check(y, x64, w64, off, b64, lambda t, s: t.clamp(min=0) if relu else t, red + 1, "y")
 
 
 @pytest.mark.parametrize("case", v.WEIGHTS, ids=_ids)
