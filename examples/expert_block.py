@@ -46,12 +46,19 @@ class ExpertBlock:
     def _w(self, name):
         return self.params[name].to(self.dtype)
 
+    def serve(self):
+        """Keep the products' weights in the rows' dtype from now on, converted once."""
+        for name in ("wr", "w1", "w2"):
+            self.params[name] = self._w(name)
+
     def forward(self, x, step, train=True):
         """The block's output and what its gradient needs; `step` numbers the dropped elements."""
         q = self.params
         n, mean, rstd = spc.layer_norm_forward(x, q["gamma"], q["beta"], stats=train)
         # the router's product: one group of all rows
-        one = torch.tensor([0, x.shape[0]], dtype=torch.int32).to(x.device)
+        # (offsets made on the device: nothing here waits for the host, or keeps a graph from
+        # being captured)
+        one = torch.arange(2, dtype=torch.int32, device=x.device) * x.shape[0]
         logits = spc.grouped_forward(n, self._w("wr"), one, out_dtype=torch.float32)
         r = spc.route_forward(logits, self.k, self.normalize)
         h = spc.grouped_forward(n, self._w("w1"), r.offsets, rows=r.rows, bias=q["b1"], relu=True)
@@ -136,7 +143,8 @@ def main():
     dtype = torch.bfloat16 if a.dtype == "bf16" else torch.float32
     losses, block, x = train(a.sites, a.steps, dtype)
     print("loss: " + " ".join("%.4f" % v for v in losses[::max(1, a.steps // 10)]))
-    # one row at a time: its k experts alone are read
+    # one row at a time: its k experts alone are read (and no weights converted)
+    block.serve()
     whole, _ = block.forward(x, 0, train=False)
     for i in range(3):
         y, _ = block.forward(x[i:i + 1], 0, train=False)

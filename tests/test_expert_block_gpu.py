@@ -68,3 +68,36 @@ def test_block_trains_and_serves_single_rows(dtype):
         y, _ = block.forward(x[i:i + 1].contiguous(), 0, train=False)
         assert torch.equal(y[0], whole[i])
     assert torch.equal(block.forward(x, 0, train=False)[0], whole)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_block_is_captured_and_serves_converted_weights(dtype):
+    """Forward and gradients in a graph, replayed on new rows between eager ones; weights converted
+    once give what converting them in every call gives."""
+    block = ExpertBlock(40, 56, 6, 2, p=0.2, dtype=dtype, seed=3)
+    x, dy = (torch.randn(130, 40, device="cuda").to(dtype) for _ in range(2))
+
+    def step():
+        y, kept = block.forward(x, 5)
+        dx, grads = block.backward(dy, kept)
+        return [y, dx, *grads.values(), block.forward(x, 0, train=False)[0]]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(3):
+        x.normal_()
+        dy.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        out = [t.clone() for t in got]
+        for a, b in zip(out, step()):
+            assert torch.equal(a, b)
+    whole, _ = block.forward(x, 0, train=False)
+    block.serve()
+    for name in ("wr", "w1", "w2"):
+        assert block._w(name) is block.params[name] and block.params[name].dtype == dtype
+    assert torch.equal(block.forward(x, 0, train=False)[0], whole)
