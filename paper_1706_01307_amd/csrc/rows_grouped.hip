@@ -565,8 +565,10 @@ __device__ __forceinline__ void store_tile(
 // ring of three or four LDS buffers: two or three stages are on their way while one is
 // multiplied, one barrier a stage.  Sums stay in fp32 and are rounded once, after bias and ReLU
 // or mask.  Whole 16-byte pieces at aligned addresses only (k_grouped_any takes the
-// others).  Bound by LDS and matrix cores in turn: a 256 x 256 bf16 stage keeps the
-// LDS about as long as the matrix cores, and a short reduction starts and ends cold.
+// others).  Neither matrix cores nor LDS are its bound: of the cycles a compute unit has
+// work, the matrix cores are busy in 34 % and the LDS in 17 (256 x 256 bf16, reductions
+// of 1024), or in 56 to 60 % and 9 to 15 (64 x 64 fp32, reductions of 96 and 200); in the
+// others the waves wait, for the stages of a tile that begins, at barriers, for stores.
 // 65,536 x 2048 -> 2048 bf16: 603 us, 912 TFLOP/s (a large library product 1,175);
 // 696,416 x 1024 -> 256 with a mask, backwards: 581 us, 628; 65,536 x 1024 -> 1024
 // fp32: 1,160 us, 118 TFLOP/s (154).
@@ -1099,9 +1101,10 @@ __global__ __launch_bounds__(kFewThreads) void k_grouped_few(GroupedArgs a) {
 // with the positions as the reduction's rows.  Chunk `job` leaves its sums as
 // part[job] (one chunk per group: dw[group] itself).  The workgroups of the
 // first rows of dw also sum dy.  No atomics: the chunks are added in their order.
-// Bound as k_grouped, and by the gathered rows' latency: 696,416 positions of
-// 16 x 256 x 1024 bf16 take 690 us and 50 for the chunks' sums, 494 TFLOP/s in all;
-// 59,520 of 8 x 96 x 200 fp32 52 + 9 us (38, three quarters of each tile filled).
+// Bound as k_grouped (matrix cores 29 % of the busy cycles, LDS 12; fp32 60 and 8), and
+// by the gathered rows' latency: 696,416 positions of 16 x 256 x 1024 bf16 take 680 us and
+// 50 for the chunks' sums, 500 TFLOP/s in all; 59,520 of 8 x 96 x 200 fp32 52 + 9 us (38
+// TFLOP/s, three quarters of each tile filled).
 struct WeightArgs {
   const void* x;
   int64_t n_x;

@@ -150,8 +150,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd_wide(
 // dx = rstd (d - mean of d - z mean of d z).  With PARAM, a lane keeps its columns' sums
 // of dy z and dy over the rows its group takes (every gridDim.x * G-th batch of
 // UR rows); the groups' sums are added through LDS in group order and leave as
-// the workgroup's row of `part` ([2][C]; dgamma and dbeta themselves where one
-// workgroup has all rows).
+// the workgroup's row of `part` ([2][C]), which k_norm_parts adds up.
 template <typename T, int LPR, int NV, int UR, bool TAIL, bool PARAM>
 __global__ __launch_bounds__(kThreads) void k_norm_bwd(
     const T* __restrict__ dy, const T* __restrict__ x, const float* __restrict__ mean,
