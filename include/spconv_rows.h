@@ -9,7 +9,15 @@
  *                (row, slot) pairs grouped by expert;
  *   grouped      products of ragged groups of rows, each group with its own
  *                weights, and their gradients;
- *   combine      the weighted sum of a row's expert outputs, and its gradients.
+ *   combine      the weighted sum of a row's expert outputs, and its gradients;
+ *   rms norm     the residual added, every row divided by its root mean square,
+ *                its output in the rows' type or in 8 bits, and its gradients;
+ *   linear       dense products with bias, activation and residual, of rows in
+ *                bf16, fp32 or 8 bits, and their gradients;
+ *   route scores routing by sigmoid or softmax scores with a bias for balance,
+ *                in groups of experts, and its gradient;
+ *   8-bit rows   rows kept in 8 bits (a checkpoint of activations), as values
+ *                again, and as operands of the gradients above.
  *
  * Conventions shared by every entry point (statuses and dtypes are those of
  * spconv.h)
@@ -30,6 +38,13 @@
  * Results. Sums, statistics and weights are held in fp32 and rounded once to
  *          the output's type (round to nearest even).  No atomics decide an
  *          order of summation: repeated calls give bit-identical results.
+ * 8 bits.  Rows in 8 bits are e4m3 values q [n][C] (4 bits of exponent, 3 of
+ *          mantissa, no infinity) and an fp32 scale a row; they stand for
+ *          q * scale.  Written with top the row's largest magnitude, at least
+ *          2^-100: scale = top / 448, q = v * (448 / top) rounded to nearest
+ *          even.  A row with an infinity or NaN gets scale NaN and q = 0: it
+ *          stands for NaN.  Where an argument's dtype can be SPCONV_E4M3, its
+ *          scale is the pointer beside it, NULL for the other dtypes.
  * Indices. offsets, rows and pos are read on the device.  Entries out of range
  *          are never followed (each entry point says what they count as).
  * Errors.  EINVAL for a bad dtype, size, flag, NULL, misaligned or too small
@@ -50,6 +65,22 @@ extern "C" {
 /* Experts and slots a routing can have. */
 #define SPCONV_ROUTE_MAX_EXPERTS 1024
 #define SPCONV_ROUTE_MAX_SLOTS 16
+/* Groups of experts. */
+#define SPCONV_ROUTE_MAX_GROUPS 64
+
+/* Rows in 8 bits (a dtype where an entry point says so). */
+#define SPCONV_E4M3 2
+
+/* Scores of a routing. */
+#define SPCONV_SCORE_SIGMOID 0
+#define SPCONV_SCORE_SOFTMAX 1
+
+/* Activations: z; max(z, 0); z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2;
+ * z / (1 + exp(-z)). */
+#define SPCONV_ACT_NONE 0
+#define SPCONV_ACT_RELU 1
+#define SPCONV_ACT_GELU 2
+#define SPCONV_ACT_SILU 3
 
 /* Layer norm of every row:
  *   mean = sum x / C, rstd = 1 / sqrt(sum (x - mean)^2 / C + eps),
@@ -203,6 +234,117 @@ int spconv_combine_forward(int dt, const void* y, int64_t m, const int32_t* pos,
 int spconv_combine_backward(int dt, const void* dout, const void* y, const int32_t* pos,
                             const float* weights, const int32_t* count, void* dy,
                             float* dweights, int64_t m, int64_t n, int k, int C, void* stream);
+
+/* Root-mean-square norm with the residual's addition:
+ *   h = x + residual rounded to dt (x itself without a residual),
+ *   rstd = 1 / sqrt(sum h^2 / C + eps),  y = h * rstd * gamma.
+ *   dt        dtype of x, residual and h
+ *   residual  or NULL
+ *   gamma     fp32 [C] or NULL (1)
+ *   eps       >= 0 and finite
+ *   h         [n][C], or NULL if it is not wanted (NULL without a residual); may
+ *             be x or residual itself
+ *   out_dt    dt, or SPCONV_E4M3: y is then in 8 bits, packed from fp32, y_scale
+ *             its scales
+ *   rstd      fp32 [n] for the gradient, or NULL */
+int spconv_rms_norm_forward(int dt, const void* x, const void* residual, const float* gamma,
+                            float eps, void* h, int out_dt, void* y, float* y_scale, float* rstd,
+                            int64_t n, int C, void* stream);
+
+/* Workspace bytes of spconv_rms_norm_backward with dgamma. */
+int spconv_rms_norm_backward_workspace(int64_t n, int C, size_t* bytes);
+
+/* Gradients of the norm.  With z = h * rstd and g = dy * gamma:
+ *   dx     = rstd * (g - z * sum (g z) / C) + dh     (the residual's is the same)
+ *   dgamma = sum over rows of dy * z                  (fp32 [C])
+ *   h_dt   dt, or SPCONV_E4M3: h was kept in 8 bits
+ *   dh     what reaches h past the norm, dtype dt, or NULL (0)
+ * dgamma may be NULL; without it no workspace is needed (NULL, 0).  An output in
+ * 8 bits has the gradient of the values it was rounded from. */
+int spconv_rms_norm_backward(int dt, const void* dy, int h_dt, const void* h, const float* h_scale,
+                             const float* rstd, const float* gamma, const void* dh, void* dx,
+                             float* dgamma, int64_t n, int C, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Rows x [n][C] of dtype dt in 8 bits. */
+int spconv_pack_rows(int dt, const void* x, void* q, float* scale, int64_t n, int C, void* stream);
+
+/* y = act(q * scale), [n][C] of dtype out_dt. */
+int spconv_unpack_rows(const void* q, const float* scale, int act, int out_dt, void* y, int64_t n,
+                       int C, void* stream);
+
+/* Gradient of an activation: dz = dy * act'(pre), with pre [n][C] the
+ * activation's input, of dtype pre_dt = dt or SPCONV_E4M3.  The ReLU's slope at 0
+ * is 0.  dz may be dy itself. */
+int spconv_activation_backward(int dt, const void* dy, int pre_dt, const void* pre,
+                               const float* pre_scale, int act, void* dz, int64_t n, int C,
+                               void* stream);
+
+/* Dense products:  z = x w + bias,  y = act(z) + residual.
+ *   in_dt     dtype of x [n][C_in]; that of w [C_in][C_out] too, bf16 for rows in
+ *             8 bits
+ *   bias      fp32 [C_out] or NULL
+ *   residual  dtype out_dt, [n][C_out], or NULL; may be y itself
+ *   y, z      dtype out_dt, [n][C_out]; z NULL if it is not wanted (the gradient
+ *             of an activation takes it); y is computed from the unrounded z
+ * C_in and C_out up to 2^23, C_in * C_out < 2^31. */
+int spconv_linear_forward(int in_dt, const void* x, const float* x_scale, const void* w,
+                          const float* bias, int act, const void* residual, int out_dt, void* y,
+                          void* z, int64_t n, int C_in, int C_out, void* stream);
+
+/* Gradient of the product with respect to its input, through the activation that
+ * the input came out of:  dx = (dy w^T) * act'(pre).
+ *   dt      dtype of dy [n][C_out] and w
+ *   act     that activation; SPCONV_ACT_NONE: dx = dy w^T, pre NULL
+ *   pre     [n][C_in], its input, of dtype pre_dt = out_dt or SPCONV_E4M3
+ *   dx      dtype out_dt, [n][C_in] */
+int spconv_linear_backward_data(int dt, const void* dy, const void* w, int act, int pre_dt,
+                                const void* pre, const float* pre_scale, int out_dt, void* dx,
+                                int64_t n, int C_in, int C_out, void* stream);
+
+/* Workspace bytes of spconv_linear_backward_weight. */
+int spconv_linear_backward_weight_workspace(int x_dt, int64_t n, int C_in, int C_out,
+                                            size_t* bytes);
+
+/* Gradients of the weights and the bias:  dw = x^T dy,  db = sum over rows of dy.
+ *   x_dt  dtype of x [n][C_in]; that of dy [n][C_out] too, bf16 for rows in 8 bits
+ *   dw    fp32 [C_in][C_out];  db fp32 [C_out] or NULL
+ * Many rows are summed in chunks of a size fixed by the arguments, the chunks in
+ * ascending order. */
+int spconv_linear_backward_weight(int x_dt, const void* x, const float* x_scale, const void* dy,
+                                  float* dw, float* db, int64_t n, int C_in, int C_out,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Routing by scores s = sigmoid(logit) or the softmax of the row's logits:
+ *   bias        fp32 [E] or NULL (0): added to the scores for the choice alone
+ *   groups      the experts are so many groups of E / groups adjacent ones, at
+ *               most SPCONV_ROUTE_MAX_GROUPS; a group is worth the sum of its two
+ *               largest biased scores (its one's), and the top_groups worth most,
+ *               of equal ones the lowest, stay
+ *   k           1 <= k <= min(SPCONV_ROUTE_MAX_SLOTS, top_groups * E / groups)
+ *   experts     int32 [n][k]: of the groups that stay, the largest biased score
+ *               first, of equal ones the lowest expert.  Scores are compared as
+ *               64-bit arithmetic has them.  An expert whose logit or biased
+ *               score is -infinity is never chosen (-1 in the slots left over);
+ *               NaN ranks above every number.
+ *   weights     fp32 [n][k]: the chosen scores without the bias; normalize = 1:
+ *               divided by their sum (0 where that is 0); times scale (> 0 and
+ *               finite).  0 where no expert is chosen.
+ *   offsets, rows, pos and the workspace (spconv_route_workspace) as for
+ *               spconv_route_forward */
+int spconv_route_scores_forward(int dt, const void* logits, const float* bias, int64_t n, int E,
+                                int k, int score, int groups, int top_groups, int normalize,
+                                float scale, int32_t* experts, float* weights, int32_t* offsets,
+                                int32_t* rows, int32_t* pos, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* Gradient of those weights with respect to the logits (the choice itself has
+ * none), dlogits [n][E] of dtype dt.  dweights of slots without an expert are not
+ * read into anything.  logits may be NULL for softmax scores with normalize = 1. */
+int spconv_route_scores_backward(int dt, const float* dweights, const void* logits,
+                                 const int32_t* experts, const float* weights, int64_t n, int E,
+                                 int k, int score, int normalize, float scale, void* dlogits,
+                                 void* stream);
 
 #ifdef __cplusplus
 }

@@ -18,9 +18,11 @@ OK, EINVAL, EDUP, ERANGE, ENOMEM, ECAP, EHIP, ESCRATCH = 0, -1, -2, -3, -4, -5, 
 VSC, SC = 0, 1
 OP_VSC, OP_SC, OP_DC = 0, 1, 2
 POOL_MAX, POOL_AVG = 0, 1
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 BUILD_ASYNC, BUILD_TRANSPOSE = 1, 2
-ROUTE_MAX_EXPERTS, ROUTE_MAX_SLOTS = 1024, 16
+ROUTE_MAX_EXPERTS, ROUTE_MAX_SLOTS, ROUTE_MAX_GROUPS = 1024, 16, 64
+SCORES = {"sigmoid": 0, "softmax": 1}
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "silu": 3}
 
 # Every symbol spconv.h declares, with its ctypes signature.
 _P, _I, _I64, _U = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint
@@ -71,6 +73,20 @@ ROWS_SIGNATURES = {
                                             _SZ, _P]),
     "spconv_combine_forward": (_I, [_I, _P, _I64, _P, _P, _P, _P, _I64, _I, _I, _P]),
     "spconv_combine_backward": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I, _I, _P]),
+    "spconv_rms_norm_forward": (_I, [_I, _P, _P, _P, _F, _P, _I, _P, _P, _P, _I64, _I, _P]),
+    "spconv_rms_norm_backward_workspace": (_I, [_I64, _I, ctypes.POINTER(_SZ)]),
+    "spconv_rms_norm_backward": (_I, [_I, _P, _I, _P, _P, _P, _P, _P, _P, _P, _I64, _I, _P, _SZ,
+                                      _P]),
+    "spconv_pack_rows": (_I, [_I, _P, _P, _P, _I64, _I, _P]),
+    "spconv_unpack_rows": (_I, [_P, _P, _I, _I, _P, _I64, _I, _P]),
+    "spconv_activation_backward": (_I, [_I, _P, _I, _P, _P, _I, _P, _I64, _I, _P]),
+    "spconv_linear_forward": (_I, [_I, _P, _P, _P, _P, _I, _P, _I, _P, _P, _I64, _I, _I, _P]),
+    "spconv_linear_backward_data": (_I, [_I, _P, _P, _I, _I, _P, _P, _I, _P, _I64, _I, _I, _P]),
+    "spconv_linear_backward_weight_workspace": (_I, [_I, _I64, _I, _I, ctypes.POINTER(_SZ)]),
+    "spconv_linear_backward_weight": (_I, [_I, _P, _P, _P, _P, _P, _I64, _I, _I, _P, _SZ, _P]),
+    "spconv_route_scores_forward": (_I, [_I, _P, _P, _I64, _I, _I, _I, _I, _I, _I, _F, _P, _P, _P,
+                                         _P, _P, _P, _SZ, _P]),
+    "spconv_route_scores_backward": (_I, [_I, _P, _P, _P, _P, _I64, _I, _I, _I, _I, _F, _P, _P]),
 }
 
 

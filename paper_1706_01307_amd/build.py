@@ -15,7 +15,8 @@ SOURCES = ["abi.hip", "rulebook.hip", "forward.hip", "forward_w0.hip", "forward_
            "forward_w2.hip", "forward_slab_ff.hip", "forward_slab_fb.hip", "forward_slab_bf.hip",
            "forward_slab_bb.hip", "ops.hip", "sort.hip", "blockcache.hip", "noalloc.hip",
            "rows_norm.hip", "rows_dropout.hip", "rows_route.hip", "rows_grouped.hip",
-           "rows_combine.hip"]
+           "rows_combine.hip", "rows_rms.hip", "rows_unpack.hip", "rows_scores.hip",
+           "rows_linear.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

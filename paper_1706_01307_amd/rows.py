@@ -7,6 +7,13 @@
     u = combine_forward(z, r.pos, r.weights)
     out = dropout_forward(u, 0.1, seed, offset=step, residual=x)
 
+    n8, h, rstd = rms_norm_forward(x, gamma, residual=stream, packed=True)   # Rows8
+    y, z = linear_forward(n8, w, bias, act="gelu", pre=True)
+    r = route_scores_forward(logits, k, bias=balance, groups=8, top_groups=4)
+    z8 = pack_rows(z)                                          # kept for the backward pass
+    dz = linear_backward_data(dy2, w2, act="gelu", pre=z8)
+    dw, db = linear_backward_weight(n8, dz)
+
 Argument marshalling only (the C ABI is include/spconv_rows.h).  Tensors are on
 torch's current device; inputs that are not contiguous are copied.  Everything,
 copies included, runs on torch's current stream or on `stream`; tensors made on
@@ -18,24 +25,28 @@ import ctypes
 import functools
 
 from . import _lib
-from ._lib import BF16, F32, ROUTE_MAX_EXPERTS, ROUTE_MAX_SLOTS
+from ._lib import (ACTIVATIONS, BF16, E4M3, F32, ROUTE_MAX_EXPERTS, ROUTE_MAX_GROUPS,
+                   ROUTE_MAX_SLOTS, SCORES)
 
 __all__ = ["Routing", "layer_norm_forward", "layer_norm_backward", "dropout_forward",
            "dropout_backward", "route_forward", "route_backward", "grouped_forward",
            "grouped_backward_data", "grouped_backward_weight", "combine_forward",
-           "combine_backward", "ROUTE_MAX_EXPERTS", "ROUTE_MAX_SLOTS"]
+           "combine_backward", "Rows8", "rms_norm_forward", "rms_norm_backward", "pack_rows",
+           "unpack_rows", "activation_backward", "linear_forward", "linear_backward_data",
+           "linear_backward_weight", "route_scores_forward", "route_scores_backward",
+           "ROUTE_MAX_EXPERTS", "ROUTE_MAX_SLOTS", "ROUTE_MAX_GROUPS"]
 
 # What every call needs, set by the first one (torch is imported late here): a
 # call on a small tensor takes as long as its marshalling, so nothing is looked
 # up twice.
 torch = None
 _CODE = {}                 # dtype -> code; the types features can have
-_FLOAT = _INT = ()         # parameters' and indices' dtypes
+_FLOAT = _INT = _E4M3 = () # parameters', indices' and 8-bit values' dtypes
 _device = _raw_stream = _lib_fn = None
 
 
 def _ready():
-    global torch, _FLOAT, _INT, _device, _raw_stream, _lib_fn
+    global torch, _FLOAT, _INT, _E4M3, _device, _raw_stream, _lib_fn
     import torch as t
     lib = _lib.load()
     t.cuda.init()
@@ -44,7 +55,7 @@ def _ready():
         lambda dev: t.cuda.current_stream(dev).cuda_stream)
     _lib_fn = {name: getattr(lib, name) for name in _lib.ROWS_SIGNATURES}
     _CODE.update({t.float32: F32, t.bfloat16: BF16})
-    _FLOAT, _INT = (t.float32,), (t.int32,)
+    _FLOAT, _INT, _E4M3 = (t.float32,), (t.int32,), (t.float8_e4m3fn,)
     torch = t
 
 
@@ -55,7 +66,7 @@ def _on_stream(fn):
     def call(*args, stream=None, **kw):
         if torch is None:
             for t in args[:1]:
-                if not getattr(t, "is_cuda", False):
+                if not getattr(getattr(t, "q", t), "is_cuda", False):
                     raise TypeError("the first argument must be a cuda tensor")
             _ready()
         if stream is None:
@@ -63,8 +74,9 @@ def _on_stream(fn):
         with torch.cuda.stream(stream):
             out = fn(*args, **kw)
         for t in list(args) + list(kw.values()):
-            if isinstance(t, torch.Tensor) and t.is_cuda:
-                t.record_stream(stream)
+            for t in (t.q, t.scale) if isinstance(t, Rows8) else (t,):
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(stream)
         return out
     return call
 
@@ -385,3 +397,258 @@ def combine_backward(dout, y, pos, weights=None, *, offsets=None, out=None):
     _call("spconv_combine_backward", _CODE[y.dtype], _ptr(dout), _ptr(y), _ptr(pos), _ptr(weights),
           count, _ptr(dy), _ptr(dw), m, n, _i32(k), _i32(C))
     return dy, dw
+
+
+# ---------------------------------------------------------------------------
+# Rows in 8 bits
+# ---------------------------------------------------------------------------
+class Rows8:
+    """Rows kept in 8 bits: they stand for q * scale.
+
+    q      float8_e4m3fn [n, C];  scale  float32 [n]
+    """
+
+    __slots__ = ("q", "scale")
+
+    def __init__(self, q, scale):
+        self.q, self.scale = q, scale
+
+
+def _given8(r, name, shape=None):
+    """(q, scale) of Rows8, contiguous, of the shape (or of two dimensions)."""
+    if not isinstance(r, Rows8):
+        raise TypeError(f"{name} must be Rows8")
+    q = _given(r.q, f"{name}.q", _E4M3, shape, 2)
+    return q, _given(r.scale, f"{name}.scale", _FLOAT, (q.shape[0],))
+
+
+def _either(t, name, dtypes, shape=None):
+    """(tensor, scales or None, type's code) of a tensor of two dimensions or of Rows8."""
+    if isinstance(t, Rows8):
+        q, scale = _given8(t, name, shape)
+        return q, scale, E4M3
+    t = _given(t, name, dtypes, shape, 2)
+    return t, None, _CODE[t.dtype]
+
+
+def _act(act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {act!r}: use one of {tuple(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _new8(n, C, like):
+    return Rows8(torch.empty((n, C), dtype=torch.float8_e4m3fn, device=like.device),
+                 torch.empty(n, dtype=torch.float32, device=like.device))
+
+
+@_on_stream
+def pack_rows(x):
+    """Rows8 of x [n, C]: e4m3 values with a scale a row, the row's largest magnitude / 448.  A row
+    with an infinity or NaN stands for NaN."""
+    x = _given(x, "x", _CODE, None, 2)
+    n, C = x.shape
+    r = _new8(n, C, x)
+    _call("spconv_pack_rows", _CODE[x.dtype], _ptr(x), _ptr(r.q), _ptr(r.scale), n, _i32(C))
+    return r
+
+
+@_on_stream
+def unpack_rows(r, dtype=None, *, act=None, out=None):
+    """act(q * scale), [n, C] of dtype (bfloat16 by default): act None, "relu", "gelu" or "silu"."""
+    q, scale = _given8(r, "r")
+    n, C = q.shape
+    dtype = _out_dtype(torch.bfloat16 if dtype is None else dtype, q)
+    y = _result(out, (n, C), dtype, q)
+    _call("spconv_unpack_rows", _ptr(q), _ptr(scale), _act(act), _CODE[dtype], _ptr(y), n, _i32(C))
+    return y
+
+
+@_on_stream
+def activation_backward(dy, pre, act, *, out=None):
+    """dy * act'(pre): pre, the activation's input, of dy's dtype or Rows8.  out may be dy."""
+    dy = _given(dy, "dy", _CODE, None, 2)
+    n, C = dy.shape
+    pre, scale, code = _either(pre, "pre", (dy.dtype,), (n, C))
+    dz = _result(out, (n, C), dy.dtype, dy)
+    _call("spconv_activation_backward", _CODE[dy.dtype], _ptr(dy), code, _ptr(pre), _ptr(scale),
+          _act(act), _ptr(dz), n, _i32(C))
+    return dz
+
+
+# ---------------------------------------------------------------------------
+# Root-mean-square norm
+# ---------------------------------------------------------------------------
+@_on_stream
+def rms_norm_forward(x, gamma=None, eps=1e-6, *, residual=None, packed=False, stats=True, out=None,
+                     sum_out=None):
+    """(y, h, rstd): h = x + residual in x's dtype (x itself without a residual) and
+    y = h / sqrt(mean of h^2 + eps) * gamma, in x's dtype or, packed, as Rows8; gamma float32 [C] or
+    None.  h and rstd (float32 [n]; None with stats=False) are what rms_norm_backward needs.
+    sum_out (for h) may be x or residual; out is for y where it is not packed."""
+    x = _given(x, "x", _CODE, None, 2)
+    n, C = x.shape
+    h = x
+    if residual is not None:
+        residual = _given(residual, "residual", (x.dtype,), (n, C))
+        h = _result(sum_out, (n, C), x.dtype, x)
+    elif sum_out is not None:
+        raise ValueError("sum_out without a residual")
+    if gamma is not None:
+        gamma = _given(gamma, "gamma", _FLOAT, (C,))
+    if packed:
+        if out is not None:
+            raise ValueError("out is for an output that is not packed")
+        y = _new8(n, C, x)
+        yp, ys, code = _ptr(y.q), _ptr(y.scale), E4M3
+    else:
+        y = _result(out, (n, C), x.dtype, x)
+        yp, ys, code = _ptr(y), None, _CODE[x.dtype]
+    rstd = torch.empty(n, dtype=torch.float32, device=x.device) if stats else None
+    _call("spconv_rms_norm_forward", _CODE[x.dtype], _ptr(x), _ptr(residual), _ptr(gamma),
+          float(eps), None if residual is None else _ptr(h), code, yp, ys, _ptr(rstd), n, _i32(C))
+    return y, h, rstd
+
+
+@_on_stream
+def rms_norm_backward(dy, h, rstd, gamma=None, *, dh=None, params=None, out=None):
+    """(dx, dgamma) of rms_norm_forward: dx, of dy's dtype, is the gradient of x and of the
+    residual; h of that dtype or Rows8; dh what reaches h past the norm.  params says whether dgamma
+    (float32 [C]) is wanted; by default it is if gamma is given."""
+    dy = _given(dy, "dy", _CODE, None, 2)
+    n, C = dy.shape
+    h, scale, code = _either(h, "h", (dy.dtype,), (n, C))
+    rstd = _given(rstd, "rstd", _FLOAT, (n,))
+    if gamma is not None:
+        gamma = _given(gamma, "gamma", _FLOAT, (C,))
+    if dh is not None:
+        dh = _given(dh, "dh", (dy.dtype,), (n, C))
+    params = gamma is not None if params is None else params
+    dx = _result(out, (n, C), dy.dtype, dy)
+    dg = ws = None
+    nbytes = 0
+    if params:
+        dg = torch.empty(C, dtype=torch.float32, device=dy.device)
+        ws, nbytes = _workspace("spconv_rms_norm_backward_workspace", dy, n, _i32(C))
+    _call("spconv_rms_norm_backward", _CODE[dy.dtype], _ptr(dy), code, _ptr(h), _ptr(scale),
+          _ptr(rstd), _ptr(gamma), _ptr(dh), _ptr(dx), _ptr(dg), n, _i32(C), _ptr(ws), nbytes)
+    return dx, dg
+
+
+# ---------------------------------------------------------------------------
+# Dense products
+# ---------------------------------------------------------------------------
+@_on_stream
+def linear_forward(x, w, bias=None, *, act=None, residual=None, pre=False, out_dtype=None,
+                   out=None):
+    """(y, z): z = x @ w + bias and y = act(z) + residual.  x [n, C_in] or Rows8, w [C_in, C_out] of
+    x's dtype (bfloat16 for Rows8), bias float32 [C_out] or None, act None, "relu", "gelu" (its tanh
+    form) or "silu", residual [n, C_out] of the output's dtype (x's by default, bfloat16 for Rows8)
+    or None.  z is None unless pre is true.  out may be residual."""
+    x, scale, code = _either(x, "x", _CODE)
+    dtype = torch.bfloat16 if code == E4M3 else x.dtype
+    w = _given(w, "w", (dtype,), None, 2)
+    n, ci = x.shape
+    co = w.shape[1]
+    if w.shape[0] != ci:
+        raise ValueError(f"x has {ci} columns, w takes {w.shape[0]}")
+    if bias is not None:
+        bias = _given(bias, "bias", _FLOAT, (co,))
+    out_dtype = _out_dtype(dtype if out_dtype is None else out_dtype, x)
+    if residual is not None:
+        residual = _given(residual, "residual", (out_dtype,), (n, co))
+    y = _result(out, (n, co), out_dtype, x)
+    z = torch.empty((n, co), dtype=out_dtype, device=x.device) if pre else None
+    _call("spconv_linear_forward", code, _ptr(x), _ptr(scale), _ptr(w), _ptr(bias), _act(act),
+          _ptr(residual), _CODE[out_dtype], _ptr(y), _ptr(z), n, _i32(ci), _i32(co))
+    return y, z
+
+
+@_on_stream
+def linear_backward_data(dy, w, *, act=None, pre=None, out_dtype=None, out=None):
+    """dx = (dy @ w^T) * act'(pre), [n, C_in]: act is the activation that the product's input came
+    out of and pre that activation's input, of the output's dtype (dy's by default) or Rows8."""
+    dy = _given(dy, "dy", _CODE, None, 2)
+    w = _given(w, "w", (dy.dtype,), None, 2)
+    n, (ci, co) = dy.shape[0], w.shape
+    if dy.shape[1] != co:
+        raise ValueError(f"dy has {dy.shape[1]} columns, w gives {co}")
+    out_dtype = _out_dtype(out_dtype, dy)
+    scale, code = None, _CODE[out_dtype]
+    if (pre is None) != (act is None):
+        raise ValueError("act and pre go together")
+    if pre is not None:
+        pre, scale, code = _either(pre, "pre", (out_dtype,), (n, ci))
+    dx = _result(out, (n, ci), out_dtype, dy)
+    _call("spconv_linear_backward_data", _CODE[dy.dtype], _ptr(dy), _ptr(w), _act(act), code,
+          _ptr(pre), _ptr(scale), _CODE[out_dtype], _ptr(dx), n, _i32(ci), _i32(co))
+    return dx
+
+
+@_on_stream
+def linear_backward_weight(x, dy, *, bias=True):
+    """(dw float32 [C_in, C_out], db float32 [C_out] or None) of linear_forward with the same x (of
+    dy's dtype, or Rows8 with a bfloat16 dy)."""
+    x, scale, code = _either(x, "x", _CODE)
+    dy = _given(dy, "dy", (torch.bfloat16 if code == E4M3 else x.dtype,), None, 2)
+    n, ci, co = x.shape[0], _i32(x.shape[1]), _i32(dy.shape[1])
+    if dy.shape[0] != n:
+        raise ValueError(f"x has {n} rows, dy {dy.shape[0]}")
+    ws, nbytes = _workspace("spconv_linear_backward_weight_workspace", x, code, n, ci, co)
+    dw = torch.empty((ci, co), dtype=torch.float32, device=x.device)
+    db = torch.empty(co, dtype=torch.float32, device=x.device) if bias else None
+    _call("spconv_linear_backward_weight", code, _ptr(x), _ptr(scale), _ptr(dy), _ptr(dw), _ptr(db),
+          n, ci, co, _ptr(ws), nbytes)
+    return dw, db
+
+
+# ---------------------------------------------------------------------------
+# Routing by scores
+# ---------------------------------------------------------------------------
+def _score(score):
+    if score not in SCORES:
+        raise ValueError(f"unknown score {score!r}: use one of {tuple(SCORES)}")
+    return SCORES[score]
+
+
+@_on_stream
+def route_scores_forward(logits, k, *, score="sigmoid", bias=None, groups=1, top_groups=1,
+                         normalize=True, scale=1.0):
+    """Send every row of logits [n, E] to the experts of its k largest scores ("sigmoid" or
+    "softmax") plus bias (float32 [E] or None; for the choice alone), from the top_groups of `groups`
+    groups of adjacent experts whose two best add up to most.  Weights are the chosen scores, divided
+    by their sum (normalize) and times scale.  Scores are compared as 64-bit arithmetic has them;
+    ties to the lowest expert; an expert whose logit is -inf is never chosen."""
+    logits = _given(logits, "logits", _CODE, None, 2)
+    n, E = logits.shape
+    if bias is not None:
+        bias = _given(bias, "bias", _FLOAT, (E,))
+    dev, k = logits.device, int(k)
+    ws, nbytes = _workspace("spconv_route_workspace", logits, n, _i32(E), _i32(k))
+    ints = functools.partial(torch.empty, dtype=torch.int32, device=dev)
+    r = Routing(ints((n, k)), torch.empty((n, k), dtype=torch.float32, device=dev), ints(E + 1),
+                ints(n * k), ints((n, k)))
+    _call("spconv_route_scores_forward", _CODE[logits.dtype], _ptr(logits), _ptr(bias), n, E, k,
+          _score(score), _i32(int(groups)), _i32(int(top_groups)), 1 if normalize else 0,
+          float(scale), _ptr(r.experts), _ptr(r.weights), _ptr(r.offsets), _ptr(r.rows),
+          _ptr(r.pos), _ptr(ws), nbytes)
+    return r
+
+
+@_on_stream
+def route_scores_backward(dweights, logits, experts, weights, *, score="sigmoid", normalize=True,
+                          scale=1.0, out=None):
+    """dlogits [n, E] (dtype of logits) from the gradient of the weights, float32 [n, k]."""
+    logits = _given(logits, "logits", _CODE, None, 2)
+    n, E = logits.shape
+    dweights = _given(dweights, "dweights", _FLOAT, None, 2)
+    k = dweights.shape[1]
+    if dweights.shape[0] != n:
+        raise ValueError(f"dweights has {dweights.shape[0]} rows, logits {n}")
+    experts = _given(experts, "experts", _INT, (n, k))
+    weights = _given(weights, "weights", _FLOAT, (n, k))
+    d = _result(out, (n, E), logits.dtype, logits)
+    _call("spconv_route_scores_backward", _CODE[logits.dtype], _ptr(dweights), _ptr(logits),
+          _ptr(experts), _ptr(weights), n, _i32(E), _i32(k), _score(score), 1 if normalize else 0,
+          float(scale), _ptr(d))
+    return d
