@@ -4,8 +4,7 @@
 // 8-bit rows are multiplied as the bf16 numbers they are (every e4m3 value is one), and the
 // row's scale is taken out of the sum: forwards it is a factor of the finished row, in the
 // weight gradient, where the sum runs over the rows, it goes to the other operand, scale *
-// dy, which enters as two bf16 numbers (its upper 8 and the next 8 bits: 2^-17 of a factor
-// is lost, less than an fp32 sum of as many terms loses).
+// dy, which enters as the sum of two f16 numbers.
 #include <type_traits>
 
 #include "rows_act.h"
@@ -56,112 +55,266 @@ __device__ __forceinline__ uint2 load8_left(const uint8_t* p, int64_t left) {
 }
 
 // The finished tile of a workgroup of WR x WC waves, FM x FN blocks each, leaves through LDS
-// as fp32 rows, a row block of every wave at a time: everything behind the product is done
-// on fp32 and rounded once, whole rows go to memory, and a lane has the same columns all along
-// (its bias stays in registers).  The residual, or the activation's input, is asked for before
-// the barrier that its block's sums wait at.
+// (BYTES of it) as fp32 rows, a row block of every wave and FNP column blocks at a time:
+// everything behind the product is done on fp32 and rounded once, whole rows go to memory, and
+// a lane has the same columns for all row blocks (their bias stays in registers).  The
+// residual, or the activation's input, is asked for before the barrier that its block's sums
+// wait at.
 // Forward: z = acc * scale + bias (z is kept if asked for), y = act(z) + residual.
 // BT (input gradient): y = acc * act'(side).
-template <typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC>
+template <typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC, int BYTES, bool PAST>
 __device__ __forceinline__ void finish_tile(u32x4_t* lds,
                                             const f32x16 (&acc)[BN / WC / 32][BM / WR / 32],
                                             const LinearArgs& a, int64_t row0, int n0) {
   constexpr int FM = BM / WR / 32, FN = BN / WC / 32, VO = Row<TO>::VEC, NT = 64 * WR * WC;
-  constexpr int RW = WR * 32, PR = BN / VO, NPC = RW * PR / NT, Q = VO / 4;
+  constexpr int RW = WR * 32, FNP = RW * BN * 4 <= BYTES ? FN : 1, CW = WC * 32 * FNP;
+  constexpr int PR = CW / VO, NPC = RW * PR / NT, Q = VO / 4;
+  static_assert(RW * CW * 4 <= BYTES, "a part of the finished tile fits");
   static_assert(NT % PR == 0 && NPC * NT == RW * PR, "a lane's pieces lie in the same columns");
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
-  const int wrow = wave / WC, wcol = wave % WC;
-  const int piece = threadIdx.x % PR, col = n0 + piece * VO, left = a.cols - col;
-  float bias[VO];
-#pragma unroll
-  for (int e = 0; e < VO; ++e) bias[e] = 0.0f;
-  if (!BT && a.bias) {
-#pragma unroll
-    for (int e = 0; e < VO; ++e)
-      if (e < left) bias[e] = a.bias[col + e];
-  }
+  const int wrow = wave / WC, wcol = wave % WC, piece = threadIdx.x % PR;
   const bool side8 = BT && a.side_scale;
 #pragma unroll
-  for (int m = 0; m < FM; ++m) {
-    u32x4_t g[NPC];
-    float xs[NPC];
-    int64_t at[NPC];
-    bool live[NPC];
+  for (int np = 0; np < FN; np += FNP) {
+    const int col = n0 + WC * 32 * np + piece * VO, left = a.cols - col;
+    float bias[VO];
 #pragma unroll
-    for (int i = 0; i < NPC; ++i) {
-      const int lr = (threadIdx.x + NT * i) / PR;
-      const int64_t r = row0 + lr / 32 * (BM / WR) + 32 * m + lr % 32;
-      live[i] = r < a.n && left > 0;
-      at[i] = r * a.cols + col;
-      xs[i] = X8 && live[i] ? a.x_scale[r] : 1.0f;
-      if (a.side && live[i]) {
-        if (side8) {
-          const uint2 u = load8_left(static_cast<const uint8_t*>(a.side) + at[i], left < VO ? left : VO);
-          g[i][0] = u.x, g[i][1] = u.y;
-          xs[i] = a.side_scale[r];
-        } else {
-          g[i] = load_left<TO, false>(static_cast<const TO*>(a.side) + at[i], left);
+    for (int e = 0; e < VO; ++e) bias[e] = 0.0f;
+    if (!BT && a.bias) {
+#pragma unroll
+      for (int e = 0; e < VO; ++e)
+        if (e < left) bias[e] = a.bias[col + e];
+    }
+#pragma unroll
+    for (int m = 0; m < FM; ++m) {
+      u32x4_t g[NPC];
+      float xs[NPC];
+      int64_t at[NPC];
+      bool live[NPC];
+#pragma unroll
+      for (int i = 0; i < NPC; ++i) {
+        const int lr = (threadIdx.x + NT * i) / PR;
+        const int64_t r = row0 + lr / 32 * (BM / WR) + 32 * m + lr % 32;
+        live[i] = r < a.n && left > 0;
+        at[i] = r * a.cols + col;
+        xs[i] = X8 && live[i] ? a.x_scale[r] : 1.0f;
+        if (a.side && live[i]) {
+          if (side8) {
+            const uint2 u = load8_left(static_cast<const uint8_t*>(a.side) + at[i],
+                                       left < VO ? left : VO);
+            g[i][0] = u.x, g[i][1] = u.y;
+            xs[i] = a.side_scale[r];
+          } else {
+            g[i] = load_left<TO, false>(static_cast<const TO*>(a.side) + at[i], left);
+          }
         }
       }
-    }
-    __syncthreads();
+      __syncthreads();
 #pragma unroll
-    for (int n = 0; n < FN; ++n)
+      for (int f = 0; f < FNP; ++f)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        // 4 adjacent columns of one row in every four registers of a lane
-        const int c = col_of<WC>(wcol, n) + 8 * q + 4 * h;
-        u32x4_t v;
+        for (int q = 0; q < 4; ++q) {
+          // 4 adjacent columns of one row in every four registers of a lane
+          const int c = col_of<WC>(wcol, f) + 8 * q + 4 * h;
+          u32x4_t v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(acc[n][m][4 * q + i]);
-        lds[out_at<float, BN>(wrow * 32 + (lane & 31), c / 4)] = v;
-      }
-    __syncthreads();
+          for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(acc[np + f][m][4 * q + i]);
+          lds[out_at<float, CW>(wrow * 32 + (lane & 31), c / 4)] = v;
+        }
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NPC; ++i) {
-      if (!live[i]) continue;
-      const int lr = (threadIdx.x + NT * i) / PR;
-      float v[VO];
+      for (int i = 0; i < NPC; ++i) {
+        if (!live[i]) continue;
+        const int lr = (threadIdx.x + NT * i) / PR;
+        float v[VO];
 #pragma unroll
-      for (int q = 0; q < Q; ++q) {
-        const u32x4_t u = lds[out_at<float, BN>(lr, piece * Q + q)];
+        for (int q = 0; q < Q; ++q) {
+          const u32x4_t u = lds[out_at<float, CW>(lr, piece * Q + q)];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * q + e] = __uint_as_float(u[e]);
-      }
-      if constexpr (BT) {
-        if (a.side) {
-          float s[VO];
-          if (side8) {
+          for (int e = 0; e < 4; ++e) v[4 * q + e] = __uint_as_float(u[e]);
+        }
+        if constexpr (BT) {
+          if (a.side) {
+            float s[VO];
+            if (side8) {
 #pragma unroll
-            for (int q = 0; q < Q; ++q) unpack_e4m3(g[i][q], s + 4 * q);
+              for (int q = 0; q < Q; ++q) unpack_e4m3(g[i][q], s + 4 * q);
 #pragma unroll
-            for (int e = 0; e < VO; ++e) s[e] *= xs[i];
-          } else {
-            unpack(g[i], s);
+              for (int e = 0; e < VO; ++e) s[e] *= xs[i];
+            } else {
+              unpack(g[i], s);
+            }
+            by_act(a.act, [&](auto k) {
+#pragma unroll
+              for (int e = 0; e < VO; ++e) v[e] *= slope<decltype(k)::value>(s[e]);
+            });
           }
+        } else {
+#pragma unroll
+          for (int e = 0; e < VO; ++e) v[e] = X8 ? v[e] * xs[i] + bias[e] : v[e] + bias[e];
+          if (a.z) store_left<TO, PAST>(static_cast<TO*>(a.z) + at[i], pack(v), left);
           by_act(a.act, [&](auto k) {
 #pragma unroll
-            for (int e = 0; e < VO; ++e) v[e] *= slope<decltype(k)::value>(s[e]);
+            for (int e = 0; e < VO; ++e) v[e] = activate<decltype(k)::value>(v[e]);
           });
+          if (a.side) {
+            float s[VO];
+            unpack(g[i], s);
+#pragma unroll
+            for (int e = 0; e < VO; ++e) v[e] += s[e];
+          }
         }
-      } else {
-#pragma unroll
-        for (int e = 0; e < VO; ++e) v[e] = X8 ? v[e] * xs[i] + bias[e] : v[e] + bias[e];
-        if (a.z) store_left<TO>(static_cast<TO*>(a.z) + at[i], pack(v), left);
-        by_act(a.act, [&](auto k) {
-#pragma unroll
-          for (int e = 0; e < VO; ++e) v[e] = activate<decltype(k)::value>(v[e]);
-        });
-        if (a.side) {
-          float s[VO];
-          unpack(g[i], s);
-#pragma unroll
-          for (int e = 0; e < VO; ++e) v[e] += s[e];
-        }
+        store_left<TO, PAST>(static_cast<TO*>(a.y) + at[i], pack(v), left);
       }
-      store_left<TO>(static_cast<TO*>(a.y) + at[i], pack(v), left);
     }
   }
+}
+
+// A workgroup's tile: rows from row0, columns from n0 (the column tiles of one row tile side by
+// side on one die, whose L2 then has their rows).
+struct TileAt {
+  int64_t row0;
+  int n0;
+};
+template <int BM, int BN> __device__ __forceinline__ TileAt tile_at(int cols) {
+  const int ncol = (cols + BN - 1) / BN;
+  const int64_t id = die_order(blockIdx.x, gridDim.x);
+  return TileAt{id / ncol * BM, static_cast<int>(id % ncol) * BN};
+}
+
+// Rows of BK e4m3 values in LDS, as RTile; a fragment is 8 bytes, widened when it is read.
+template <int R, int BK> struct RTile8 {
+  static constexpr int PR = BK / 16, PIECES = R * PR;      // (a piece is a step of the reduction)
+  __device__ static int at(int row, int piece) {
+    return row * PR + (piece ^ (PR == 4 ? (row >> 2) & 3 : (row >> 3) & 1));
+  }
+  struct Reader {
+    int place[PR];
+    __device__ Reader(int r0, int lane) {
+#pragma unroll
+      for (int s = 0; s < PR; ++s)
+        place[s] = lane_place(at(r0 + (lane & 31), s) * 16 + 8 * (lane >> 5));
+    }
+    __device__ bf16x8 operator()(const u32x4_t* t, int b, int s) const {
+      const uint2 u = lds_at<uint2>(t, place[s] + b * 32 * BK);
+      return __builtin_bit_cast(bf16x8, widen(u.x, u.y));
+    }
+  };
+};
+
+// Rows x weights of whole aligned 16-byte pieces: BT false: w is [red][cols] (the forward), BT
+// true: w is [cols][red] (the input gradient).  A workgroup of WR x WC waves takes a tile of BM
+// rows by BN columns, in stages of BK of the reduction through a ring of LDS buffers: all but
+// one stage are on their way while that one is multiplied, one barrier a stage.
+template <typename T, typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC, bool PAST>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_linear(LinearArgs a) {
+  // (rows in 8 bits: 64 of them are too few pieces for the lanes in stages of 32)
+  constexpr int KB = X8 && BM == 64 ? 128 : 64, BK = kBK<T, KB>, NT = 64 * WR * WC;
+  constexpr int kRing = 3;
+  typedef std::conditional_t<X8, RTile8<BM, BK>, RTile<T, BM, KB>> TA;
+  typedef RTile<T, BN, KB> TBr;
+  typedef KTile<T, BN, KB> TBk;
+  constexpr int VEC = Row<T>::VEC, VX = X8 ? 16 : VEC;     // elements of a piece
+  constexpr int FM = BM / WR / 32, FN = BN / WC / 32;
+  constexpr int PA = TA::PIECES / NT, PB = TBk::PIECES / NT;
+  constexpr int NP = TA::PIECES + TBk::PIECES;
+  static_assert(PA * NT == TA::PIECES && PB * NT == TBk::PIECES, "whole pieces a lane");
+  // (the first one also takes the finished tile; separate arrays, so that the compiler
+  // knows which loads a read waits for)
+  constexpr int kOut = WR * 32 * WC * 32 / 4, NP0 = kOut > NP ? kOut : NP;
+  __shared__ u32x4_t s_buf0[NP0], s_buf1[NP], s_buf2[NP];
+  typedef std::conditional_t<X8, uint8_t, T> TX;
+  const TX* const x = static_cast<const TX*>(a.x);
+  const T* const w = static_cast<const T*>(a.w);
+  const TileAt t = tile_at<BM, BN>(a.cols);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+
+  // What this lane stages of the rows: rows ra0 + NT / PR * i, of each the piece that
+  // belongs at its place in LDS.  A row that is not there is read as zeros, at one place all
+  // along (step 0).
+  constexpr int PRA = TA::PR, PRB = TBr::PR;
+  static_assert(NT / PRA % 16 == 0 && NT / PRB % 16 == 0, "a lane's pieces have one place in their rows");
+  const int ra0 = threadIdx.x / PRA, ka = (TA::at(ra0, threadIdx.x % PRA) - ra0 * PRA) * VX;
+  const TX* const zero = reinterpret_cast<const TX*>(&g_zeros);
+  const TX* pa[PA];
+  int step[PA];
+#pragma unroll
+  for (int i = 0; i < PA; ++i) {
+    const int64_t r = t.row0 + ra0 + NT / PRA * i;
+    step[i] = r < a.n ? BK : 0;
+    pa[i] = r < a.n ? x + r * a.red + ka : zero;
+  }
+  const int nk = (a.red + BK - 1) / BK;
+  // And of the weights, from the stage's own place; columns past the last one are read as
+  // others (nothing of them is stored).
+  const int kb = BT ? threadIdx.x / PRB : threadIdx.x / TBk::PR;
+  const int kr = BT ? (TBr::at(kb, threadIdx.x % PRB) - kb * PRB) * VEC : 0;
+  uint32_t pb[PB];
+#pragma unroll
+  for (int i = 0; i < PB; ++i) {
+    if constexpr (BT) {
+      const int n = kb + NT / PRB * i;
+      pb[i] = static_cast<uint32_t>(t.n0 + n < a.cols ? n : 0) * a.red + kr;
+    } else {
+      const int n = (TBk::at(kb, threadIdx.x % TBk::PR) - kb * TBk::PR) * VEC;
+      pb[i] = static_cast<uint32_t>(kb + NT / TBk::PR * i) * a.cols + (t.n0 + n < a.cols ? n : 0);
+    }
+  }
+  // Stages past the last one are asked for too, as zeros, so that the number of loads
+  // behind a stage's own is known.
+  int rk = 0;                                      // the next stage to request
+  auto request = [&](u32x4_t* buf) {
+    const int left = a.red - rk;                   // of the reduction
+    const T* const ws = BT ? w + static_cast<int64_t>(t.n0) * a.red + rk
+                           : w + static_cast<int64_t>(rk) * a.cols + t.n0;
+    if (left >= BK) {
+#pragma unroll
+      for (int i = 0; i < PA; ++i) {
+        load_to_lds(pa[i], buf + NT * i + 64 * wave);
+        pa[i] += step[i];
+      }
+#pragma unroll
+      for (int i = 0; i < PB; ++i)
+        load_to_lds(ws + pb[i], buf + TA::PIECES + NT * i + 64 * wave);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PA; ++i)
+        load_to_lds(ka < left ? pa[i] : zero, buf + NT * i + 64 * wave);
+#pragma unroll
+      for (int i = 0; i < PB; ++i)
+        load_to_lds((BT ? kr : kb + NT / TBk::PR * i) < left
+                        ? static_cast<const void*>(ws + pb[i]) : &g_zeros,
+                    buf + TA::PIECES + NT * i + 64 * wave);
+    }
+    rk += BK;
+  };
+
+  const typename TA::Reader rows_of(wave / WC * (BM / WR), lane);
+  const std::conditional_t<BT, typename TBr::Reader, typename TBk::template Reader<32 * WC, FN>>
+      weights_of(32 * (wave % WC), lane);
+  f32x16 acc[FN][FM];
+#pragma unroll
+  for (int n = 0; n < FN; ++n)
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
+  auto stage = [&](const u32x4_t* buf, u32x4_t* before) {
+    stage_barrier<(PA + PB) * (kRing - 2)>();
+    request(before);
+    multiply_stage<T, KB, FM, FN>(
+        acc, [&](int m, int q) { return rows_of(buf, m, q); },
+        [&](int n, int q) { return weights_of(buf + TA::PIECES, BT ? WC * n : n, q); });
+  };
+  request(s_buf0);
+  request(s_buf1);
+  for (int s = 0; s < nk; s += kRing) {
+    stage(s_buf0, s_buf2);
+    if (s + 1 < nk) stage(s_buf1, s_buf0);
+    if (s + 2 < nk) stage(s_buf2, s_buf1);
+  }
+  stage_barrier<0>();                              // (no load is on its way to s_buf0)
+  finish_tile<TO, X8, BT, BM, BN, WR, WC, NP0 * 16, PAST>(s_buf0, acc, a, t.row0, t.n0);
 }
 
 // Rows x weights for any alignment and width: BT false: w is [red][cols] (the forward), BT true:
@@ -178,12 +331,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_any(LinearArgs a) {
   constexpr int FM = BM / 64, FN = BN / 64;
   constexpr int PA = TA::PIECES / kThreads, PB = TBk::PIECES / kThreads;
   constexpr int NP = TA::PIECES + TBk::PIECES;
-  static_assert(NP * 16 >= 64 * BN * 4, "a row block of the finished tile fits");
   __shared__ u32x4_t s_buf[NP];
-  const int ncol = (a.cols + BN - 1) / BN;
-  const int64_t id = die_order(blockIdx.x, gridDim.x);
-  const int64_t row0 = id / ncol * BM;
-  const int n0 = static_cast<int>(id % ncol) * BN;
+  const TileAt t = tile_at<BM, BN>(a.cols);
+  const int64_t row0 = t.row0;
+  const int n0 = t.n0;
   const T* const w = static_cast<const T*>(a.w);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int ra0 = threadIdx.x >> 3, ka = (threadIdx.x & 7) * VEC;
@@ -241,13 +392,106 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_any(LinearArgs a) {
         acc, [&](int m, int q) { return rows_of(s_buf, m, q); },
         [&](int n, int q) { return weights_of(s_buf + TA::PIECES, BT ? 2 * n : n, q); });
   }
-  finish_tile<TO, X8, BT, BM, BN, 2, 2>(s_buf, acc, a, row0, n0);
+  finish_tile<TO, X8, BT, BM, BN, 2, 2, NP * 16, false>(s_buf, acc, a, row0, n0);
+}
+
+// Few rows (one at a time): the weights' bytes, once, and the time to the last of them are all
+// there is.  A workgroup of 16 waves takes up to 4 rows and 64 bytes of columns, 4 lanes
+// side by side; its 256 slices of the reduction run down the weights' rows on the vector ALU,
+// 8 loads of a slice in flight, and are added over the lanes, then the waves, in order.
+constexpr int kFewThreads = 1024, kFewRows = 4;
+template <typename T, typename TO, bool X8>
+__global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
+  constexpr int VEC = Row<T>::VEC, R = kFewRows, CL = 4, NC = CL * VEC, KS = kFewThreads / CL;
+  constexpr int KC = 2048, UN = 8;                 // of the reduction in LDS; loads in flight
+  constexpr int NW = kFewThreads / 64;
+  __shared__ float s_x[R][KC];
+  __shared__ float s_sum[NW][R][NC];
+  const T* const w = static_cast<const T*>(a.w);
+  const TileAt t = tile_at<R, NC>(a.cols);
+  const int slice = threadIdx.x / CL, c = t.n0 + threadIdx.x % CL * VEC;
+  float acc[R][VEC];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[r][i] = 0.0f;
+  const int sr = threadIdx.x / (kFewThreads / R);  // the row a lane stages
+  const int64_t src = t.row0 + sr;
+  for (int k0 = 0; k0 < a.red; k0 += KC) {
+    const int kc = a.red - k0 < KC ? a.red - k0 : KC;
+    u32x4_t u[UN];
+    auto request = [&](int k1) {
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        const int k = k1 + KS * i;
+        u[i] = load_piece(k < kc && c < a.cols ? w + static_cast<int64_t>(k0 + k) * a.cols + c
+                                               : reinterpret_cast<const T*>(&g_zeros));
+      }
+    };
+    request(slice);                                // (on their way while the rows are staged)
+    __syncthreads();
+    for (int k = threadIdx.x % (kFewThreads / R); k < kc; k += kFewThreads / R) {
+      float v = 0.0f;
+      if (src < a.n) {
+        const int64_t at = src * a.red + k0 + k;
+        if constexpr (X8)
+          v = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<const uint8_t*>(a.x)[at], false)[0];
+        else
+          v = Row<T>::get(static_cast<const T*>(a.x)[at]);
+      }
+      s_x[sr][k] = v;
+    }
+    __syncthreads();
+    for (int k1 = slice; k1 < kc; k1 += KS * UN) {
+      if (k1 != slice) request(k1);
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        const int k = k1 + KS * i;
+        if (k >= kc) break;
+        float v[VEC];
+        unpack(u[i], v);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[r][e] = fmaf(s_x[r][k], v[e], acc[r][e]);
+      }
+    }
+  }
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float v = acc[r][e];
+      v += row_rotate<8>(v);
+      v += row_rotate<4>(v);
+      const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                      false);
+      v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+      const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                      false);
+      v = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+      if (lane < CL) s_sum[wave][r][lane * VEC + e] = v;
+    }
+  __syncthreads();
+  if (threadIdx.x >= R * NC) return;
+  const int r = threadIdx.x / NC, col = t.n0 + threadIdx.x % NC;
+  if (t.row0 + r >= a.n || col >= a.cols) return;
+  const int64_t at = (t.row0 + r) * a.cols + col;
+  float z = 0.0f;
+#pragma unroll
+  for (int q = 0; q < NW; ++q) z += s_sum[q][r][threadIdx.x % NC];
+  if (X8) z *= a.x_scale[t.row0 + r];
+  if (a.bias) z += a.bias[col];
+  if (a.z) static_cast<TO*>(a.z)[at] = Row<TO>::put(z);
+  by_act(a.act, [&](auto k) { z = activate<decltype(k)::value>(z); });
+  if (a.side) z += Row<TO>::get(static_cast<const TO*>(a.side)[at]);
+  static_cast<TO*>(a.y)[at] = Row<TO>::put(z);
 }
 
 // Weight gradient of a BC x BN tile over a chunk of the rows: dw[c][n] = sum_j x[j][c] dy[j][n],
-// the rows staged as the reduction, through registers.  Chunk `job` leaves its sums as
-// part[job]; the workgroups of the first rows of dw also sum dy.  No atomics: the chunks are
-// added in their order.
+// the rows staged as the reduction.  Chunk `job` leaves its sums as part[job]; the workgroups of
+// the first rows of dw also sum dy.  No atomics: the chunks are added in their order.
 struct LinearWeight {
   const void* x;
   const float* x_scale;
@@ -257,47 +501,193 @@ struct LinearWeight {
   int C_in, C_out;
   hipStream_t st;
 };
-template <typename T, bool X8, int BC, int BN>
-__global__ __launch_bounds__(kThreads, 2) void k_linear_dw(LinearWeight a) {
-  constexpr int KB = 128, WC = 2;
+// A workgroup's tile of dw and its rows.
+struct WeightJob {
+  int64_t job, begin, end;
+  int c0, n0;
+};
+template <int BC, int BN> __device__ __forceinline__ WeightJob weight_job(const LinearWeight& a) {
+  const int64_t nc = (a.C_in + BC - 1) / BC, nn = (a.C_out + BN - 1) / BN;
+  const int64_t id = die_order(blockIdx.x, gridDim.x), job = id / (nc * nn);
+  const int64_t begin = job * a.chunk, end = begin + a.chunk < a.n ? begin + a.chunk : a.n;
+  return WeightJob{job, begin, end, static_cast<int>(id / nn % nc) * BC,
+                   static_cast<int>(id % nn) * BN};
+}
+// The finished tile, straight from the registers (32 bytes of a row by two lanes).
+template <int FC, int FN>
+__device__ __forceinline__ void store_sums(const f32x16 (&acc)[FN][FC], const LinearWeight& a,
+                                           int64_t job, int r0, int c0, float unit) {
+  const int lane = threadIdx.x & 63;
+  float* out = a.dw + job * a.C_in * a.C_out;
+#pragma unroll
+  for (int n = 0; n < FN; ++n)
+#pragma unroll
+    for (int m = 0; m < FC; ++m) {
+      const int64_t r = r0 + 32 * m + (lane & 31);
+      if (r >= a.C_in) continue;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = c0 + 32 * n + 8 * q + 4 * (lane >> 5);
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = acc[n][m][4 * q + i] * unit;
+        if (c < a.C_out) store_left(out + r * a.C_out + c, pack(v), a.C_out - c);
+      }
+    }
+}
+
+// Whole aligned 16-byte pieces: straight to LDS through a ring of three stages of 64 bytes.
+template <typename T, int BC, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw_ring(LinearWeight a) {
+  constexpr int KB = 64, kRing = 3;
   typedef KTile<T, BC, KB> TX;
   typedef KTile<T, BN, KB> TY;
-  constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = kThreads;
-  constexpr int FC = BC / 64, FN = BN / 64;
+  constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = 64 * WR * WC;
+  constexpr int FC = BC / WR / 32, FN = BN / WC / 32;
+  constexpr int PX = TX::PIECES / NT, PY = TY::PIECES / NT, NP = TX::PIECES + TY::PIECES;
+  static_assert(NT / TX::PR % 4 == 0 && NT / TY::PR % 4 == 0 && (sizeof(T) == 2 || (NT / TX::PR % 8 == 0 && NT / TY::PR % 8 == 0)),
+                "a lane's pieces of a stage have one place in their rows");
+  __shared__ u32x4_t s_buf0[NP], s_buf1[NP], s_buf2[NP];
+  const T *const x = static_cast<const T*>(a.x), *const dy = static_cast<const T*>(a.dy);
+  const WeightJob t = weight_job<BC, BN>(a);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int jx = threadIdx.x / TX::PR, jy = threadIdx.x / TY::PR;
+  const int cx = t.c0 + (TX::at(jx, threadIdx.x % TX::PR) - jx * TX::PR) * VEC;
+  const int cy = t.n0 + (TY::at(jy, threadIdx.x % TY::PR) - jy * TY::PR) * VEC;
+  // columns past the last one are read as others: nothing of them is stored
+  const T* px = x + (t.begin + jx) * a.C_in + (cx < a.C_in ? cx : 0);
+  const T* py = dy + (t.begin + jy) * a.C_out + (cy < a.C_out ? cy : 0);
+  const int64_t sx = static_cast<int64_t>(NT / TX::PR) * a.C_in;
+  const int64_t sy = static_cast<int64_t>(NT / TY::PR) * a.C_out;
+  const T* const zero = reinterpret_cast<const T*>(&g_zeros);
+  int64_t rj = t.begin;                            // the next stage to request
+  // (stages past the last one are asked for too, as zeros)
+  auto request = [&](u32x4_t* buf) {
+    const int64_t left = t.end - rj;
+#pragma unroll
+    for (int i = 0; i < PX; ++i)
+      load_to_lds(left >= BK || jx + NT / TX::PR * i < left ? px + sx * i : zero,
+                  buf + NT * i + 64 * wave);
+#pragma unroll
+    for (int i = 0; i < PY; ++i)
+      load_to_lds(left >= BK || jy + NT / TY::PR * i < left ? py + sy * i : zero,
+                  buf + TX::PIECES + NT * i + 64 * wave);
+    rj += BK;
+    px += static_cast<int64_t>(BK) * a.C_in;
+    py += static_cast<int64_t>(BK) * a.C_out;
+  };
+  const int wr = wave / WC * (BC / WR), wc = wave % WC * (BN / WC);
+  const bool bias = a.db && t.c0 == 0 && wr == 0;  // (uniform over the wave)
+  f32x16 acc[FN][FC];
+  float sum[FN];
+#pragma unroll
+  for (int n = 0; n < FN; ++n) {
+    sum[n] = 0.0f;
+#pragma unroll
+    for (int m = 0; m < FC; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
+  }
+  const typename TX::template Reader<32, FC> x_of(wr, lane);
+  const typename TY::template Reader<32, FN> dy_of(wc, lane);
+  auto stage = [&](const u32x4_t* buf, u32x4_t* before) {
+    stage_barrier<(PX + PY) * (kRing - 2)>();
+    request(before);
+    multiply_stage<T, KB, FC, FN>(
+        acc, [&](int m, int q) { return x_of(buf, m, q); },
+        [&](int n, int q) {
+          const typename Mma<T>::Frag f = dy_of(buf + TX::PIECES, n, q);
+          if (bias) sum[n] = frag_sum(sum[n], f);
+          return f;
+        });
+  };
+  const int64_t nk = t.end > t.begin ? (t.end - t.begin + BK - 1) / BK : 0;
+  request(s_buf0);
+  request(s_buf1);
+  for (int64_t s = 0; s < nk; s += kRing) {
+    stage(s_buf0, s_buf2);
+    if (s + 1 < nk) stage(s_buf1, s_buf0);
+    if (s + 2 < nk) stage(s_buf2, s_buf1);
+  }
+  stage_barrier<0>();                              // (no load to LDS outlives the workgroup)
+  if (bias) {
+#pragma unroll
+    for (int n = 0; n < FN; ++n) {
+      const float v = sum[n] + __shfl_xor(sum[n], 32, 64);
+      const int col = t.n0 + wc + 32 * n + lane;
+      if (lane < 32 && col < a.C_out) a.db[t.job * a.C_out + col] = v;
+    }
+  }
+  store_sums<FC, FN>(acc, a, t.job, t.c0 + wr, t.n0 + wc, 1.0f);
+}
+
+// The matrix cores' step for 8-bit rows: both operands in f16.
+struct MmaHalf {
+  typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+  __device__ static f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+};
+// Eight e4m3 values as f16, exactly.
+__device__ __forceinline__ u32x4_t widen_half(uint32_t lo, uint32_t hi) {
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  u32x4_t v;
+  v[0] = __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
+  v[1] = __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
+  v[2] = __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
+  v[3] = __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+  return v;
+}
+
+// The same through registers: cut or unaligned pieces, and rows in 8 bits (X8), whose scale goes
+// to the other operand.  v = scale * dy enters as two f16 numbers, v 2^-e and what it leaves:
+// 22 bits.  e follows the largest finite |v| that the workgroup has met (it is told of a
+// stage's in front of the barrier that the stage waits at anyway; the sums so far are moved
+// when it grows): what is 2^17 below it loses bits, but nothing over 2^-40 of it.
+// WHOLE: rows are of whole pieces.
+template <typename T, bool X8, int BC, int BN, int WR, int WC, int KB, bool WHOLE>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
+  typedef KTile<T, BC, KB> TX;
+  typedef KTile<T, BN, KB> TY;
+  constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = 64 * WR * WC;
+  constexpr int FC = BC / WR / 32, FN = BN / WC / 32;
   constexpr int PX = TX::PIECES / NT, PY = TY::PIECES / NT, NL = X8 ? 2 : 1;
   __shared__ u32x4_t s_x[TX::PIECES], s_y[NL][TY::PIECES];
   __shared__ float s_db[NT / TY::PR][BN + 1];
+  __shared__ float s_top[2][WR * WC];
   const T* const dy = static_cast<const T*>(a.dy);
-  const int64_t nc = (a.C_in + BC - 1) / BC, nn = (a.C_out + BN - 1) / BN;
-  const int64_t id = die_order(blockIdx.x, gridDim.x), job = id / (nc * nn);
-  const int c0 = static_cast<int>(id / nn % nc) * BC, n0 = static_cast<int>(id % nn) * BN;
-  const int64_t begin = job * a.chunk, end = begin + a.chunk < a.n ? begin + a.chunk : a.n;
+  const WeightJob t = weight_job<BC, BN>(a);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int jx = threadIdx.x / TX::PR, px = threadIdx.x % TX::PR;
   const int jy = threadIdx.x / TY::PR, py = threadIdx.x % TY::PR;
-  const int cx = c0 + px * VEC, cy = n0 + py * VEC;
+  const int cx = t.c0 + px * VEC, cy = t.n0 + py * VEC;
+  uint2 rx8[PX];
   u32x4_t rx[PX], ry[PY];
   float rs[PY];
   auto request = [&](int64_t j0) {
 #pragma unroll
     for (int i = 0; i < PX; ++i) {
       const int64_t j = j0 + jx + NT / TX::PR * i;
-      const int left = j < end ? a.C_in - cx : 0;
+      const int left = j < t.end ? a.C_in - cx : 0;
       if constexpr (X8) {
-        const uint2 u = load8_left(static_cast<const uint8_t*>(a.x) + j * a.C_in + cx, left);
-        rx[i] = widen(u.x, u.y);
+        const uint8_t* p = static_cast<const uint8_t*>(a.x) + j * a.C_in + cx;
+        if constexpr (WHOLE)
+          __builtin_memcpy(&rx8[i], left > 0 ? p : reinterpret_cast<const uint8_t*>(&g_zeros), 8);
+        else
+          rx8[i] = load8_left(p, left);
       } else {
-        rx[i] = load_left<T, false>(static_cast<const T*>(a.x) + j * a.C_in + cx, left);
+        rx[i] = load_left<T, WHOLE>(static_cast<const T*>(a.x) + j * a.C_in + cx, left);
       }
     }
 #pragma unroll
     for (int i = 0; i < PY; ++i) {
       const int64_t j = j0 + jy + NT / TY::PR * i;
-      ry[i] = load_left<T, false>(dy + j * a.C_out + cy, j < end ? a.C_out - cy : 0);
-      rs[i] = X8 && j < end ? a.x_scale[j] : 0.0f;
+      ry[i] = load_left<T, WHOLE>(dy + j * a.C_out + cy, j < t.end ? a.C_out - cy : 0);
+      rs[i] = X8 && j < t.end ? a.x_scale[j] : 0.0f;
     }
   };
-  const bool bias = a.db && c0 == 0;               // (uniform)
+  const bool bias = a.db && t.c0 == 0;             // (uniform)
   float sum[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
@@ -308,78 +698,124 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_dw(LinearWeight a) {
     for (int m = 0; m < FC; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.0f;
-  const int wr = wave / WC * (BC / 2), wc = wave % WC * (BN / 2);
+  const int wr = wave / WC * (BC / WR), wc = wave % WC * (BN / WC);
   const typename TX::template Reader<32, FC> x_of(wr, lane);
   const typename TY::template Reader<32, FN> dy_of(wc, lane);
-  if (begin < end) request(begin);
-  for (int64_t j0 = begin; j0 < end; j0 += BK) {
-    __syncthreads();
+  int power = -126;                                // e: |v| 2^-e < 2^15
+  int turn = 0;
+  if (t.begin < t.end) request(t.begin);
+  for (int64_t j0 = t.begin; j0 < t.end; j0 += BK) {
+    float v[X8 ? PY : 1][VEC];
+    if constexpr (X8) {
+      float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < PX; ++i) s_x[TX::at(jx + NT / TX::PR * i, px)] = rx[i];
+      for (int i = 0; i < PY; ++i) {
+        unpack(ry[i], v[i]);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          if (bias) sum[e] += v[i][e];
+          v[i][e] *= rs[i];
+          const float m = __uint_as_float(magnitude(v[i][e]));
+          top = m < INFINITY && m > top ? m : top;
+        }
+      }
+      top = group_reduce<64>(top, [](float p, float q) { return q > p ? q : p; });
+      if (lane == 0) s_top[turn][wave] = top;
+    } else if (bias) {
+#pragma unroll
+      for (int i = 0; i < PY; ++i) {
+        float u[VEC];
+        unpack(ry[i], u);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] += u[e];
+      }
+    }
+    __syncthreads();
+    if constexpr (X8) {
+      float top = s_top[turn][0];
+#pragma unroll
+      for (int q = 1; q < WR * WC; ++q) top = s_top[turn][q] > top ? s_top[turn][q] : top;
+      turn ^= 1;
+      // top < 2^(its exponent + 1)
+      int need = static_cast<int>(__float_as_uint(top) >> 23) - 127 + 1 - 15;
+      need = __builtin_amdgcn_readfirstlane(need < -126 ? -126 : need);
+      if (need > power) {
+        const float f = ldexpf(1.0f, power - need);
+        power = need;
+#pragma unroll
+        for (int n = 0; n < FN; ++n)
+#pragma unroll
+          for (int m = 0; m < FC; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[n][m][i] *= f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PX; ++i)
+      s_x[TX::at(jx + NT / TX::PR * i, px)] = X8 ? widen_half(rx8[i].x, rx8[i].y) : rx[i];
 #pragma unroll
     for (int i = 0; i < PY; ++i) {
       const int to = TY::at(jy + NT / TY::PR * i, py);
       if constexpr (X8) {
-        float v[VEC], lo[VEC];
-        unpack(ry[i], v);
-        if (bias) {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        const float unit = __uint_as_float(static_cast<uint32_t>(127 - power) << 23);
+        u32x4_t hi, lo;
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) sum[e] += v[e];
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          v[e] *= rs[i];
-          const float up = Row<T>::get(Row<T>::put(v[e]));
+        for (int e = 0; e < VEC; e += 2) {
+          const f2 u = {v[i][e] * unit, v[i][e + 1] * unit};
+          const h2 up = __builtin_convertvector(u, h2);
+          const f2 back = __builtin_convertvector(up, f2);
           // (an infinity or NaN is all in the upper part)
-          lo[e] = magnitude(up) < 0x7f800000u ? v[e] - up : 0.0f;
+          const f2 rest = {magnitude(u[0]) < 0x7f800000u ? u[0] - back[0] : 0.0f,
+                           magnitude(u[1]) < 0x7f800000u ? u[1] - back[1] : 0.0f};
+          hi[e / 2] = __builtin_bit_cast(uint32_t, up);
+          lo[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, h2));
         }
-        s_y[0][to] = pack(v);
-        s_y[NL - 1][to] = pack(lo);
+        s_y[0][to] = hi;
+        s_y[NL - 1][to] = lo;
       } else {
-        if (bias) {
-          float v[VEC];
-          unpack(ry[i], v);
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) sum[e] += v[e];
-        }
         s_y[0][to] = ry[i];
       }
     }
     __syncthreads();
-    if (j0 + BK < end) request(j0 + BK);
+    if (j0 + BK < t.end) request(j0 + BK);
+    if constexpr (X8) {
 #pragma unroll
-    for (int l = 0; l < NL; ++l)
+      for (int q = 0; q < BK / 16; ++q) {
+        bf16x8 fx[FC], fy[NL][FN];
+#pragma unroll
+        for (int m = 0; m < FC; ++m) fx[m] = x_of(s_x, m, q);
+#pragma unroll
+        for (int l = 0; l < NL; ++l)
+#pragma unroll
+          for (int n = 0; n < FN; ++n) fy[l][n] = dy_of(s_y[l], n, q);
+#pragma unroll
+        for (int l = 0; l < NL; ++l)
+#pragma unroll
+          for (int n = 0; n < FN; ++n)
+#pragma unroll
+            for (int m = 0; m < FC; ++m) acc[n][m] = MmaHalf::mma(fy[l][n], fx[m], acc[n][m]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
       multiply_stage<T, KB, FC, FN>(
           acc, [&](int m, int q) { return x_of(s_x, m, q); },
-          [&](int n, int q) { return dy_of(s_y[l], n, q); });
+          [&](int n, int q) { return dy_of(s_y[0], n, q); });
+    }
   }
   if (bias) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) s_db[jy][py * VEC + e] = sum[e];
     __syncthreads();
-    if (threadIdx.x < BN && n0 + static_cast<int>(threadIdx.x) < a.C_out) {
+    if (threadIdx.x < BN && t.n0 + static_cast<int>(threadIdx.x) < a.C_out) {
       float s = 0.0f;
 #pragma unroll
       for (int q = 0; q < NT / TY::PR; ++q) s += s_db[q][threadIdx.x];
-      a.db[job * a.C_out + n0 + threadIdx.x] = s;
+      a.db[t.job * a.C_out + t.n0 + threadIdx.x] = s;
     }
   }
-  float* out = a.dw + job * a.C_in * a.C_out;
-#pragma unroll
-  for (int n = 0; n < FN; ++n)
-#pragma unroll
-    for (int m = 0; m < FC; ++m) {
-      const int64_t r = c0 + wr + 32 * m + (lane & 31);
-      if (r >= a.C_in) continue;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = n0 + wc + 32 * n + 8 * q + 4 * (lane >> 5);
-        float v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = acc[n][m][4 * q + i];
-        if (c < a.C_out) store_left(out + r * a.C_out + c, pack(v), a.C_out - c);
-      }
-    }
+  store_sums<FC, FN>(acc, a, t.job, t.c0 + wr, t.n0 + wc, X8 ? ldexpf(1.0f, power) : 1.0f);
 }
 
 // The chunks' sums: kThreads / RUNS lanes side by side with four values each, RUNS of them down
@@ -422,33 +858,82 @@ __global__ __launch_bounds__(kThreads) void k_linear_sum(const float* __restrict
   }
 }
 
+template <int BM, int BN> bool grid_of(const LinearArgs& a, int threads, uint32_t* blocks) {
+  const int64_t n = (a.n + BM - 1) / BM * ((a.cols + BN - 1) / BN);
+  *blocks = static_cast<uint32_t>(n);
+  return grid_fits(n, threads);
+}
 template <typename T, typename TO, bool X8, bool BT, int BM, int BN>
 int run_any(const LinearArgs& a) {
-  const int64_t blocks = (a.n + BM - 1) / BM * ((a.cols + BN - 1) / BN);
-  if (!grid_fits(blocks, kThreads)) return SPCONV_EINVAL;
-  k_linear_any<T, TO, X8, BT, BM, BN><<<static_cast<uint32_t>(blocks), kThreads, 0, a.st>>>(a);
+  uint32_t blocks;
+  if (!grid_of<BM, BN>(a, kThreads, &blocks)) return SPCONV_EINVAL;
+  k_linear_any<T, TO, X8, BT, BM, BN><<<blocks, kThreads, 0, a.st>>>(a);
   return launched();
 }
+template <typename T, typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC>
+int run_tiles(const LinearArgs& a) {
+  constexpr int NT = 64 * WR * WC;
+  uint32_t blocks;
+  if (!grid_of<BM, BN>(a, NT, &blocks)) return SPCONV_EINVAL;
+  if (linear_past(a.n, a.cols, (a.z ? 2 : 1) * static_cast<int>(sizeof(TO))))
+    k_linear<T, TO, X8, BT, BM, BN, WR, WC, true><<<blocks, NT, 0, a.st>>>(a);
+  else
+    k_linear<T, TO, X8, BT, BM, BN, WR, WC, false><<<blocks, NT, 0, a.st>>>(a);
+  return launched();
+}
+// The kernel that linear_plan says.
 template <typename T, typename TO, bool X8, bool BT> int by_size(const LinearArgs& a) {
-  const int64_t tiles = (a.n + 127) / 128 * ((a.cols + 127) / 128);
-  if (a.cols <= 64 || tiles < 1024) return run_any<T, TO, X8, BT, 64, 64>(a);
-  return run_any<T, TO, X8, BT, 128, 128>(a);
+  const bool whole = (X8 ? a.red % 16 == 0 && aligned_to(a.x, 16) : whole_rows<T>(a.x, a.red)) &&
+                     whole_rows<T>(a.w, BT ? a.red : a.cols);
+  const LinearPlan p = linear_plan(sizeof(T) == 4 ? SPCONV_F32 : SPCONV_BF16, BT, a.n, a.red,
+                                   a.cols, whole);
+  if constexpr (!BT) {
+    if (p.kernel == LinearKernel::kFew) {
+      uint32_t blocks;
+      if (!grid_of<kFewRows, 4 * Row<T>::VEC>(a, kFewThreads, &blocks)) return SPCONV_EINVAL;
+      k_linear_few<T, TO, X8><<<blocks, kFewThreads, 0, a.st>>>(a);
+      return launched();
+    }
+  }
+  if (p.kernel == LinearKernel::kAny)
+    return p.tile == 64 ? run_any<T, TO, X8, BT, 64, 64>(a) : run_any<T, TO, X8, BT, 128, 128>(a);
+  if constexpr (sizeof(T) == 2) {
+    if (p.tile == 256) return run_tiles<T, TO, X8, BT, 256, 128, 4, 2>(a);
+  }
+  if (p.tile == 128) return run_tiles<T, TO, X8, BT, 128, 128, 2, 2>(a);
+  return run_tiles<T, TO, X8, BT, 64, 64, 2, 2>(a);
 }
 
-// How the weight gradient is cut.
-DwPlan weight_plan(int x_dt, int64_t n, int C_in, int C_out) {
-  DwPlan p = dw_plan(x_dt == SPCONV_F32 ? SPCONV_F32 : SPCONV_BF16, n, 1, C_in, C_out, false);
-  if (!p.chunk) p.chunk = n < 1 ? 1 : n;
-  p.jobs = n < 1 ? 1 : (n + p.chunk - 1) / p.chunk;
-  p.bytes = p.jobs > 1
-                ? static_cast<size_t>(p.jobs) * (static_cast<size_t>(C_in) * C_out + C_out) * 4
-                : 0;
-  return p;
-}
 template <typename T, bool X8> void run_dw(const LinearWeight& a, const DwPlan& p) {
   const uint32_t blocks = static_cast<uint32_t>(p.jobs * p.tiles);
-  if (p.tile == 128) k_linear_dw<T, X8, 128, 128><<<blocks, kThreads, 0, a.st>>>(a);
-  else k_linear_dw<T, X8, 64, 64><<<blocks, kThreads, 0, a.st>>>(a);
+  const bool wx = X8 ? a.C_in % 8 == 0 : whole_rows<T>(a.x, a.C_in);
+  const bool whole = wx && whole_rows<T>(a.dy, a.C_out);
+  if constexpr (X8) {
+    if (p.tile == 256) {
+      if (whole) k_linear_dw<T, X8, 256, 128, 4, 2, 64, true><<<blocks, 512, 0, a.st>>>(a);
+      else k_linear_dw<T, X8, 256, 128, 4, 2, 64, false><<<blocks, 512, 0, a.st>>>(a);
+    } else if (p.tile == 128) {
+      if (whole) k_linear_dw<T, X8, 128, 128, 2, 2, 128, true><<<blocks, 256, 0, a.st>>>(a);
+      else k_linear_dw<T, X8, 128, 128, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
+    } else {
+      if (whole) k_linear_dw<T, X8, 64, 64, 2, 2, 128, true><<<blocks, 256, 0, a.st>>>(a);
+      else k_linear_dw<T, X8, 64, 64, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
+    }
+  } else {
+    if constexpr (sizeof(T) == 2) {
+      if (whole && p.tile == 256) {
+        k_linear_dw_ring<T, 256, 128, 4, 2><<<blocks, 512, 0, a.st>>>(a);
+        return;
+      }
+    }
+    if (p.tile == 128) {
+      if (whole) k_linear_dw_ring<T, 128, 128, 2, 2><<<blocks, 256, 0, a.st>>>(a);
+      else k_linear_dw<T, false, 128, 128, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
+    } else {
+      if (whole) k_linear_dw_ring<T, 64, 64, 2, 2><<<blocks, 256, 0, a.st>>>(a);
+      else k_linear_dw<T, false, 64, 64, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
+    }
+  }
 }
 
 bool linear_sizes_ok(int64_t n, int C_in, int C_out) {
@@ -513,7 +998,7 @@ extern "C" int spconv_linear_backward_weight_workspace(int x_dt, int64_t n, int 
                                                        size_t* bytes) {
   if ((!dtype_ok(x_dt) && x_dt != SPCONV_E4M3) || !linear_sizes_ok(n, C_in, C_out) || !bytes)
     return SPCONV_EINVAL;
-  *bytes = weight_plan(x_dt, n, C_in, C_out).bytes;
+  *bytes = linear_dw_plan(x_dt, n, C_in, C_out).bytes;
   return SPCONV_OK;
 }
 
@@ -522,7 +1007,7 @@ extern "C" int spconv_linear_backward_weight(int x_dt, const void* x, const floa
                                              int C_in, int C_out, void* workspace,
                                              size_t workspace_bytes, void* stream) {
   if (!rows_type_ok(x_dt, x_scale, n) || !linear_sizes_ok(n, C_in, C_out)) return SPCONV_EINVAL;
-  const DwPlan plan = weight_plan(x_dt, n, C_in, C_out);
+  const DwPlan plan = linear_dw_plan(x_dt, n, C_in, C_out);
   if (!ptr_ok(x, n, row_bytes(x_dt)) || !ptr_ok(dy, n, x_dt == SPCONV_F32 ? 4 : 2) ||
       !ptr_ok(dw, 1, 4) || !aligned_to(db, 4) ||
       (plan.bytes && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < plan.bytes)))

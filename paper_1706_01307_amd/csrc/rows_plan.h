@@ -1,6 +1,7 @@
 // Which kernels and tiles the grouped products and their weight gradient take
-// (rows_grouped.hip), by rules on sizes, types and alignment: plain arithmetic on the
-// host, apart from the kernels so that it can be asked without a GPU.
+// (rows_grouped.hip), and the dense ones (rows_linear.hip), by rules on sizes, types and
+// alignment: plain arithmetic on the host, apart from the kernels so that it can be asked
+// without a GPU.
 #pragma once
 
 #include <cstddef>
@@ -159,6 +160,86 @@ inline DwPlan dw_plan(int dt, int64_t m, int E, int C_in, int C_out, bool wide) 
 // The runs (1 or 8) that the chunks' sums of a group are added in (k_grouped_dw_sum).
 inline int dw_sum_runs(const DwPlan& p, int E, int64_t values) {
   return (values + 1023) / 1024 * E < 1024 && p.jobs > 4ll * E ? 8 : 1;
+}
+
+// ---------------------------------------------------------------------------
+// Dense products (rows_linear.hip)
+// ---------------------------------------------------------------------------
+enum class LinearKernel { kFew, kAny, kTiles };
+struct LinearPlan {
+  LinearKernel kernel;
+  int tile;                    // kAny: 64, 128 squared; kTiles: too, 256: 256 rows x 128 columns
+};
+
+// k_linear_few as for grouped products; k_linear_any where pieces may be cut or unaligned;
+// else k_linear in tiles of 256 x 128 (not fp32), 128 x 128 or 64 x 64, the largest that
+// two (fp32: three) workgroups a compute unit fill.  (us in tiles of 64, 128 and 256, bf16:
+// 348,208 x 256 -> 1024 642, 329 and 317; 65,536 x 512 -> 512 73, 54 and 49; 16,384 x 2048
+// -> 2048 255, 159 and 145, of 256 x 256 146; 8,000 x 512 -> 512 12, 12 and 15.  fp32, 65,536
+// x 1024 -> 1024: 1,259 and 1,072.)
+inline LinearPlan linear_plan(int in_dt, bool backward, int64_t n, int red, int cols, bool whole) {
+  const bool f32 = in_dt == SPCONV_F32;
+  if (!backward && few_is_faster(f32, n, 1, red, cols)) return {LinearKernel::kFew, 0};
+  const int64_t c128 = (cols + 127) / 128, c64 = (cols + 63) / 64;
+  const int64_t t128 = (n + 127) / 128 * c128, t256 = (n + 255) / 256 * c128;
+  const bool waste = f32 && c64 % 2 && c64 > 2 && c64 < 16;   // of the last 128 columns
+  const bool small = cols <= 64 || t128 < (f32 ? 768 : 512) || waste;
+  if (!whole) return {LinearKernel::kAny, small ? 64 : 128};
+  if (small) return {LinearKernel::kTiles, 64};
+  return {LinearKernel::kTiles, !f32 && t256 >= 512 ? 256 : 128};
+}
+// Whether finished rows are stored past the caches: 32 MB of them are in no L2 anyway when
+// somebody reads them, and push out the operands meanwhile (348,208 x 256 -> 1024 with the
+// activation's input: 543 us, and 416 past them).
+inline bool linear_past(int64_t n, int cols, int bytes) {
+  return static_cast<double>(n) * cols * bytes > 32e6;
+}
+
+// The weight gradient's tiles (64 or 128 squared, or 256: of 256 x 128) and chunks of rows, by
+// an estimate in us: a stage of 32 rows (fp32: 16) of a tile takes `alone` with one
+// workgroup a compute unit and `full` with all of `slots` on the card, a workgroup 3 besides
+// its stages, the chunks' sums are written and read at 4 MB a us and take a launch.
+// (us by jobs, bf16 348,208 x 1024 x 256 in tiles of 256: 32 360, 64 271, 128 292; 16,384 x
+// 2048 x 2048: 2 232, 4 162, 8 198, of 128 3 178; 902,504 x 64 x 64 of 64: 256 60, 512 45,
+// 1,024 55; 8,000 x 512 x 512 of 64: 4 26, 8 20, 32 25.  Rows in 8 bits, 16,384 x 2048 x
+// 2048 of 256: 2 411, 4 408; fp32 65,536 x 1024 x 1024 of 128: 4 1,203, 12 1,066.)
+inline DwPlan linear_dw_plan(int x_dt, int64_t n, int C_in, int C_out) {
+  struct Rate { int tile; double alone, full, slots; };
+  static const Rate bf16[3] = {{64, 0.5, 0.62, 1024}, {128, 0.77, 0.9, 768}, {256, 0.82, 1.05, 512}};
+  static const Rate f32[2] = {{64, 0.52, 1.15, 1024}, {128, 1.17, 3.05, 768}};
+  static const Rate e4m3[3] = {{64, 0.6, 1.22, 1024}, {128, 1.17, 1.6, 512}, {256, 1.54, 2.9, 512}};
+  const Rate* rate = x_dt == SPCONV_F32 ? f32 : x_dt == SPCONV_BF16 ? bf16 : e4m3;
+  const int kinds = x_dt == SPCONV_F32 ? 2 : 3, rows = x_dt == SPCONV_F32 ? 16 : 32;
+  const double values = static_cast<double>(C_in) * C_out + C_out;
+  if (n < 1) n = 1;
+  DwPlan best{0, 0, 0, 0, 0};
+  double least = 0.0;
+  for (int i = 0; i < kinds; ++i) {
+    const Rate& r = rate[i];
+    const int BN = r.tile == 256 ? 128 : r.tile;
+    if (i && (C_out <= BN / 2 || C_in <= r.tile / 2)) break;
+    const int64_t tiles = ((C_in + r.tile - 1ll) / r.tile) * ((C_out + BN - 1ll) / BN);
+    auto consider = [&](int64_t jobs) {
+      if (jobs < 1) return;
+      const int64_t chunk = ((n + jobs - 1) / jobs + 63) / 64 * 64;
+      jobs = (n + chunk - 1) / chunk;
+      const double total = static_cast<double>(jobs) * tiles, load = total / 256.0;
+      const double deep = r.slots / 256.0, more = load < 1 ? 0 : load > deep ? 1 : (load - 1) / (deep - 1);
+      const double unit = (chunk < n ? chunk : n) / static_cast<double>(rows) *
+                              (r.alone + (r.full - r.alone) * more) + 3.0;
+      const double rounds = total / r.slots;
+      const double whole = rounds <= 1 ? 1 : rounds > 3 ? rounds + 0.5 : static_cast<int64_t>(rounds - 1e-9) + 1;
+      const double us = unit * whole + (jobs > 1 ? 4.0 + jobs * values * 8.0 / 4e6 : 0.0);
+      if (best.tiles && !(us < least)) return;
+      least = us;
+      best = DwPlan{r.tile, chunk, jobs, tiles, 0};
+    };
+    for (int64_t jobs = 1; jobs <= 4096 && jobs <= n; jobs *= 2) consider(jobs);
+    for (int k = 1; k <= 3; ++k) consider(k * static_cast<int64_t>(r.slots) / tiles);
+  }
+  if (best.jobs > 1)
+    best.bytes = static_cast<size_t>(best.jobs) * (static_cast<size_t>(C_in) * C_out + C_out) * 4;
+  return best;
 }
 
 }  // namespace spc
