@@ -102,186 +102,203 @@ struct ScoreArgs {
   hipStream_t st;
 };
 
-// The scores of a lane's NV * VEC columns of a row, x: sigmoid, or softmax with the row's
-// maximum `top` (0 if all are closed).  fp32 ones are within 4 units of the sigmoid's or 32
-// of the softmax's last place (expf, the sum of 16 terms and 6 steps, a division).
-template <typename F, int LPR, int NV, int VEC>
-__device__ __forceinline__ void scores_of(const float (&x)[NV][VEC], bool softmax, float top,
-                                          F (&s)[NV][VEC]) {
-  F sum = 0;
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const F a = softmax ? static_cast<F>(x[j][i]) - static_cast<F>(top) : -static_cast<F>(x[j][i]);
-      F e;
-      if constexpr (sizeof(F) == 4) e = expf(a); else e = exp(a);
-      s[j][i] = softmax ? e : F(1) / (F(1) + e);
-      sum += e;
-    }
-  if (softmax) {
-    sum = over_row<LPR>(sum, [](F a, F b) { return a + b; });
-    const F inv = sum == 0 ? F(0) : F(1) / sum;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) s[j][i] = sizeof(F) == 4 ? s[j][i] * inv : s[j][i] / (sum == 0 ? F(1) : sum);
-  }
-}
-
-// The choice of one row from its biased scores v (-infinity: closed), of which `keep` is what
-// is kept of a chosen one.  near: twice the error of an fp32 score; the function returns
-// whether a gap that decides is within it (F double: never).  s_v, s_worth: the row's own LDS.
-template <typename T, typename F, int LPR, int NV, int VEC>
-__device__ __forceinline__ bool choose(const ScoreArgs& a, const T* logits, F (&v)[NV][VEC],
-                                       const float (&keep)[NV][VEC], F near, F* s_v, F* s_worth,
-                                       int16_t* s_expert, float* s_weight) {
+// What a wave or a part of it shares of a row in LDS: the groups' choice.  v: a lane's biased
+// scores, N of them, of columns col(i) (those of E and beyond, and closed ones, -infinity); on
+// return those of groups that go are -infinity too.  s_v: E words; a group's worth takes the
+// place of its first score.  The gap between the last group that stays and the best that goes is
+// returned as whether it is within `near` and the roundings of a sum.
+template <typename F, int LPR, int N, typename Col>
+__device__ __forceinline__ bool keep_groups(F (&v)[N], Col col, int lane, const ScoreArgs& a,
+                                            F near, F unit, F* s_v) {
   typedef Order<F> O;
   typedef typename O::U U;
-  constexpr bool kFast = sizeof(F) == 4;
-  constexpr F kUnit = F(0x1p-22);                  // 4 units: of the biased score, twice
-  const int lane = threadIdx.x % LPR, E = a.E;
-  bool close = false;
-  if (a.groups > 1) {
-    const int per = E / a.groups;
+  const int per = a.E / a.groups;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const int c = (lane + LPR * j) * VEC + i;
-        if (c < E) s_v[c] = v[j][i];
-      }
-    row_fence();
-    // a group is worth its two best
-    for (int g = lane; g < a.groups; g += LPR) {
-      U o1 = 0, o2 = 0;
-      for (int i = 0; i < per; ++i) {
-        const U o = O::of(s_v[g * per + i]);
-        if (o > o1) o2 = o1, o1 = o; else if (o > o2) o2 = o;
-      }
-      F worth = O::value(o1 > O::kClosed ? o1 : O::kClosed);
-      if (o2 > O::kClosed) worth += O::value(o2);
-      s_worth[g] = worth;
+  for (int i = 0; i < N; ++i)
+    if (col(i) < a.E) s_v[col(i)] = v[i];
+  row_fence();
+  for (int g = lane; g < a.groups; g += LPR) {
+    U o1 = 0, o2 = 0;
+    for (int i = 0; i < per; ++i) {
+      const U o = O::of(s_v[g * per + i]);
+      if (o > o1) o2 = o1, o1 = o; else if (o > o2) o2 = o;
     }
-    row_fence();
-    uint32_t stay[2] = {0u, 0u};
-    F low = INFINITY, high = -INFINITY;            // the last that stays, the best that goes
-    bool odd = false;                              // (NaN among them)
-    for (int g = lane; g < a.groups; g += LPR) {
-      const F worth = s_worth[g];
-      const U o = O::of(worth);
-      int rank = 0;
-      for (int q = 0; q < a.groups; ++q) {
-        const U oq = O::of(s_worth[q]);
-        rank += oq > o || (oq == o && q < g);
-      }
-      const bool in = rank < a.top_groups && o > O::kClosed;
-      if (in) stay[g >> 5] |= 1u << (g & 31);
-      odd |= worth != worth;
-      if (in) low = worth < low ? worth : low;
-      else high = worth > high ? worth : high;
-    }
-    const auto either = [](uint32_t p, uint32_t q) { return p | q; };
-    stay[0] = over_row<LPR>(stay[0], either);
-    stay[1] = over_row<LPR>(stay[1], either);
-    if constexpr (kFast) {
-      low = over_row<LPR>(low, [](F p, F q) { return q < p ? q : p; });
-      high = over_row<LPR>(high, [](F p, F q) { return q > p ? q : p; });
-      close |= over_row<LPR>(odd ? 1u : 0u, either) != 0;
-      if (a.top_groups < a.groups && high > -INFINITY && low < INFINITY)
-        close |= !(low - high > 2 * near + 2 * kUnit * (fabsf(low) + fabsf(high)));
-    }
-    const float inv = 1.0f / per;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        // (exact: columns are below 2^10, and half a step from the border)
-        const int g = static_cast<int>(((lane + LPR * j) * VEC + i + 0.5f) * inv);
-        if (!((stay[(g >> 5) & 1] >> (g & 31)) & 1u)) v[j][i] = -INFINITY;
-      }
+    F worth = O::value(o1 > O::kClosed ? o1 : O::kClosed);
+    if (o2 > O::kClosed) worth += O::value(o2);
+    s_v[g * per] = worth;
   }
-  U o[NV][VEC];
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) o[j][i] = (lane + LPR * j) * VEC + i < E ? O::of(v[j][i]) : 0u;
-  U before = 0;
-  uint32_t before_c = 0;
-  // (fp32: one more than is chosen, and on while it ties with the last)
-  for (int s = 0; s < E; ++s) {
-    if (s >= a.k && (!kFast || s > a.k)) break;
-    U bo = 0;
-    uint32_t bc = 0xffffffffu;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i)
-        if (o[j][i] > bo) {                        // ascending columns: the lowest of equals
-          bo = o[j][i];
-          bc = (lane + LPR * j) * VEC + i;
-        }
-    best_of_row<LPR>(bo, bc);
-    const bool some = bo > O::kClosed;
-    if constexpr (kFast) {
-      if (s > 0 && some) {
-        const F p = O::value(before), q = O::value(bo);
-        if (!(p - q > near + kUnit * (fabsf(p) + fabsf(q)))) {
-          // equal logits with equal biases have equal scores in any arithmetic
-          bool same = Row<T>::get(logits[before_c]) == Row<T>::get(logits[bc]) &&
-                      (!a.bias || a.bias[before_c] == a.bias[bc]);
-          // (past the last choice a tie hides what comes behind it)
-          close |= !same || s >= a.k;
-        }
-      }
-      before = bo;
-      before_c = bc;
-      if (s >= a.k) break;
+  row_fence();
+  uint32_t stay[2] = {0u, 0u};
+  F low = INFINITY, high = -INFINITY;              // the last that stays, the best that goes
+  bool odd = false;                                // (NaN among them)
+  for (int g = lane; g < a.groups; g += LPR) {
+    const F worth = s_v[g * per];
+    const U o = O::of(worth);
+    int rank = 0;
+    for (int q = 0; q < a.groups; ++q) {
+      const U oq = O::of(s_v[q * per]);
+      rank += oq > o || (oq == o && q < g);
     }
-    float mine = 0.0f;
-    bool owner = false;
+    const bool in = rank < a.top_groups && o > O::kClosed;
+    if (in) stay[g >> 5] |= 1u << (g & 31);
+    odd |= worth != worth;
+    if (in) low = worth < low ? worth : low;
+    else high = worth > high ? worth : high;
+  }
+  const auto either = [](uint32_t p, uint32_t q) { return p | q; };
+  stay[0] = over_row<LPR>(stay[0], either);
+  if (a.groups > 32) stay[1] = over_row<LPR>(stay[1], either);
+  bool close = false;
+  if (unit > 0) {
+    low = over_row<LPR>(low, [](F p, F q) { return q < p ? q : p; });
+    high = over_row<LPR>(high, [](F p, F q) { return q > p ? q : p; });
+    close = over_row<LPR>(odd ? 1u : 0u, either) != 0;
+    if (a.top_groups < a.groups && high > -INFINITY && low < INFINITY)
+      close |= !(low - high > 2 * near + 2 * unit * (fabsf(low) + fabsf(high)));
+  }
+  const float inv = 1.0f / per;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i)
-        if (static_cast<uint32_t>((lane + LPR * j) * VEC + i) == bc) {
-          o[j][i] = 0u;                            // take it out
-          mine = keep[j][i];
-          owner = true;
-        }
-    if (some ? owner : lane == 0) {
-      s_expert[s] = static_cast<int16_t>(some ? static_cast<int32_t>(bc) : -1);
-      s_weight[s] = mine;
-    }
-    if (!some && s + 1 < a.k) {
-      // none is left: nor for the slots behind
-      for (int t = s + 1 + lane; t < a.k; t += LPR) s_expert[t] = -1, s_weight[t] = 0.0f;
-      break;
-    }
+  for (int i = 0; i < N; ++i) {
+    // (exact: columns are below 2^10, and half a step from the border)
+    const int g = static_cast<int>((col(i) + 0.5f) * inv);
+    if (!((stay[(g >> 5) & 1] >> (g & 31)) & 1u)) v[i] = -INFINITY;
   }
   return close;
 }
 
+// The k largest of a row's fp32 scores, and whether a gap that decides is within `near` and the
+// bias' rounding.  The largest value of the row is found first and its lowest column then: fewer
+// operations than with both at once, and the score itself need not be carried (rows_weights
+// takes the chosen logits again).
+template <typename T, int LPR, int N, typename Col>
+__device__ __forceinline__ bool choose_fast(const ScoreArgs& a, const T* logits,
+                                            const float (&v)[N], Col col, int lane, float near,
+                                            float unit, int16_t* s_expert) {
+  uint32_t o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = col(i) < a.E ? order_of(v[i]) : 0u;
+  bool close = false;
+  uint32_t before = 0, before_c = 0;
+  // (one more than is chosen)
+  const int last = a.k < a.E ? a.k : a.k - 1;
+  for (int s = 0; s <= last; ++s) {
+    uint32_t best = 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) best = o[i] > best ? o[i] : best;
+    best = over_row<LPR>(best, [](uint32_t p, uint32_t q) { return q > p ? q : p; });
+    if (best <= kNone) {
+      // none is left: nor for the slots behind
+      for (int t = s + lane; t < a.k; t += LPR) s_expert[t] = -1;
+      break;
+    }
+    int mine = N;
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) mine = o[i] == best ? i : mine;
+    uint32_t c = 0xffffffffu;
+    if (mine < N) c = col(mine);
+    const uint32_t own = c;
+    c = over_row<LPR>(c, [](uint32_t p, uint32_t q) { return q < p ? q : p; });
+    if (s > 0) {
+      const float p = value_of(before), q = value_of(best);
+      if (!(p - q > near + unit * (fabsf(p) + fabsf(q)))) {
+        // equal logits with equal biases have equal scores in any arithmetic (but past
+        // the last choice a tie hides what comes behind it)
+        close |= s >= a.k || Row<T>::get(logits[before_c]) != Row<T>::get(logits[c]) ||
+                 (a.bias && a.bias[before_c] != a.bias[c]);
+      }
+    }
+    before = best;
+    before_c = c;
+    if (s >= a.k) break;
+    mine = own == c ? mine : N;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = i == mine ? 0u : o[i];
+    if (lane == 0) s_expert[s] = static_cast<int16_t>(c);
+  }
+  return close;
+}
+
+// A row again, by a whole wave in 64 bits.
+template <typename T>
+__device__ void choose_slow(const ScoreArgs& a, const T* logits, double* s_v, int16_t* s_expert) {
+  constexpr int N = kMaxE / 64;
+  typedef Order<double> O;
+  const int lane = threadIdx.x & 63;
+  const auto col = [&](int i) { return lane + 64 * i; };
+  double v[N];
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float x = col(i) < a.E ? Row<T>::get(logits[col(i)]) : -INFINITY;
+    v[i] = x;
+    top = x > top || x != x ? x : top;
+  }
+  if (a.softmax) {
+    top = over_row<64>(top, [](float p, float q) { return q > p || q != q ? q : p; });
+    if (top == -INFINITY) top = 0.0f;
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (64 * i >= a.E) break;
+    const double x = v[i];
+    const double e = exp(a.softmax ? x - static_cast<double>(top) : -x);
+    sum += e;
+    v[i] = x == -INFINITY ? -INFINITY : a.softmax ? e : 1.0 / (1.0 + e);
+  }
+  if (a.softmax) {
+    sum = over_row<64>(sum, [](double p, double q) { return p + q; });
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = v[i] == -INFINITY ? v[i] : v[i] / (sum == 0.0 ? 1.0 : sum);
+  }
+  if (a.bias) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (col(i) < a.E && v[i] != -INFINITY) v[i] += a.bias[col(i)];
+  }
+  if (a.groups > 1) keep_groups<double, 64>(v, col, lane, a, 0.0, 0.0, s_v);
+  uint64_t o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = col(i) < a.E ? O::of(v[i]) : 0u;
+  for (int s = 0; s < a.k; ++s) {
+    uint64_t best = 0;
+    uint32_t c = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (o[i] > best) best = o[i], c = col(i);
+    best_of_row<64>(best, c);
+    const bool some = best > O::kClosed;
+    if (lane == 0) s_expert[s] = static_cast<int16_t>(some ? static_cast<int32_t>(c) : -1);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (static_cast<uint32_t>(col(i)) == c) o[i] = 0;
+  }
+}
+
 // LPR lanes hold a row of at most LPR * NV * VEC logits, 16 a lane.
 template <typename T, int LPR, int NV, bool TAIL>
-__global__ __launch_bounds__(kThreads) void k_scores(ScoreArgs a) {
-  constexpr int VEC = Row<T>::VEC, G = kThreads / LPR;
-  static_assert(NV * VEC <= 16, "the row's LDS is sized for it");
-  __shared__ int16_t s_expert[kPairs];
+__global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
+  constexpr int VEC = Row<T>::VEC, G = kThreads / LPR, N = NV * VEC;
+  static_assert(N <= 16, "the row's LDS is sized for it");
+  // Rows' scores while their groups are chosen (a word apart from the next row's, for other
+  // banks), then a wave's in 64 bits, then the waves' counts.
+  constexpr int kWords = kThreads * 16 + G;
+  __shared__ __attribute__((aligned(8))) float s_room[kWords];
+  static_assert(kWords >= kWaves * kMaxE, "the counts fit");
+  __shared__ int16_t s_expert[kPairs], s_slow[kThreads];
   __shared__ float s_weight[kPairs];
-  // a row's scores (a word apart from the next row's, for other banks), its groups' worth;
-  // then the waves' counts
-  constexpr int kWords = kThreads * 16 + G, kWorth = G * (LPR < 16 ? LPR * 16 < kMaxG ? LPR * 16 : kMaxG : kMaxG);
-  __shared__ double s_room[kWords];
-  __shared__ double s_worth[kWorth];
-  __shared__ int32_t s_start[kMaxE], s_wave[kWaves];
-  static_assert(sizeof(s_room) >= sizeof(int32_t) * kWaves * kMaxE, "the counts fit");
+  __shared__ int32_t s_start[kMaxE], s_wave[kWaves], s_nslow;
+  // (the whole row's softmax, where the weights ask for it: in s_start, free until then)
+  float* const s_top = reinterpret_cast<float*>(s_start);
+  float* const s_sum = s_top + kThreads;
   const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR, E = a.E;
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * a.rows_blk;
   const int nrow = static_cast<int>(a.n - row0 < a.rows_blk ? a.n - row0 : a.rows_blk);
-  const T* const logits = static_cast<const T*>(a.logits);
-  constexpr int kRowWorth = kWorth / G;
-  float bias[NV][VEC], x[NV][VEC], next[NV][VEC];
+  const T* const logits = static_cast<const T*>(a.logits) + row0 * E;
+  const auto col = [&](int i) { return (lane + LPR * (i / VEC)) * VEC + i % VEC; };
+  if (threadIdx.x == 0) s_nslow = 0;
+  __syncthreads();
+  float bias[NV][VEC], next[NV][VEC];
   auto request = [&](int q) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -289,7 +306,7 @@ __global__ __launch_bounds__(kThreads) void k_scores(ScoreArgs a) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) next[j][i] = -INFINITY;
       if (q < nrow && c < E) {
-        load_row<T, TAIL>(logits + (row0 + q) * E, c, E, next[j]);
+        load_row<T, TAIL>(logits + static_cast<int64_t>(q) * E, c, E, next[j]);
         if constexpr (TAIL) {
 #pragma unroll
           for (int i = 0; i < VEC; ++i)
@@ -307,81 +324,79 @@ __global__ __launch_bounds__(kThreads) void k_scores(ScoreArgs a) {
   }
   request(group);
   for (int q = group; q < nrow; q += G) {          // (a group's lanes stay together)
+    float x[N], v[N];
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) x[j][i] = next[j][i];
+    for (int i = 0; i < N; ++i) x[i] = next[i / VEC][i % VEC];
     request(q + G);
-    float top = -INFINITY;
+    // fp32 scores: within 4 units of the sigmoid, or 32 of the softmax's largest (exp, the
+    // sum of 16 terms and 6 steps, a division); twice as much for both sides of a gap
+    float near = 0x1p-21f;
     if (a.softmax) {
+      float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) top = x[j][i] > top || x[j][i] != x[j][i] ? x[j][i] : top;
+      for (int i = 0; i < N; ++i) top = x[i] > top || x[i] != x[i] ? x[i] : top;
       top = over_row<LPR>(top, [](float p, float r) { return r > p || r != r ? r : p; });
       if (top == -INFINITY) top = 0.0f;
-    }
-    // what is kept of a chosen score: the score, or, for weights by a softmax over the
-    // chosen, the logit
-    float s[NV][VEC], v[NV][VEC];
-    scores_of<float, LPR>(x, a.softmax, top, s);
-    float most = 1.0f;
-    if (a.softmax) {
-      most = 0.0f;
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
+      for (int i = 0; i < N; ++i) sum += v[i] = expf(x[i] - top);
+      sum = over_row<LPR>(sum, [](float p, float r) { return p + r; });
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) most = s[j][i] > most ? s[j][i] : most;
-      most = 8.0f * over_row<LPR>(most, [](float p, float r) { return r > p ? r : p; });
+      for (int i = 0; i < N; ++i) v[i] *= inv;
+      near = 0x1p-18f * inv;                       // (the largest is exp(0) / sum)
+      if (lane == 0) s_top[q] = top, s_sum[q] = inv;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_rcpf(1.0f + expf(-x[i]));
     }
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        v[j][i] = x[j][i] == -INFINITY ? -INFINITY : s[j][i] + bias[j][i];
-        if (a.softmax && a.normalize) s[j][i] = x[j][i];
-      }
-    int16_t* const ex = s_expert + q * a.k;
+    for (int i = 0; i < N; ++i)
+      v[i] = x[i] == -INFINITY ? -INFINITY : v[i] + bias[i / VEC][i % VEC];
+    constexpr float kUnit = 0x1p-22f;              // 4 units: of the biased score, twice
+    bool close = false;
+    if (a.groups > 1)
+      close = keep_groups<float, LPR>(v, col, lane, a, near, kUnit,
+                                      s_room + group * (LPR * N + 1));
+    close |= choose_fast<T, LPR>(a, logits + static_cast<int64_t>(q) * E, v, col, lane, near, kUnit,
+                                 s_expert + q * a.k);
+    if (close && lane == 0) s_slow[atomicAdd(&s_nslow, 1)] = static_cast<int16_t>(q);
+  }
+  __syncthreads();
+  const int nslow = s_nslow, wave = threadIdx.x >> 6;
+  // as many waves as the room has rows of E doubles for
+  const int most = kWords / (2 * E), takes = most < kWaves ? most : kWaves;
+  if (wave < takes)
+    for (int i = wave; i < nslow; i += takes) {
+      const int q = s_slow[i];
+      choose_slow(a, logits + static_cast<int64_t>(q) * E,
+                  reinterpret_cast<double*>(s_room) + wave * E, s_expert + q * a.k);
+    }
+  __syncthreads();
+  // The weights, a row a lane, from the chosen logits.
+  for (int q = threadIdx.x; q < nrow; q += kThreads) {
+    const int16_t* const ex = s_expert + q * a.k;
     float* const wt = s_weight + q * a.k;
-    const int at = group * (LPR * NV * VEC + 1);
-    const T* const row = logits + (row0 + q) * E;
-    // 8 units of the largest score (softmax: 64)
-    const bool close = choose<T, float, LPR, NV, VEC>(
-        a, row, v, s, 0x1p-21f * most, reinterpret_cast<float*>(s_room + at),
-        reinterpret_cast<float*>(s_worth + group * kRowWorth), ex, wt);
-    if (close) {                                   // (the same for all of the row's lanes)
-      double d[NV][VEC];
-      scores_of<double, LPR>(x, a.softmax, top, d);
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          d[j][i] = x[j][i] == -INFINITY ? -INFINITY : d[j][i] + bias[j][i];
-      row_fence();
-      choose<T, double, LPR, NV, VEC>(a, row, d, s, 0.0, s_room + at, s_worth + group * kRowWorth,
-                                      ex, wt);
+    const T* const row = logits + static_cast<int64_t>(q) * E;
+    float top = a.softmax ? s_top[q] : 0.0f, sum = 0.0f;
+#pragma unroll 8
+    for (int t = 0; t < a.k; ++t) wt[t] = ex[t] < 0 ? -INFINITY : Row<T>::get(row[ex[t]]);
+    if (a.softmax && a.normalize) {
+      top = -INFINITY;
+      for (int t = 0; t < a.k; ++t) top = wt[t] > top || wt[t] != wt[t] ? wt[t] : top;
     }
-    row_fence();
-    // The weights, every lane those of its slots.
-    float peak = -INFINITY, sum = 0.0f;
-    if (a.normalize) {
-      if (a.softmax) {
-        for (int t = 0; t < a.k; ++t)
-          if (ex[t] >= 0) peak = wt[t] > peak || wt[t] != wt[t] ? wt[t] : peak;
-      }
-      for (int t = 0; t < a.k; ++t)
-        if (ex[t] >= 0) sum += a.softmax ? expf(wt[t] - peak) : wt[t];
+    for (int t = 0; t < a.k; ++t) {
+      const float x = wt[t];
+      float w = 0.0f;
+      if (ex[t] >= 0) w = a.softmax ? expf(x - top) : 1.0f / (1.0f + expf(-x));
+      wt[t] = w;
+      sum += w;
     }
-    row_fence();
-    for (int t = lane; t < a.k; t += LPR) {
-      float w = ex[t] < 0 ? 0.0f : wt[t];
-      if (a.normalize) {
-        if (a.softmax && ex[t] >= 0) w = expf(w - peak);
-        w = sum == 0.0f ? 0.0f : w / sum;
-      }
+    const float f = a.normalize ? 1.0f : a.softmax ? s_sum[q] : 1.0f;
+    for (int t = 0; t < a.k; ++t) {
+      float w = wt[t] * f;
+      if (a.normalize) w = sum == 0.0f ? 0.0f : w / sum;
       wt[t] = w * a.scale;
     }
-    row_fence();
   }
   __syncthreads();
   auto& s_count = *reinterpret_cast<int32_t(*)[kWaves][kMaxE]>(s_room);
