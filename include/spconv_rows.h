@@ -339,8 +339,8 @@ int spconv_route_scores_forward(int dt, const void* logits, const float* bias, i
                                 size_t workspace_bytes, void* stream);
 
 /* Gradient of those weights with respect to the logits (the choice itself has
- * none), dlogits [n][E] of dtype dt.  dweights of slots without an expert are not
- * read into anything.  logits may be NULL for softmax scores with normalize = 1. */
+ * none), dlogits [n][E] of dtype dt.  experts are a forward's: an expert at most
+ * once a row.  dweights of slots without an expert are not read into anything.  logits may be NULL for softmax scores with normalize = 1. */
 int spconv_route_scores_backward(int dt, const float* dweights, const void* logits,
                                  const int32_t* experts, const float* weights, int64_t n, int E,
                                  int k, int score, int normalize, float scale, void* dlogits,

@@ -16,27 +16,17 @@ namespace {
 
 constexpr int kMaxG = SPCONV_ROUTE_MAX_GROUPS;
 
-// The order of scores as unsigned numbers, as order_of: NaN largest, -0 equal to +0.
-template <typename F> struct Order;
-template <> struct Order<float> {
-  typedef uint32_t U;
-  static constexpr U kClosed = kNone;              // -infinity
-  __device__ static U of(float v) { return order_of(v); }
-  __device__ static float value(U o) { return value_of(o); }
-};
-template <> struct Order<double> {
-  typedef uint64_t U;
-  static constexpr U kClosed = 0x000fffffffffffffull;
-  __device__ static U of(double v) {
-    if (v != v) return ~0ull;
-    const U u = __builtin_bit_cast(U, v + 0.0);
-    return u >> 63 ? ~u : u | 1ull << 63;
-  }
-  __device__ static double value(U o) {
-    return __builtin_bit_cast(double, o == ~0ull ? 0x7ff8000000000000ull
-                                                 : o >> 63 ? o & ~(1ull << 63) : ~o);
-  }
-};
+// The order of 64-bit scores as unsigned numbers, as order_of: NaN largest, -0 equal to +0.
+constexpr uint64_t kNone64 = 0x000fffffffffffffull;        // the order of -infinity
+__device__ __forceinline__ uint64_t order_of(double v) {
+  if (v != v) return ~0ull;
+  const uint64_t u = __builtin_bit_cast(uint64_t, v + 0.0);
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double value_of(uint64_t o) {
+  return __builtin_bit_cast(double, o == ~0ull ? 0x7ff8000000000000ull
+                                               : o >> 63 ? o & ~(1ull << 63) : ~o);
+}
 
 // The value of the lane at the other end of a butterfly step among LPR lanes.
 template <int STEP> __device__ __forceinline__ uint32_t other32(uint32_t v) {
@@ -58,13 +48,30 @@ template <int STEP, typename V> __device__ __forceinline__ V other(V v) {
     return __builtin_bit_cast(V, hi << 32 | lo);
   }
 }
+// (op is commutative: it does not matter which of the two a lane's own is)
+template <int STEP, typename V, typename Op> __device__ __forceinline__ V swap_step(V v, Op op) {
+  if constexpr (sizeof(V) == 4) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    if constexpr (STEP == 16) {
+      const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+      return op(__builtin_bit_cast(V, static_cast<uint32_t>(r[0])),
+                __builtin_bit_cast(V, static_cast<uint32_t>(r[1])));
+    } else {
+      const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+      return op(__builtin_bit_cast(V, static_cast<uint32_t>(r[0])),
+                __builtin_bit_cast(V, static_cast<uint32_t>(r[1])));
+    }
+  } else {
+    return op(v, other<STEP>(v));
+  }
+}
 template <int LPR, typename V, typename Op> __device__ __forceinline__ V over_row(V v, Op op) {
   if constexpr (LPR > 1) v = op(v, other<1>(v));
   if constexpr (LPR > 2) v = op(v, other<2>(v));
   if constexpr (LPR > 4) v = op(v, other<4>(v));
   if constexpr (LPR > 8) v = op(v, other<8>(v));
-  if constexpr (LPR > 16) v = op(v, other<16>(v));
-  if constexpr (LPR > 32) v = op(v, other<32>(v));
+  if constexpr (LPR > 16) v = swap_step<16>(v, op);
+  if constexpr (LPR > 32) v = swap_step<32>(v, op);
   return v;
 }
 // The largest (order, lowest column) of the row's lanes.
@@ -102,86 +109,136 @@ struct ScoreArgs {
   hipStream_t st;
 };
 
-// What a wave or a part of it shares of a row in LDS: the groups' choice.  v: a lane's biased
-// scores, N of them, of columns col(i) (those of E and beyond, and closed ones, -infinity); on
-// return those of groups that go are -infinity too.  s_v: E words; a group's worth takes the
-// place of its first score.  The gap between the last group that stays and the best that goes is
-// returned as whether it is within `near` and the roundings of a sum.
-template <typename F, int LPR, int N, typename Col>
-__device__ __forceinline__ bool keep_groups(F (&v)[N], Col col, int lane, const ScoreArgs& a,
-                                            F near, F unit, F* s_v) {
-  typedef Order<F> O;
-  typedef typename O::U U;
-  const int per = a.E / a.groups;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (col(i) < a.E) s_v[col(i)] = v[i];
-  row_fence();
-  for (int g = lane; g < a.groups; g += LPR) {
-    U o1 = 0, o2 = 0;
-    for (int i = 0; i < per; ++i) {
-      const U o = O::of(s_v[g * per + i]);
-      if (o > o1) o2 = o1, o1 = o; else if (o > o2) o2 = o;
-    }
-    F worth = O::value(o1 > O::kClosed ? o1 : O::kClosed);
-    if (o2 > O::kClosed) worth += O::value(o2);
-    s_v[g * per] = worth;
-  }
-  row_fence();
-  uint32_t stay[2] = {0u, 0u};
-  F low = INFINITY, high = -INFINITY;              // the last that stays, the best that goes
+constexpr float kUnit = 0x1p-22f;                  // 4 units: of a biased score, twice
+
+// The two largest of two pairs (first >= second).
+__device__ __forceinline__ void merge_two(uint32_t& a1, uint32_t& a2, uint32_t b1, uint32_t b2) {
+  const uint32_t low = a1 < b1 ? a1 : b1, rest = a2 > b2 ? a2 : b2;
+  a1 = a1 > b1 ? a1 : b1;
+  a2 = low > rest ? low : rest;
+}
+__device__ __forceinline__ float worth_of(uint32_t o1, uint32_t o2) {
+  const float w = value_of(o1 > kNone ? o1 : kNone);
+  return o2 > kNone ? w + value_of(o2) : w;
+}
+
+// The groups of a row that stay, by fp32 scores: o, the orders of a lane's NV * VEC biased scores,
+// become 0 where their group goes.  Returns whether the gap between the last group that stays and
+// the best that goes is within `near` and the roundings of the sums.  s_w: a word a group.
+// Where a group is of whole pieces of 2^i lanes, its two best are found in registers, piece by
+// piece and then over those lanes; else by reading its scores from s_v (E words; s_w then is
+// every per-th of them).
+template <int LPR, int NV, int VEC>
+__device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, const ScoreArgs& a,
+                                            float near, float* s_v) {
+  const int per = a.E / a.groups, span = per / VEC;          // (pieces of a group)
+  const auto col = [&](int i) { return (lane + LPR * (i / VEC)) * VEC + i % VEC; };
+  const auto either = [](uint32_t p, uint32_t q) { return p | q; };
+  float low = INFINITY, high = -INFINITY;
   bool odd = false;                                // (NaN among them)
-  for (int g = lane; g < a.groups; g += LPR) {
-    const F worth = s_v[g * per];
-    const U o = O::of(worth);
-    int rank = 0;
-    for (int q = 0; q < a.groups; ++q) {
-      const U oq = O::of(s_v[q * per]);
-      rank += oq > o || (oq == o && q < g);
-    }
-    const bool in = rank < a.top_groups && o > O::kClosed;
-    if (in) stay[g >> 5] |= 1u << (g & 31);
+  auto note = [&](float worth, bool in) {
     odd |= worth != worth;
     if (in) low = worth < low ? worth : low;
     else high = worth > high ? worth : high;
-  }
-  const auto either = [](uint32_t p, uint32_t q) { return p | q; };
-  stay[0] = over_row<LPR>(stay[0], either);
-  if (a.groups > 32) stay[1] = over_row<LPR>(stay[1], either);
-  bool close = false;
-  if (unit > 0) {
-    low = over_row<LPR>(low, [](F p, F q) { return q < p ? q : p; });
-    high = over_row<LPR>(high, [](F p, F q) { return q > p ? q : p; });
-    close = over_row<LPR>(odd ? 1u : 0u, either) != 0;
-    if (a.top_groups < a.groups && high > -INFINITY && low < INFINITY)
-      close |= !(low - high > 2 * near + 2 * unit * (fabsf(low) + fabsf(high)));
-  }
-  const float inv = 1.0f / per;
+  };
+  if (per % VEC == 0 && (span & (span - 1)) == 0 && span <= LPR) {
+    uint32_t o1[NV], o2[NV];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    // (exact: columns are below 2^10, and half a step from the border)
-    const int g = static_cast<int>((col(i) + 0.5f) * inv);
-    if (!((stay[(g >> 5) & 1] >> (g & 31)) & 1u)) v[i] = -INFINITY;
+    for (int j = 0; j < NV; ++j) {
+      o1[j] = o2[j] = 0u;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) merge_two(o1[j], o2[j], o[j * VEC + i], 0u);
+    }
+    auto step = [&](auto d) {
+      if (decltype(d)::value >= span) return;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        merge_two(o1[j], o2[j], other<decltype(d)::value>(o1[j]), other<decltype(d)::value>(o2[j]));
+    };
+    if constexpr (LPR > 1) step(std::integral_constant<int, 1>());
+    if constexpr (LPR > 2) step(std::integral_constant<int, 2>());
+    if constexpr (LPR > 4) step(std::integral_constant<int, 4>());
+    if constexpr (LPR > 8) step(std::integral_constant<int, 8>());
+    if constexpr (LPR > 16) step(std::integral_constant<int, 16>());
+    if constexpr (LPR > 32) step(std::integral_constant<int, 32>());
+    float worth[NV];
+    uint32_t ow[NV];
+    int g[NV], rank[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      worth[j] = worth_of(o1[j], o2[j]);
+      ow[j] = order_of(worth[j]);
+      g[j] = static_cast<int>((lane + LPR * j + 0.5f) * (1.0f / span));
+      rank[j] = 0;
+      if ((lane + LPR * j) % span == 0 && g[j] < a.groups) s_v[g[j]] = __uint_as_float(ow[j]);
+    }
+    row_fence();
+    for (int q = 0; q < a.groups; ++q) {
+      const uint32_t oq = __float_as_uint(s_v[q]);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) rank[j] += oq > ow[j] || (oq == ow[j] && q < g[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const bool in = rank[j] < a.top_groups && ow[j] > kNone;
+      if (g[j] < a.groups) note(worth[j], in);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) o[j * VEC + i] = in ? o[j * VEC + i] : 0u;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV * VEC; ++i)
+      if (col(i) < a.E) s_v[col(i)] = __uint_as_float(o[i]);
+    row_fence();
+    for (int g = lane; g < a.groups; g += LPR) {
+      uint32_t o1 = 0, o2 = 0;
+      for (int i = 0; i < per; ++i) merge_two(o1, o2, __float_as_uint(s_v[g * per + i]), 0u);
+      s_v[g * per] = worth_of(o1, o2);             // (in the place of its first score)
+    }
+    row_fence();
+    uint32_t stay[2] = {0u, 0u};
+    for (int g = lane; g < a.groups; g += LPR) {
+      const float worth = s_v[g * per];
+      const uint32_t ow = order_of(worth);
+      int rank = 0;
+      for (int q = 0; q < a.groups; ++q) {
+        const uint32_t oq = order_of(s_v[q * per]);
+        rank += oq > ow || (oq == ow && q < g);
+      }
+      const bool in = rank < a.top_groups && ow > kNone;
+      if (in) stay[g >> 5] |= 1u << (g & 31);
+      note(worth, in);
+    }
+    stay[0] = over_row<LPR>(stay[0], either);
+    stay[1] = over_row<LPR>(stay[1], either);
+    const float inv = 1.0f / per;
+#pragma unroll
+    for (int i = 0; i < NV * VEC; ++i) {
+      // (exact: columns are below 2^10, and half a step from the border)
+      const int g = static_cast<int>((col(i) + 0.5f) * inv);
+      if (!((stay[(g >> 5) & 1] >> (g & 31)) & 1u)) o[i] = 0u;
+    }
   }
-  return close;
+  low = over_row<LPR>(low, [](float p, float q) { return q < p ? q : p; });
+  high = over_row<LPR>(high, [](float p, float q) { return q > p ? q : p; });
+  if (over_row<LPR>(odd ? 1u : 0u, either)) return true;
+  return a.top_groups < a.groups && high > -INFINITY && low < INFINITY &&
+         !(low - high > 2 * near + 2 * kUnit * (fabsf(low) + fabsf(high)));
 }
 
-// The k largest of a row's fp32 scores, and whether a gap that decides is within `near` and the
-// bias' rounding.  The largest value of the row is found first and its lowest column then: fewer
-// operations than with both at once, and the score itself need not be carried (rows_weights
-// takes the chosen logits again).
-template <typename T, int LPR, int N, typename Col>
+// The k largest of a row's fp32 scores, of orders o, and whether a gap that decides is within
+// `near` and the bias' rounding.  The row's largest value is found first and its lowest column
+// then: fewer operations than with both at once, and no score need be carried (the weights are
+// computed from the chosen logits again).
+template <typename T, int LPR, int NV, int VEC>
 __device__ __forceinline__ bool choose_fast(const ScoreArgs& a, const T* logits,
-                                            const float (&v)[N], Col col, int lane, float near,
-                                            float unit, int16_t* s_expert) {
-  uint32_t o[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) o[i] = col(i) < a.E ? order_of(v[i]) : 0u;
+                                            uint32_t (&o)[NV * VEC], int lane, float near,
+                                            int16_t* s_expert) {
+  constexpr int N = NV * VEC;
   bool close = false;
   uint32_t before = 0, before_c = 0;
-  // (one more than is chosen)
-  const int last = a.k < a.E ? a.k : a.k - 1;
-  for (int s = 0; s <= last; ++s) {
+  // (one more than is chosen, and on while it ties with the last)
+  for (int s = 0; s < a.E; ++s) {
     uint32_t best = 0u;
 #pragma unroll
     for (int i = 0; i < N; ++i) best = o[i] > best ? o[i] : best;
@@ -194,84 +251,102 @@ __device__ __forceinline__ bool choose_fast(const ScoreArgs& a, const T* logits,
     int mine = N;
 #pragma unroll
     for (int i = N - 1; i >= 0; --i) mine = o[i] == best ? i : mine;
-    uint32_t c = 0xffffffffu;
-    if (mine < N) c = col(mine);
-    const uint32_t own = c;
-    c = over_row<LPR>(c, [](uint32_t p, uint32_t q) { return q < p ? q : p; });
+    const uint32_t own = mine < N ? (lane + LPR * (mine / VEC)) * VEC + mine % VEC : 0xffffffffu;
+    const uint32_t c = over_row<LPR>(own, [](uint32_t p, uint32_t q) { return q < p ? q : p; });
     if (s > 0) {
       const float p = value_of(before), q = value_of(best);
-      if (!(p - q > near + unit * (fabsf(p) + fabsf(q)))) {
-        // equal logits with equal biases have equal scores in any arithmetic (but past
-        // the last choice a tie hides what comes behind it)
-        close |= s >= a.k || Row<T>::get(logits[before_c]) != Row<T>::get(logits[c]) ||
+      if (!(p - q > near + kUnit * (fabsf(p) + fabsf(q)))) {
+        // equal logits with equal biases have equal scores in any arithmetic
+        close |= Row<T>::get(logits[before_c]) != Row<T>::get(logits[c]) ||
                  (a.bias && a.bias[before_c] != a.bias[c]);
+      } else if (s >= a.k) {
+        break;
       }
+      if (close) break;                            // (choose_slow writes the row)
     }
     before = best;
     before_c = c;
-    if (s >= a.k) break;
     mine = own == c ? mine : N;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = i == mine ? 0u : o[i];
-    if (lane == 0) s_expert[s] = static_cast<int16_t>(c);
+    if (lane == 0 && s < a.k) s_expert[s] = static_cast<int16_t>(c);
   }
   return close;
 }
 
-// A row again, by a whole wave in 64 bits.
+// A row again, by a whole wave in 64 bits, out of LDS: s_v has room for E scores, s_w for a
+// value a group.
 template <typename T>
-__device__ void choose_slow(const ScoreArgs& a, const T* logits, double* s_v, int16_t* s_expert) {
-  constexpr int N = kMaxE / 64;
-  typedef Order<double> O;
-  const int lane = threadIdx.x & 63;
-  const auto col = [&](int i) { return lane + 64 * i; };
-  double v[N];
-  float top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float x = col(i) < a.E ? Row<T>::get(logits[col(i)]) : -INFINITY;
-    v[i] = x;
-    top = x > top || x != x ? x : top;
-  }
+__device__ __forceinline__ void choose_slow(const ScoreArgs& a, const T* logits, double* s_v,
+                                            double* s_w, int16_t* s_expert) {
+  const int lane = threadIdx.x & 63, E = a.E;
+  double top = 0.0, sum = 1.0;
   if (a.softmax) {
-    top = over_row<64>(top, [](float p, float q) { return q > p || q != q ? q : p; });
-    if (top == -INFINITY) top = 0.0f;
-  }
-  double sum = 0.0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (64 * i >= a.E) break;
-    const double x = v[i];
-    const double e = exp(a.softmax ? x - static_cast<double>(top) : -x);
-    sum += e;
-    v[i] = x == -INFINITY ? -INFINITY : a.softmax ? e : 1.0 / (1.0 + e);
-  }
-  if (a.softmax) {
+    float t = -INFINITY;
+#pragma unroll 1
+    for (int c = lane; c < E; c += 64) {
+      const float x = Row<T>::get(logits[c]);
+      t = x > t || x != x ? x : t;
+    }
+    t = over_row<64>(t, [](float p, float q) { return q > p || q != q ? q : p; });
+    top = t == -INFINITY ? 0.0f : t;
+    sum = 0.0;
+#pragma unroll 1
+    for (int c = lane; c < E; c += 64) sum += exp(Row<T>::get(logits[c]) - top);
     sum = over_row<64>(sum, [](double p, double q) { return p + q; });
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = v[i] == -INFINITY ? v[i] : v[i] / (sum == 0.0 ? 1.0 : sum);
+    if (sum == 0.0) sum = 1.0;
   }
-  if (a.bias) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (col(i) < a.E && v[i] != -INFINITY) v[i] += a.bias[col(i)];
+#pragma unroll 1
+  for (int c = lane; c < E; c += 64) {
+    const double x = Row<T>::get(logits[c]), e = exp(a.softmax ? x - top : -x);
+    const double v = (a.softmax ? e / sum : 1.0 / (1.0 + e)) + (a.bias ? a.bias[c] : 0.0f);
+    s_v[c] = x == -INFINITY ? x : v;
   }
-  if (a.groups > 1) keep_groups<double, 64>(v, col, lane, a, 0.0, 0.0, s_v);
-  uint64_t o[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) o[i] = col(i) < a.E ? O::of(v[i]) : 0u;
+  row_fence();
+  if (a.groups > 1) {                              // (a lane a group)
+    const int per = E / a.groups;
+    uint64_t ow = 0;
+    if (lane < a.groups) {
+      uint64_t o1 = 0, o2 = 0;
+#pragma unroll 1
+      for (int i = 0; i < per; ++i) {
+        const uint64_t o = order_of(s_v[lane * per + i]);
+        if (o > o1) o2 = o1, o1 = o; else if (o > o2) o2 = o;
+      }
+      double w = value_of(o1 > kNone64 ? o1 : kNone64);
+      if (o2 > kNone64) w += value_of(o2);
+      s_w[lane] = w;
+      ow = order_of(w);
+    }
+    row_fence();
+    if (lane < a.groups) {
+      int rank = 0;
+#pragma unroll 1
+      for (int q = 0; q < a.groups; ++q) {
+        const uint64_t oq = order_of(s_w[q]);
+        rank += oq > ow || (oq == ow && q < lane);
+      }
+      if (rank >= a.top_groups)
+#pragma unroll 1
+        for (int i = 0; i < per; ++i) s_v[lane * per + i] = -INFINITY;
+    }
+    row_fence();
+  }
   for (int s = 0; s < a.k; ++s) {
     uint64_t best = 0;
     uint32_t c = 0xffffffffu;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (o[i] > best) best = o[i], c = col(i);
+#pragma unroll 1
+    for (int i = lane; i < E; i += 64) {
+      const uint64_t o = order_of(s_v[i]);
+      if (o > best) best = o, c = i;
+    }
     best_of_row<64>(best, c);
-    const bool some = best > O::kClosed;
-    if (lane == 0) s_expert[s] = static_cast<int16_t>(some ? static_cast<int32_t>(c) : -1);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (static_cast<uint32_t>(col(i)) == c) o[i] = 0;
+    const bool some = best > kNone64;
+    if (lane == 0) {
+      s_expert[s] = static_cast<int16_t>(some ? static_cast<int32_t>(c) : -1);
+      if (some) s_v[c] = -INFINITY;
+    }
+    row_fence();
   }
 }
 
@@ -288,6 +363,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
   __shared__ int16_t s_expert[kPairs], s_slow[kThreads];
   __shared__ float s_weight[kPairs];
   __shared__ int32_t s_start[kMaxE], s_wave[kWaves], s_nslow;
+  __shared__ double s_worth[kWaves][kMaxG];
   // (the whole row's softmax, where the weights ask for it: in s_start, free until then)
   float* const s_top = reinterpret_cast<float*>(s_start);
   float* const s_sum = s_top + kThreads;
@@ -295,7 +371,6 @@ __global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * a.rows_blk;
   const int nrow = static_cast<int>(a.n - row0 < a.rows_blk ? a.n - row0 : a.rows_blk);
   const T* const logits = static_cast<const T*>(a.logits) + row0 * E;
-  const auto col = [&](int i) { return (lane + LPR * (i / VEC)) * VEC + i % VEC; };
   if (threadIdx.x == 0) s_nslow = 0;
   __syncthreads();
   float bias[NV][VEC], next[NV][VEC];
@@ -349,16 +424,15 @@ __global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_rcpf(1.0f + expf(-x[i]));
     }
+    uint32_t o[N];
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      v[i] = x[i] == -INFINITY ? -INFINITY : v[i] + bias[i / VEC][i % VEC];
-    constexpr float kUnit = 0x1p-22f;              // 4 units: of the biased score, twice
+      o[i] = x[i] == -INFINITY ? 0u : order_of(v[i] + bias[i / VEC][i % VEC]);
     bool close = false;
     if (a.groups > 1)
-      close = keep_groups<float, LPR>(v, col, lane, a, near, kUnit,
-                                      s_room + group * (LPR * N + 1));
-    close |= choose_fast<T, LPR>(a, logits + static_cast<int64_t>(q) * E, v, col, lane, near, kUnit,
-                                 s_expert + q * a.k);
+      close = keep_groups<LPR, NV, VEC>(o, lane, a, near, s_room + group * (LPR * N + 1));
+    close |= choose_fast<T, LPR, NV, VEC>(a, logits + static_cast<int64_t>(q) * E, o, lane, near,
+                                          s_expert + q * a.k);
     if (close && lane == 0) s_slow[atomicAdd(&s_nslow, 1)] = static_cast<int16_t>(q);
   }
   __syncthreads();
@@ -369,7 +443,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
     for (int i = wave; i < nslow; i += takes) {
       const int q = s_slow[i];
       choose_slow(a, logits + static_cast<int64_t>(q) * E,
-                  reinterpret_cast<double*>(s_room) + wave * E, s_expert + q * a.k);
+                  reinterpret_cast<double*>(s_room) + wave * E, s_worth[wave], s_expert + q * a.k);
     }
   __syncthreads();
   // The weights, a row a lane, from the chosen logits.
@@ -419,32 +493,52 @@ struct ScoreGrad {
   hipStream_t st;
 };
 
-// The gradient: every lane sums the row's slots itself (they are the same addresses for the
-// whole row), then finds its columns among them.
+// The gradient: a row's lanes share its slots, and leave each slot's gradient at its expert's
+// column in LDS, from where every lane takes its columns'.
 template <typename T, int LPR, int NV, bool TAIL>
 __global__ __launch_bounds__(kThreads) void k_scores_bwd(ScoreGrad a) {
-  constexpr int VEC = Row<T>::VEC, G = kThreads / LPR;
+  constexpr int VEC = Row<T>::VEC, G = kThreads / LPR, W = LPR * NV * VEC;
+  __shared__ __attribute__((aligned(16))) float s_grad[G * W];
   const int lane = threadIdx.x % LPR, E = a.E, k = a.k;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * G + threadIdx.x / LPR;
-  if (r >= a.n) return;
+  if (r >= a.n) return;                            // (a row's lanes together; no barriers)
   const T* const logits = a.logits ? static_cast<const T*>(a.logits) + r * E : nullptr;
+  float* const row = s_grad + threadIdx.x / LPR * W;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < VEC; i += 4)
+      *reinterpret_cast<float4*>(row + (lane + LPR * j) * VEC + i) = make_float4(0, 0, 0, 0);
+  // this lane's slots (the whole row's dot product and sum of scores)
+  constexpr int S = (kMaxK + LPR - 1) / LPR;
+  int32_t e[S];
+  float w[S], dw[S], p[S];
+  float dot = 0.0f, sum = 0.0f;
+#pragma unroll
+  for (int t = 0; t < S; ++t) {
+    const int s = lane + LPR * t;
+    e[t] = -1, w[t] = dw[t] = p[t] = 0.0f;
+    if (LPR * t >= k) continue;                    // (uniform)
+    e[t] = s < k ? a.experts[r * k + s] : -1;
+    if (e[t] >= E) e[t] = -1;
+    w[t] = e[t] < 0 ? 0.0f : a.weights[r * k + s];
+    dw[t] = e[t] < 0 ? 0.0f : a.dweights[r * k + s];
+    p[t] = 0.0f;
+    if (!a.softmax && e[t] >= 0) p[t] = 1.0f / (1.0f + expf(-Row<T>::get(logits[e[t]])));
+  }
+#pragma unroll
+  for (int t = 0; t < S; ++t) {
+    if (e[t] >= 0) dot += w[t] * dw[t];
+    sum += p[t];
+  }
+  const auto add = [](float u, float v) { return u + v; };
+  dot = over_row<LPR>(dot, add);
+  sum = over_row<LPR>(sum, add);
   float g[NV][VEC];
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int i = 0; i < VEC; ++i) g[j][i] = 0.0f;
-  float dot = 0.0f, sum = 0.0f;
-  auto expert = [&](int s) {
-    const int32_t e = a.experts[r * k + s];
-    return e < E ? e : -1;
-  };
-  auto score = [&](int32_t e) { return 1.0f / (1.0f + expf(-Row<T>::get(logits[e]))); };
-  for (int s = 0; s < k; ++s) {
-    const int32_t e = expert(s);
-    if (e < 0) continue;
-    dot += a.weights[r * k + s] * a.dweights[r * k + s];
-    if (!a.softmax && a.normalize) sum += score(e);
-  }
   if (a.softmax && !a.normalize) {
     // the whole row's softmax
     float top = -INFINITY, all = 0.0f;
@@ -460,42 +554,41 @@ __global__ __launch_bounds__(kThreads) void k_scores_bwd(ScoreGrad a) {
         top = g[j][i] > top || g[j][i] != g[j][i] ? g[j][i] : top;
       }
     }
-    top = over_row<LPR>(top, [](float p, float q) { return q > p || q != q ? q : p; });
+    top = over_row<LPR>(top, [](float u, float v) { return v > u || v != v ? v : u; });
     if (top == -INFINITY) top = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) all += g[j][i] = expf(g[j][i] - top);
-    all = over_row<LPR>(all, [](float p, float q) { return p + q; });
+    all = over_row<LPR>(all, add);
     const float f = all == 0.0f ? 0.0f : -dot / all;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) g[j][i] *= f;
   }
+  row_fence();
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  for (int s = 0; s < k; ++s) {
-    const int32_t e = expert(s);
-    if (e < 0) continue;
-    const float w = a.weights[r * k + s], dw = a.dweights[r * k + s];
+#pragma unroll
+  for (int t = 0; t < S; ++t) {
+    if (LPR * t >= k || e[t] < 0) continue;
     float d;
     if (a.softmax) {
-      d = w * (a.normalize ? dw - dot / a.scale : dw);
+      d = w[t] * (a.normalize ? dw[t] - dot / a.scale : dw[t]);
     } else {
-      const float p = score(e);
-      d = a.normalize ? (dw * a.scale - dot) * inv : dw * a.scale;
-      d = d * p * (1.0f - p);
+      d = a.normalize ? (dw[t] * a.scale - dot) * inv : dw[t] * a.scale;
+      d = d * p[t] * (1.0f - p[t]);
     }
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i)
-        if ((lane + LPR * j) * VEC + i == e) g[j][i] += d;
+    atomicAdd(row + e[t], d);                      // (an expert is chosen once: no order in it)
   }
+  row_fence();
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (lane + LPR * j) * VEC;
-    if (c < E) store_row<T, TAIL>(static_cast<T*>(a.dlogits) + r * E, c, E, g[j]);
+    if (c >= E) continue;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) g[j][i] += row[c + i];
+    store_row<T, TAIL>(static_cast<T*>(a.dlogits) + r * E, c, E, g[j]);
   }
 }
 
