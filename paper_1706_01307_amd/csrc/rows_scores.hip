@@ -124,10 +124,9 @@ __device__ __forceinline__ float worth_of(uint32_t o1, uint32_t o2) {
 
 // The groups of a row that stay, by fp32 scores: o, the orders of a lane's NV * VEC biased scores,
 // become 0 where their group goes.  Returns whether the gap between the last group that stays and
-// the best that goes is within `near` and the roundings of the sums.  s_w: a word a group.
+// the best that goes is within `near` and the roundings of the sums.  s_v: E words.
 // Where a group is of whole pieces of 2^i lanes, its two best are found in registers, piece by
-// piece and then over those lanes; else by reading its scores from s_v (E words; s_w then is
-// every per-th of them).
+// piece and then over those lanes; else by reading its scores from s_v.
 template <int LPR, int NV, int VEC>
 __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, const ScoreArgs& a,
                                             float near, float* s_v) {
@@ -190,14 +189,17 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
     for (int i = 0; i < NV * VEC; ++i)
       if (col(i) < a.E) s_v[col(i)] = __uint_as_float(o[i]);
     row_fence();
+#pragma unroll 1
     for (int g = lane; g < a.groups; g += LPR) {
       uint32_t o1 = 0, o2 = 0;
       for (int i = 0; i < per; ++i) merge_two(o1, o2, __float_as_uint(s_v[g * per + i]), 0u);
       s_v[g * per] = worth_of(o1, o2);             // (in the place of its first score)
     }
     row_fence();
-    uint32_t stay[2] = {0u, 0u};
-    for (int g = lane; g < a.groups; g += LPR) {
+    uint32_t stay = 0;                             // (of this lane's groups)
+    int t = 0;
+#pragma unroll 1
+    for (int g = lane; g < a.groups; g += LPR, ++t) {
       const float worth = s_v[g * per];
       const uint32_t ow = order_of(worth);
       int rank = 0;
@@ -206,17 +208,20 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
         rank += oq > ow || (oq == ow && q < g);
       }
       const bool in = rank < a.top_groups && ow > kNone;
-      if (in) stay[g >> 5] |= 1u << (g & 31);
       note(worth, in);
+      stay |= in ? 1u << t : 0u;
     }
-    stay[0] = over_row<LPR>(stay[0], either);
-    stay[1] = over_row<LPR>(stay[1], either);
+    row_fence();
+    t = 0;
+#pragma unroll 1
+    for (int g = lane; g < a.groups; g += LPR, ++t) s_v[g * per] = stay >> t & 1 ? 1.0f : 0.0f;
+    row_fence();
     const float inv = 1.0f / per;
 #pragma unroll
     for (int i = 0; i < NV * VEC; ++i) {
       // (exact: columns are below 2^10, and half a step from the border)
       const int g = static_cast<int>((col(i) + 0.5f) * inv);
-      if (!((stay[(g >> 5) & 1] >> (g & 31)) & 1u)) o[i] = 0u;
+      if (col(i) < a.E && s_v[g * per] == 0.0f) o[i] = 0u;
     }
   }
   low = over_row<LPR>(low, [](float p, float q) { return q < p ? q : p; });
