@@ -68,7 +68,9 @@ template <typename T, bool Z8, bool GRAD> int run(int act, const ActArgs& a) {
   return by_act(act, [&](auto k) {
     constexpr int ACT = decltype(k)::value;
     if (pieces <= 4) return run_lanes<T, Z8, GRAD, ACT, 4>(a);
+    if (pieces <= 8) return run_lanes<T, Z8, GRAD, ACT, 8>(a);
     if (pieces <= 16) return run_lanes<T, Z8, GRAD, ACT, 16>(a);
+    if (pieces <= 32) return run_lanes<T, Z8, GRAD, ACT, 32>(a);
     return run_lanes<T, Z8, GRAD, ACT, 64>(a);
   });
 }
