@@ -647,7 +647,7 @@ __device__ __forceinline__ u32x4_t widen_half(uint32_t lo, uint32_t hi) {
 // when it grows): what is 2^17 below it loses bits, but nothing over 2^-40 of it.
 // WHOLE: rows are of whole pieces.
 template <typename T, bool X8, int BC, int BN, int WR, int WC, int KB, bool WHOLE>
-__global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
+__global__ __launch_bounds__(64 * WR * WC, WR * WC / 2) void k_linear_dw(LinearWeight a) {
   typedef KTile<T, BC, KB> TX;
   typedef KTile<T, BN, KB> TY;
   constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = 64 * WR * WC;
