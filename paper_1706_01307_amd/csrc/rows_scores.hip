@@ -109,6 +109,7 @@ struct ScoreArgs {
   hipStream_t st;
 };
 
+constexpr float kLog2e = 1.44269504f;
 constexpr float kUnit = 0x1p-22f;                  // 4 units: of a biased score, twice
 
 // The two largest of two pairs (first >= second).
@@ -232,17 +233,25 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
 }
 
 // The k largest of a row's fp32 scores, of orders o, and whether a gap that decides is within
-// `near` and the bias' rounding.  The row's largest value is found first and its lowest column
-// then: fewer operations than with both at once, and no score need be carried (the weights are
-// computed from the chosen logits again).
-template <typename T, int LPR, int NV, int VEC>
+// `near` and the bias' rounding.  For the search the column, from the last one down, takes the
+// place of an order's lowest bits (as many as columns have), so that one search finds both, of equal
+// scores the lowest column, and no two are equal; scores that those bits would tell apart
+// are computed again, two at a time (score(column), as they were).  (Value and column searched for
+// apart: 116 us for 348,208 x 64 to 8, and 100 so.)
+template <typename T, int LPR, int NV, int VEC, typename Score>
 __device__ __forceinline__ bool choose_fast(const ScoreArgs& a, const T* logits,
                                             uint32_t (&o)[NV * VEC], int lane, float near,
-                                            int16_t* s_expert) {
+                                            uint32_t mask, Score score, int16_t* s_expert) {
   constexpr int N = NV * VEC;
+  const uint32_t first = mask - lane * VEC;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    o[i] = o[i] ? (o[i] & ~mask) | (first - (LPR * VEC * (i / VEC) + i % VEC)) : 0u;
+  // of a score: kUnit, and mask + 1 units of order
+  const float unit = kUnit + (mask + 1) * 0x1p-23f;
   bool close = false;
-  uint32_t before = 0, before_c = 0;
-  // (one more than is chosen, and on while it ties with the last)
+  uint32_t before = 0;
+  // (on behind the last choice while those bits could tell one from it)
   for (int s = 0; s < a.E; ++s) {
     uint32_t best = 0u;
 #pragma unroll
@@ -253,27 +262,24 @@ __device__ __forceinline__ bool choose_fast(const ScoreArgs& a, const T* logits,
       for (int t = s + lane; t < a.k; t += LPR) s_expert[t] = -1;
       break;
     }
-    int mine = N;
-#pragma unroll
-    for (int i = N - 1; i >= 0; --i) mine = o[i] == best ? i : mine;
-    const uint32_t own = mine < N ? (lane + LPR * (mine / VEC)) * VEC + mine % VEC : 0xffffffffu;
-    const uint32_t c = over_row<LPR>(own, [](uint32_t p, uint32_t q) { return q < p ? q : p; });
+    const uint32_t c = mask - (best & mask);
     if (s > 0) {
-      const float p = value_of(before), q = value_of(best);
-      if (!(p - q > near + kUnit * (fabsf(p) + fabsf(q)))) {
+      const float p = value_of(before & ~mask), q = value_of(best & ~mask);
+      if (!(p - q > near + unit * (fabsf(p) + fabsf(q)))) {
         // equal logits with equal biases have equal scores in any arithmetic
-        close |= Row<T>::get(logits[before_c]) != Row<T>::get(logits[c]) ||
-                 (a.bias && a.bias[before_c] != a.bias[c]);
+        const uint32_t d = mask - (before & mask);
+        if (Row<T>::get(logits[d]) != Row<T>::get(logits[c]) || (a.bias && a.bias[d] != a.bias[c])) {
+          const float u = score(d), v = score(c);
+          close = !(u - v > near + kUnit * (fabsf(u) + fabsf(v)));
+          if (close) break;                        // (choose_slow writes the row)
+        }
       } else if (s >= a.k) {
         break;
       }
-      if (close) break;                            // (choose_slow writes the row)
     }
-    before = best;
-    before_c = c;
-    mine = own == c ? mine : N;
+    if (s < a.k) before = best;
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = i == mine ? 0u : o[i];
+    for (int i = 0; i < N; ++i) o[i] = o[i] == best ? 0u : o[i];
     if (lane == 0 && s < a.k) s_expert[s] = static_cast<int16_t>(c);
   }
   return close;
@@ -402,32 +408,38 @@ __global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
     for (int i = 0; i < VEC; ++i) bias[j][i] = 0.0f;
     if (a.bias && c < E) load_f32<VEC, TAIL>(a.bias, c, E, bias[j]);
   }
+  uint32_t mask = 1;
+  while (mask < static_cast<uint32_t>(E)) mask *= 2;
+  --mask;                                          // (columns are at most this)
   request(group);
   for (int q = group; q < nrow; q += G) {          // (a group's lanes stay together)
     float x[N], v[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = next[i / VEC][i % VEC];
     request(q + G);
-    // fp32 scores: within 4 units of the sigmoid, or 32 of the softmax's largest (exp, the
-    // sum of 16 terms and 6 steps, a division); twice as much for both sides of a gap
-    float near = 0x1p-21f;
+    // fp32 scores: within 4 units of 1 of the sigmoid (exp2 and the reciprocal a unit each, the
+    // exponent's rounding times s (1 - s) |x| < 0.28), or 32 of the softmax's largest (those,
+    // times p |x| < 0.37 p's largest, and the sum of 16 terms and 6 steps); twice as
+    // much for both sides of a gap
+    float near = 0x1p-21f, top = -INFINITY, inv = 0.0f;
     if (a.softmax) {
-      float top = -INFINITY, sum = 0.0f;
+      float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < N; ++i) top = x[i] > top || x[i] != x[i] ? x[i] : top;
       top = over_row<LPR>(top, [](float p, float r) { return r > p || r != r ? r : p; });
       if (top == -INFINITY) top = 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) sum += v[i] = expf(x[i] - top);
+      for (int i = 0; i < N; ++i) sum += v[i] = __builtin_amdgcn_exp2f((x[i] - top) * kLog2e);
       sum = over_row<LPR>(sum, [](float p, float r) { return p + r; });
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] *= inv;
       near = 0x1p-18f * inv;                       // (the largest is exp(0) / sum)
       if (lane == 0) s_top[q] = top, s_sum[q] = inv;
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_rcpf(1.0f + expf(-x[i]));
+      for (int i = 0; i < N; ++i)
+        v[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * -kLog2e));
     }
     uint32_t o[N];
 #pragma unroll
@@ -436,8 +448,17 @@ __global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
     bool close = false;
     if (a.groups > 1)
       close = keep_groups<LPR, NV, VEC>(o, lane, a, near, s_room + group * (LPR * N + 1));
-    close |= choose_fast<T, LPR, NV, VEC>(a, logits + static_cast<int64_t>(q) * E, o, lane, near,
-                                          s_expert + q * a.k);
+    const T* const row = logits + static_cast<int64_t>(q) * E;
+    if (!close)
+      close = choose_fast<T, LPR, NV, VEC>(
+          a, row, o, lane, near, mask,
+          [&](uint32_t c) {
+            const float xc = Row<T>::get(row[c]);
+            const float vc = a.softmax ? __builtin_amdgcn_exp2f((xc - top) * kLog2e) * inv
+                                       : __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(xc * -kLog2e));
+            return vc + (a.bias ? a.bias[c] : 0.0f);
+          },
+          s_expert + q * a.k);
     if (close && lane == 0) s_slow[atomicAdd(&s_nslow, 1)] = static_cast<int16_t>(q);
   }
   __syncthreads();
