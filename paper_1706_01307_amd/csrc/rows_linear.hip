@@ -15,6 +15,7 @@ namespace spc {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kSplit = 8;      // slices of the reduction where k_linear has few tiles
 
 struct LinearArgs {
   const void* x;               // [n][red]
@@ -62,16 +63,20 @@ __device__ __forceinline__ uint2 load8_left(const uint8_t* p, int64_t left) {
 // wait at.
 // Forward: z = acc * scale + bias (z is kept if asked for), y = act(z) + residual.
 // BT (input gradient): y = acc * act'(side).
-template <typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC, int BYTES, bool PAST>
+// SPLIT: so many groups of WR x WC waves have a slice of the reduction each; their sums are
+// added here, in order.
+template <typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC, int BYTES, bool PAST,
+          int SPLIT = 1>
 __device__ __forceinline__ void finish_tile(u32x4_t* lds,
                                             const f32x16 (&acc)[BN / WC / 32][BM / WR / 32],
                                             const LinearArgs& a, int64_t row0, int n0) {
-  constexpr int FM = BM / WR / 32, FN = BN / WC / 32, VO = Row<TO>::VEC, NT = 64 * WR * WC;
-  constexpr int RW = WR * 32, FNP = RW * BN * 4 <= BYTES ? FN : 1, CW = WC * 32 * FNP;
-  constexpr int PR = CW / VO, NPC = RW * PR / NT, Q = VO / 4;
-  static_assert(RW * CW * 4 <= BYTES, "a part of the finished tile fits");
-  static_assert(NT % PR == 0 && NPC * NT == RW * PR, "a lane's pieces lie in the same columns");
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
+  constexpr int FM = BM / WR / 32, FN = BN / WC / 32, VO = Row<TO>::VEC, NT = 64 * WR * WC * SPLIT;
+  constexpr int RW = WR * 32, FNP = RW * BN * 4 * SPLIT <= BYTES ? FN : 1, CW = WC * 32 * FNP;
+  constexpr int PR = CW / VO, NPC = RW * PR > NT ? RW * PR / NT : 1, Q = VO / 4;
+  constexpr int PART = RW * CW / 4;                // pieces of a slice's part
+  static_assert(PART * SPLIT * 16 <= BYTES, "a part of the finished tile fits");
+  static_assert(NT % PR == 0 && NPC * NT >= RW * PR, "a lane's pieces lie in the same columns");
+  const int slice = threadIdx.x / (64 * WR * WC), wave = (threadIdx.x >> 6) % (WR * WC), lane = threadIdx.x & 63, h = lane >> 5;
   const int wrow = wave / WC, wcol = wave % WC, piece = threadIdx.x % PR;
   const bool side8 = BT && a.side_scale;
 #pragma unroll
@@ -95,7 +100,7 @@ __device__ __forceinline__ void finish_tile(u32x4_t* lds,
       for (int i = 0; i < NPC; ++i) {
         const int lr = (threadIdx.x + NT * i) / PR;
         const int64_t r = row0 + lr / 32 * (BM / WR) + 32 * m + lr % 32;
-        live[i] = r < a.n && left > 0;
+        live[i] = r < a.n && left > 0 && (NPC * NT == RW * PR || lr < RW);
         at[i] = r * a.cols + col;
         xs[i] = X8 && live[i] ? a.x_scale[r] : 1.0f;
         if (a.side && live[i]) {
@@ -119,7 +124,7 @@ __device__ __forceinline__ void finish_tile(u32x4_t* lds,
           u32x4_t v;
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(acc[np + f][m][4 * q + i]);
-          lds[out_at<float, CW>(wrow * 32 + (lane & 31), c / 4)] = v;
+          lds[slice * PART + out_at<float, CW>(wrow * 32 + (lane & 31), c / 4)] = v;
         }
       __syncthreads();
 #pragma unroll
@@ -129,9 +134,16 @@ __device__ __forceinline__ void finish_tile(u32x4_t* lds,
         float v[VO];
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-          const u32x4_t u = lds[out_at<float, CW>(lr, piece * Q + q)];
+          const int at = out_at<float, CW>(lr, piece * Q + q);
+          const u32x4_t u = lds[at];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[4 * q + e] = __uint_as_float(u[e]);
+#pragma unroll
+          for (int p = 1; p < SPLIT; ++p) {
+            const u32x4_t more = lds[p * PART + at];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * q + e] += __uint_as_float(more[e]);
+          }
         }
         if constexpr (BT) {
           if (a.side) {
@@ -206,8 +218,9 @@ template <int R, int BK> struct RTile8 {
 // true: w is [cols][red] (the input gradient).  A workgroup of WR x WC waves takes a tile of BM
 // rows by BN columns, in stages of BK of the reduction through a ring of LDS buffers: all but
 // one stage are on their way while that one is multiplied, one barrier a stage.
-template <typename T, typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC, bool PAST>
-__global__ __launch_bounds__(64 * WR * WC, 2) void k_linear(LinearArgs a) {
+template <typename T, typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC, bool PAST,
+          int SPLIT>
+__global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a) {
   // (rows in 8 bits: 64 of them are too few pieces for the lanes in stages of 32)
   constexpr int KB = X8 && BM == 64 ? 128 : 64, BK = kBK<T, KB>, NT = 64 * WR * WC;
   constexpr int kRing = 3;
@@ -222,19 +235,24 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear(LinearArgs a) {
   // (the first one also takes the finished tile; separate arrays, so that the compiler
   // knows which loads a read waits for)
   constexpr int kOut = WR * 32 * WC * 32 / 4, NP0 = kOut > NP ? kOut : NP;
-  __shared__ u32x4_t s_buf0[NP0], s_buf1[NP], s_buf2[NP];
+  __shared__ u32x4_t s_buf0[NP0 * SPLIT], s_buf1[NP * SPLIT], s_buf2[NP * SPLIT];
   typedef std::conditional_t<X8, uint8_t, T> TX;
   const TX* const x = static_cast<const TX*>(a.x);
   const T* const w = static_cast<const T*>(a.w);
   const TileAt t = tile_at<BM, BN>(a.cols);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  // (of a slice of the reduction; its buffers are the slice's part of each)
+  const int slice = SPLIT > 1 ? threadIdx.x / NT : 0, tid = threadIdx.x - slice * NT;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = threadIdx.x & 63;
+  const int ours = __builtin_amdgcn_readfirstlane(slice * NP);
+  const int nk = (a.red + BK * SPLIT - 1) / (BK * SPLIT);    // stages of a slice
+  const int k0 = slice * nk * BK, kend = k0 + nk * BK < a.red ? k0 + nk * BK : a.red;
 
   // What this lane stages of the rows: rows ra0 + NT / PR * i, of each the piece that
   // belongs at its place in LDS.  A row that is not there is read as zeros, at one place all
   // along (step 0).
   constexpr int PRA = TA::PR, PRB = TBr::PR;
   static_assert(NT / PRA % 16 == 0 && NT / PRB % 16 == 0, "a lane's pieces have one place in their rows");
-  const int ra0 = threadIdx.x / PRA, ka = (TA::at(ra0, threadIdx.x % PRA) - ra0 * PRA) * VX;
+  const int ra0 = tid / PRA, ka = (TA::at(ra0, tid % PRA) - ra0 * PRA) * VX;
   const TX* const zero = reinterpret_cast<const TX*>(&g_zeros);
   const TX* pa[PA];
   int step[PA];
@@ -242,13 +260,12 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear(LinearArgs a) {
   for (int i = 0; i < PA; ++i) {
     const int64_t r = t.row0 + ra0 + NT / PRA * i;
     step[i] = r < a.n ? BK : 0;
-    pa[i] = r < a.n ? x + r * a.red + ka : zero;
+    pa[i] = r < a.n ? x + r * a.red + k0 + ka : zero;
   }
-  const int nk = (a.red + BK - 1) / BK;
   // And of the weights, from the stage's own place; columns past the last one are read as
   // others (nothing of them is stored).
-  const int kb = BT ? threadIdx.x / PRB : threadIdx.x / TBk::PR;
-  const int kr = BT ? (TBr::at(kb, threadIdx.x % PRB) - kb * PRB) * VEC : 0;
+  const int kb = BT ? tid / PRB : tid / TBk::PR;
+  const int kr = BT ? (TBr::at(kb, tid % PRB) - kb * PRB) * VEC : 0;
   uint32_t pb[PB];
 #pragma unroll
   for (int i = 0; i < PB; ++i) {
@@ -256,15 +273,16 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear(LinearArgs a) {
       const int n = kb + NT / PRB * i;
       pb[i] = static_cast<uint32_t>(t.n0 + n < a.cols ? n : 0) * a.red + kr;
     } else {
-      const int n = (TBk::at(kb, threadIdx.x % TBk::PR) - kb * TBk::PR) * VEC;
+      const int n = (TBk::at(kb, tid % TBk::PR) - kb * TBk::PR) * VEC;
       pb[i] = static_cast<uint32_t>(kb + NT / TBk::PR * i) * a.cols + (t.n0 + n < a.cols ? n : 0);
     }
   }
   // Stages past the last one are asked for too, as zeros, so that the number of loads
   // behind a stage's own is known.
-  int rk = 0;                                      // the next stage to request
+  int rk = k0;                                     // the next stage to request
   auto request = [&](u32x4_t* buf) {
-    const int left = a.red - rk;                   // of the reduction
+    buf += ours;
+    const int left = kend - rk;                    // of the slice
     const T* const ws = BT ? w + static_cast<int64_t>(t.n0) * a.red + rk
                            : w + static_cast<int64_t>(rk) * a.cols + t.n0;
     if (left >= BK) {
@@ -303,8 +321,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear(LinearArgs a) {
     stage_barrier<(PA + PB) * (kRing - 2)>();
     request(before);
     multiply_stage<T, KB, FM, FN>(
-        acc, [&](int m, int q) { return rows_of(buf, m, q); },
-        [&](int n, int q) { return weights_of(buf + TA::PIECES, BT ? WC * n : n, q); });
+        acc, [&](int m, int q) { return rows_of(buf + ours, m, q); },
+        [&](int n, int q) { return weights_of(buf + ours + TA::PIECES, BT ? WC * n : n, q); });
   };
   request(s_buf0);
   request(s_buf1);
@@ -314,7 +332,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear(LinearArgs a) {
     if (s + 2 < nk) stage(s_buf2, s_buf1);
   }
   stage_barrier<0>();                              // (no load is on its way to s_buf0)
-  finish_tile<TO, X8, BT, BM, BN, WR, WC, NP0 * 16, PAST>(s_buf0, acc, a, t.row0, t.n0);
+  finish_tile<TO, X8, BT, BM, BN, WR, WC, NP0 * SPLIT * 16, PAST, SPLIT>(s_buf0, acc, a, t.row0,
+                                                                        t.n0);
 }
 
 // Rows x weights for any alignment and width: BT false: w is [red][cols] (the forward), BT true:
@@ -395,13 +414,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_any(LinearArgs a) {
   finish_tile<TO, X8, BT, BM, BN, 2, 2, NP * 16, false>(s_buf, acc, a, row0, n0);
 }
 
-// Few rows (one at a time): the weights' bytes, once, and the time to the last of them are all
+// Few fp32 rows (one at a time): the weights' bytes, once, and the time to the last of them are all
 // there is.  A workgroup of 16 waves takes up to 4 rows and 64 bytes of columns, 4 lanes
 // side by side; its 256 slices of the reduction run down the weights' rows on the vector ALU,
 // 8 loads of a slice in flight, and are added over the lanes, then the waves, in order.
 constexpr int kFewThreads = 1024, kFewRows = 4;
-template <typename T, typename TO, bool X8>
+template <typename TO>
 __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
+  typedef float T;
   constexpr int VEC = Row<T>::VEC, R = kFewRows, CL = 4, NC = CL * VEC, KS = kFewThreads / CL;
   constexpr int KC = 2048, UN = 8;                 // of the reduction in LDS; loads in flight
   constexpr int NW = kFewThreads / 64;
@@ -433,11 +453,7 @@ __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
     for (int k = threadIdx.x % (kFewThreads / R); k < kc; k += kFewThreads / R) {
       float v = 0.0f;
       if (src < a.n) {
-        const int64_t at = src * a.red + k0 + k;
-        if constexpr (X8)
-          v = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<const uint8_t*>(a.x)[at], false)[0];
-        else
-          v = Row<T>::get(static_cast<const T*>(a.x)[at]);
+        v = static_cast<const T*>(a.x)[src * a.red + k0 + k];
       }
       s_x[sr][k] = v;
     }
@@ -481,12 +497,80 @@ __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
   float z = 0.0f;
 #pragma unroll
   for (int q = 0; q < NW; ++q) z += s_sum[q][r][threadIdx.x % NC];
-  if (X8) z *= a.x_scale[t.row0 + r];
   if (a.bias) z += a.bias[col];
   if (a.z) static_cast<TO*>(a.z)[at] = Row<TO>::put(z);
   by_act(a.act, [&](auto k) { z = activate<decltype(k)::value>(z); });
   if (a.side) z += Row<TO>::get(static_cast<const TO*>(a.side)[at]);
   static_cast<TO*>(a.y)[at] = Row<TO>::put(z);
+}
+
+// The same for the input gradient, where a row of weights is the reduction: a wave takes two of
+// them, its lanes side by side along them, and adds the lanes up at the end.
+template <typename TO>
+__global__ __launch_bounds__(kThreads) void k_linear_few_back(LinearArgs a) {
+  typedef float T;
+  constexpr int VEC = Row<T>::VEC, R = kFewRows, NC = 2, KC = 2048;
+  __shared__ __attribute__((aligned(16))) float s_x[R][KC];
+  const T *const x = static_cast<const T*>(a.x), *const w = static_cast<const T*>(a.w);
+  const TileAt t = tile_at<R, NC * kThreads / 64>(a.cols);
+  const int lane = threadIdx.x & 63, c0 = t.n0 + static_cast<int>(threadIdx.x >> 6) * NC;
+  float acc[NC][R];
+#pragma unroll
+  for (int n = 0; n < NC; ++n)
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[n][r] = 0.0f;
+  for (int k0 = 0; k0 < a.red; k0 += KC) {
+    const int kc = a.red - k0 < KC ? a.red - k0 : KC;
+    __syncthreads();
+    for (int k = threadIdx.x; k < kc; k += kThreads)
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        s_x[r][k] = t.row0 + r < a.n ? Row<T>::get(x[(t.row0 + r) * a.red + k0 + k]) : 0.0f;
+    __syncthreads();
+#pragma unroll 4
+    for (int k = lane * VEC; k < kc; k += 64 * VEC) {
+      float v[NC][VEC];
+#pragma unroll
+      for (int n = 0; n < NC; ++n)
+        unpack(load_piece(c0 + n < a.cols ? w + static_cast<int64_t>(c0 + n) * a.red + k0 + k
+                                          : reinterpret_cast<const T*>(&g_zeros)), v[n]);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < VEC; e += 4) {
+          const float4 d = *reinterpret_cast<const float4*>(&s_x[r][k + e]);
+#pragma unroll
+          for (int n = 0; n < NC; ++n) {
+            acc[n][r] = fmaf(d.x, v[n][e], acc[n][r]);
+            acc[n][r] = fmaf(d.y, v[n][e + 1], acc[n][r]);
+            acc[n][r] = fmaf(d.z, v[n][e + 2], acc[n][r]);
+            acc[n][r] = fmaf(d.w, v[n][e + 3], acc[n][r]);
+          }
+        }
+    }
+  }
+  float mine = 0.0f;                               // lane r NC + n: row r, column n
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const float v = group_sum<64>(acc[n][r]);
+      mine = lane == r * NC + n ? v : mine;
+    }
+  const int64_t row = t.row0 + lane / NC;
+  const int col = c0 + lane % NC;
+  if (lane >= R * NC || row >= a.n || col >= a.cols) return;
+  const int64_t at = row * a.cols + col;
+  if (a.side) {
+    float z;
+    if (a.side_scale)
+      z = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<const uint8_t*>(a.side)[at], false)[0] *
+          a.side_scale[row];
+    else
+      z = Row<TO>::get(static_cast<const TO*>(a.side)[at]);
+    by_act(a.act, [&](auto k) { mine *= slope<decltype(k)::value>(z); });
+  }
+  static_cast<TO*>(a.y)[at] = Row<TO>::put(mine);
 }
 
 // Weight gradient of a BC x BN tile over a chunk of the rows: dw[c][n] = sum_j x[j][c] dy[j][n],
@@ -876,9 +960,15 @@ int run_tiles(const LinearArgs& a) {
   uint32_t blocks;
   if (!grid_of<BM, BN>(a, NT, &blocks)) return SPCONV_EINVAL;
   if (linear_past(a.n, a.cols, (a.z ? 2 : 1) * static_cast<int>(sizeof(TO))))
-    k_linear<T, TO, X8, BT, BM, BN, WR, WC, true><<<blocks, NT, 0, a.st>>>(a);
+    k_linear<T, TO, X8, BT, BM, BN, WR, WC, true, 1><<<blocks, NT, 0, a.st>>>(a);
   else
-    k_linear<T, TO, X8, BT, BM, BN, WR, WC, false><<<blocks, NT, 0, a.st>>>(a);
+    k_linear<T, TO, X8, BT, BM, BN, WR, WC, false, 1><<<blocks, NT, 0, a.st>>>(a);
+  return launched();
+}
+template <typename T, typename TO, bool X8, bool BT> int run_split(const LinearArgs& a) {
+  uint32_t blocks;
+  if (!grid_of<32, 32>(a, 64 * kSplit, &blocks)) return SPCONV_EINVAL;
+  k_linear<T, TO, X8, BT, 32, 32, 1, 1, false, kSplit><<<blocks, 64 * kSplit, 0, a.st>>>(a);
   return launched();
 }
 // The kernel that linear_plan says.
@@ -887,11 +977,16 @@ template <typename T, typename TO, bool X8, bool BT> int by_size(const LinearArg
                      whole_rows<T>(a.w, BT ? a.red : a.cols);
   const LinearPlan p = linear_plan(sizeof(T) == 4 ? SPCONV_F32 : SPCONV_BF16, BT, a.n, a.red,
                                    a.cols, whole);
-  if constexpr (!BT) {
+  if constexpr (sizeof(T) == 4) {
     if (p.kernel == LinearKernel::kFew) {
       uint32_t blocks;
-      if (!grid_of<kFewRows, 4 * Row<T>::VEC>(a, kFewThreads, &blocks)) return SPCONV_EINVAL;
-      k_linear_few<T, TO, X8><<<blocks, kFewThreads, 0, a.st>>>(a);
+      if constexpr (BT) {
+        if (!grid_of<kFewRows, 8>(a, kThreads, &blocks)) return SPCONV_EINVAL;
+        k_linear_few_back<TO><<<blocks, kThreads, 0, a.st>>>(a);
+      } else {
+        if (!grid_of<kFewRows, 16>(a, kFewThreads, &blocks)) return SPCONV_EINVAL;
+        k_linear_few<TO><<<blocks, kFewThreads, 0, a.st>>>(a);
+      }
       return launched();
     }
   }
@@ -901,6 +996,7 @@ template <typename T, typename TO, bool X8, bool BT> int by_size(const LinearArg
     if (p.tile == 256) return run_tiles<T, TO, X8, BT, 256, 128, 4, 2>(a);
   }
   if (p.tile == 128) return run_tiles<T, TO, X8, BT, 128, 128, 2, 2>(a);
+  if (p.kernel == LinearKernel::kSplit) return run_split<T, TO, X8, BT>(a);
   return run_tiles<T, TO, X8, BT, 64, 64, 2, 2>(a);
 }
 

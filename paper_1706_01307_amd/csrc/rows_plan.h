@@ -165,28 +165,34 @@ inline int dw_sum_runs(const DwPlan& p, int E, int64_t values) {
 // ---------------------------------------------------------------------------
 // Dense products (rows_linear.hip)
 // ---------------------------------------------------------------------------
-enum class LinearKernel { kFew, kAny, kTiles };
+enum class LinearKernel { kFew, kAny, kTiles, kSplit };
 struct LinearPlan {
   LinearKernel kernel;
   int tile;                    // kAny: 64, 128 squared; kTiles: too, 256: 256 rows x 128 columns
 };
 
-// k_linear_few as for grouped products; k_linear_any where pieces may be cut or unaligned;
-// else k_linear in tiles of 256 x 128 (not fp32), 128 x 128 or 64 x 64, the largest that
-// two (fp32: three) workgroups a compute unit fill.  (us in tiles of 64, 128 and 256, bf16:
-// 348,208 x 256 -> 1024 642, 329 and 317; 65,536 x 512 -> 512 73, 54 and 49; 16,384 x 2048
-// -> 2048 255, 159 and 145, of 256 x 256 146; 8,000 x 512 -> 512 12, 12 and 15.  fp32, 65,536
-// x 1024 -> 1024: 1,259 and 1,072.)
+// k_linear_few for up to 16 fp32 rows (us of it and of kSplit, 1 row 2048 -> 512: 5.6 and 14.5, its
+// gradient 3.3 and 5.7; 16 rows 512 -> 512: 4.7 and 5.9; bf16 the other way round, 1 row 2048 ->
+// 2048: 8.1 and 6.3); k_linear_any where pieces may be cut or unaligned; else k_linear, in
+// tiles of 256 x 128 (not fp32), 128 x 128 or 64 x 64, the largest that two (fp32: three)
+// workgroups a compute unit fill, or where tiles of 32 x 32 are so few that a compute unit
+// has one of them (fp32: two), those with the reduction in eight slices (kSplit).  (us in tiles of
+// 64, 128 and 256, bf16: 348,208 x 256 -> 1024 642, 329 and 317; 65,536 x 512 -> 512 73, 54 and 49;
+// 16,384 x 2048 -> 2048 255, 159 and 145, of 256 x 256 146; 8,000 x 512 -> 512 12, 12 and 15.  fp32,
+// 65,536 x 1024 -> 1024: 1,259 and 1,072.  Of 64 and sliced of 32, bf16: 64 x 2048 -> 512 14.1 and
+// 6.5; 64 x 256 -> 256 4.4 and 4.0; 1,000 x 512 -> 512 5.9 and 8.1; fp32: 200 x 2048 -> 512 47 and
+// 17, 500 x 512 -> 512 14.3 and 6.4, 2,000 x 512 -> 512 15.5 and 21.7.)
 inline LinearPlan linear_plan(int in_dt, bool backward, int64_t n, int red, int cols, bool whole) {
   const bool f32 = in_dt == SPCONV_F32;
-  if (!backward && few_is_faster(f32, n, 1, red, cols)) return {LinearKernel::kFew, 0};
-  const int64_t c128 = (cols + 127) / 128, c64 = (cols + 63) / 64;
+  if (f32 && n <= 16 && (backward ? red : cols) % 4 == 0) return {LinearKernel::kFew, 0};
+  const int64_t c128 = (cols + 127) / 128, c64 = (cols + 63) / 64, c32 = (cols + 31) / 32;
   const int64_t t128 = (n + 127) / 128 * c128, t256 = (n + 255) / 256 * c128;
   const bool waste = f32 && c64 % 2 && c64 > 2 && c64 < 16;   // of the last 128 columns
   const bool small = cols <= 64 || t128 < (f32 ? 768 : 512) || waste;
   if (!whole) return {LinearKernel::kAny, small ? 64 : 128};
-  if (small) return {LinearKernel::kTiles, 64};
-  return {LinearKernel::kTiles, !f32 && t256 >= 512 ? 256 : 128};
+  if (!small) return {LinearKernel::kTiles, !f32 && t256 >= 512 ? 256 : 128};
+  if (red > 64 && (n + 31) / 32 * c32 <= (f32 ? 512 : 256)) return {LinearKernel::kSplit, 32};
+  return {LinearKernel::kTiles, 64};
 }
 // Whether finished rows are stored past the caches: 32 MB of them are in no L2 anyway when
 // somebody reads them, and push out the operands meanwhile (348,208 x 256 -> 1024 with the

@@ -149,7 +149,7 @@ def test_products_reach_every_kernel(plans):
         vec = 4 if dt == "f32" else 8
         whole = red % (16 if dt == "e4m3" else vec) == 0 and (red if backward else cols) % vec == 0
         plans.plan_linear(0 if dt == "f32" else 1, backward, n, red, cols, whole, out)
-        got = (("few", "any", "tiles")[out[0]], out[1])
+        got = (("few", "any", "tiles", "split")[out[0]], out[1])
         assert got == want, (dt, backward, n, red, cols)
         seen.add((dt, backward) + got)
     tiles = {"f32": (64, 128), "bf16": (64, 128, 256), "e4m3": (64, 128, 256)}
@@ -159,7 +159,8 @@ def test_products_reach_every_kernel(plans):
                 assert (dt, backward, "any", t) in seen
             for t in tiles[dt]:
                 assert (dt, backward, "tiles", t) in seen
-        assert (dt, 0, "few", 0) in seen
+            assert (dt, backward, "split", 32) in seen
+    assert ("f32", 0, "few", 0) in seen and ("f32", 1, "few", 0) in seen
 
 
 def test_weight_gradient_chunks_cover_the_rows(plans):
