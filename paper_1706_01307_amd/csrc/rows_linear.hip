@@ -724,11 +724,33 @@ __device__ __forceinline__ u32x4_t widen_half(uint32_t lo, uint32_t hi) {
   return v;
 }
 
+// The largest finite |dy| of a piece of eight (as bf16, by their bits).
+__device__ __forceinline__ float top_of(u32x4_t u) {
+  typedef uint16_t s2 __attribute__((ext_vector_type(2)));
+  s2 t = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const s2 m = __builtin_bit_cast(s2, u[i] & 0x7fff7fffu);
+    t = __builtin_elementwise_max(t, m);
+  }
+  const uint32_t most = t[0] > t[1] ? t[0] : t[1];
+  if (most < 0x7f80u) return __uint_as_float(most << 16);
+  float v[8], top = 0.0f;                          // (an infinity or NaN among them)
+  unpack(u, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float m = __uint_as_float(magnitude(v[i]));
+    top = m < INFINITY && m > top ? m : top;
+  }
+  return top;
+}
+
 // The same through registers: cut or unaligned pieces, and rows in 8 bits (X8), whose scale goes
 // to the other operand.  v = scale * dy enters as two f16 numbers, v 2^-e and what it leaves:
 // 22 bits.  e follows the largest finite |v| that the workgroup has met (it is told of a
 // stage's in front of the barrier that the stage waits at anyway; the sums so far are moved
-// when it grows): what is 2^17 below it loses bits, but nothing over 2^-40 of it.
+// when it grows): what is 2^17 below it loses bits, but nothing over 2^-40 of it.  (A dy that is
+// not finite leaves its column NaN.)
 // WHOLE: rows are of whole pieces.
 template <typename T, bool X8, int BC, int BN, int WR, int WC, int KB, bool WHOLE>
 __global__ __launch_bounds__(64 * WR * WC, WR * WC / 2) void k_linear_dw(LinearWeight a) {
@@ -789,23 +811,17 @@ __global__ __launch_bounds__(64 * WR * WC, WR * WC / 2) void k_linear_dw(LinearW
   int turn = 0;
   if (t.begin < t.end) request(t.begin);
   for (int64_t j0 = t.begin; j0 < t.end; j0 += BK) {
-    float v[X8 ? PY : 1][VEC];
     if constexpr (X8) {
       float top = 0.0f;
 #pragma unroll
       for (int i = 0; i < PY; ++i) {
-        unpack(ry[i], v[i]);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          if (bias) sum[e] += v[i][e];
-          v[i][e] *= rs[i];
-          const float m = __uint_as_float(magnitude(v[i][e]));
-          top = m < INFINITY && m > top ? m : top;
-        }
+        const float m = top_of(ry[i]) * rs[i];
+        top = m < INFINITY && m > top ? m : top;
       }
       top = group_reduce<64>(top, [](float p, float q) { return q > p ? q : p; });
       if (lane == 0) s_top[turn][wave] = top;
-    } else if (bias) {
+    }
+    if (bias) {
 #pragma unroll
       for (int i = 0; i < PY; ++i) {
         float u[VEC];
@@ -815,6 +831,7 @@ __global__ __launch_bounds__(64 * WR * WC, WR * WC / 2) void k_linear_dw(LinearW
       }
     }
     __syncthreads();
+    float unit = 1.0f;
     if constexpr (X8) {
       float top = s_top[turn][0];
 #pragma unroll
@@ -833,6 +850,7 @@ __global__ __launch_bounds__(64 * WR * WC, WR * WC / 2) void k_linear_dw(LinearW
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[n][m][i] *= f;
       }
+      unit = __uint_as_float(static_cast<uint32_t>(127 - power) << 23);
     }
 #pragma unroll
     for (int i = 0; i < PX; ++i)
@@ -843,16 +861,17 @@ __global__ __launch_bounds__(64 * WR * WC, WR * WC / 2) void k_linear_dw(LinearW
       if constexpr (X8) {
         typedef _Float16 h2 __attribute__((ext_vector_type(2)));
         typedef float f2 __attribute__((ext_vector_type(2)));
-        const float unit = __uint_as_float(static_cast<uint32_t>(127 - power) << 23);
+        // (kept finite beside a row of zeros, whose products are too small for `power`)
+        float by = rs[i] * unit;
+        by = by > 0x1p127f && rs[i] < INFINITY ? 0x1p127f : by;
+        float v[VEC];
+        unpack(ry[i], v);
         u32x4_t hi, lo;
 #pragma unroll
         for (int e = 0; e < VEC; e += 2) {
-          const f2 u = {v[i][e] * unit, v[i][e + 1] * unit};
+          const f2 u = {v[e] * by, v[e + 1] * by};
           const h2 up = __builtin_convertvector(u, h2);
-          const f2 back = __builtin_convertvector(up, f2);
-          // (an infinity or NaN is all in the upper part)
-          const f2 rest = {magnitude(u[0]) < 0x7f800000u ? u[0] - back[0] : 0.0f,
-                           magnitude(u[1]) < 0x7f800000u ? u[1] - back[1] : 0.0f};
+          const f2 rest = {u[0] - static_cast<float>(up[0]), u[1] - static_cast<float>(up[1])};
           hi[e / 2] = __builtin_bit_cast(uint32_t, up);
           lo[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, h2));
         }
