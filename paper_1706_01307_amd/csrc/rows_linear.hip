@@ -753,7 +753,7 @@ __device__ __forceinline__ float top_of(u32x4_t u) {
 // not finite leaves its column NaN.)
 // WHOLE: rows are of whole pieces.
 template <typename T, bool X8, int BC, int BN, int WR, int WC, int KB, bool WHOLE>
-__global__ __launch_bounds__(64 * WR * WC, WR * WC / 2) void k_linear_dw(LinearWeight a) {
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
   typedef KTile<T, BC, KB> TX;
   typedef KTile<T, BN, KB> TY;
   constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = 64 * WR * WC;
@@ -1025,8 +1025,8 @@ template <typename T, bool X8> void run_dw(const LinearWeight& a, const DwPlan& 
   const bool whole = wx && whole_rows<T>(a.dy, a.C_out);
   if constexpr (X8) {
     if (p.tile == 256) {
-      if (whole) k_linear_dw<T, X8, 256, 128, 4, 2, 64, true><<<blocks, 512, 0, a.st>>>(a);
-      else k_linear_dw<T, X8, 256, 128, 4, 2, 64, false><<<blocks, 512, 0, a.st>>>(a);
+      if (whole) k_linear_dw<T, X8, 256, 128, 2, 2, 64, true><<<blocks, 256, 0, a.st>>>(a);
+      else k_linear_dw<T, X8, 256, 128, 2, 2, 64, false><<<blocks, 256, 0, a.st>>>(a);
     } else if (p.tile == 128) {
       if (whole) k_linear_dw<T, X8, 128, 128, 2, 2, 128, true><<<blocks, 256, 0, a.st>>>(a);
       else k_linear_dw<T, X8, 128, 128, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
