@@ -55,6 +55,15 @@ __device__ __forceinline__ uint2 load8_left(const uint8_t* p, int64_t left) {
   return u;
 }
 
+// A barrier for what the waves exchange through LDS alone: loads and stores of memory go on
+// (__syncthreads waits for them: in the end of every part of a finished tile for its stores).
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // The finished tile of a workgroup of WR x WC waves, FM x FN blocks each, leaves through LDS
 // (BYTES of it) as fp32 rows, a row block of every wave and FNP column blocks at a time:
 // everything behind the product is done on fp32 and rounded once, whole rows go to memory, and
@@ -114,7 +123,7 @@ __device__ __forceinline__ void finish_tile(u32x4_t* lds,
           }
         }
       }
-      __syncthreads();
+      lds_barrier();
 #pragma unroll
       for (int f = 0; f < FNP; ++f)
 #pragma unroll
@@ -126,7 +135,7 @@ __device__ __forceinline__ void finish_tile(u32x4_t* lds,
           for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(acc[np + f][m][4 * q + i]);
           lds[slice * PART + out_at<float, CW>(wrow * 32 + (lane & 31), c / 4)] = v;
         }
-      __syncthreads();
+      lds_barrier();
 #pragma unroll
       for (int i = 0; i < NPC; ++i) {
         if (!live[i]) continue;
