@@ -29,6 +29,7 @@ struct LinearArgs {
   int64_t n;
   int red, cols;               // reduction, output columns
   hipStream_t st;
+  int touch = 0;               // touch_rows
 };
 
 // Eight e4m3 values as bf16, exactly.
@@ -223,6 +224,31 @@ template <int R, int BK> struct RTile8 {
   };
 };
 
+// Workgroups of a die that run together.
+template <int BM> constexpr int kResident = BM == 256 ? 64 : BM == 128 ? 96 : 160;
+// The first 4 bytes of every line of this workgroup's share of the rows that will be read `ahead`
+// tiles on by this die, into its L2 (and, unread, into LDS at `room`, 256 bytes a wave): the
+// column tiles of one row tile run side by side and would all wait for its rows, three stages of
+// them at a time.  To be waited for before the workgroup ends.
+template <int BM, int BN, int NT>
+__device__ __forceinline__ void touch_rows(const void* x, int64_t row_bytes, int64_t n, int cols,
+                                           int ahead, u32x4_t* room) {
+  const int64_t total = gridDim.x, local = blockIdx.x / 8, die = blockIdx.x % 8;
+  if (local + ahead >= total / 8 + (die < total % 8)) return;
+  const int ncol = (cols + BN - 1) / BN;
+  const int64_t id = die_order(blockIdx.x, total) + ahead, row0 = id / ncol * BM;
+  const int64_t bytes = (n - row0 < BM ? n - row0 : BM) * row_bytes;
+  // (whole lines from the tile's first byte on, and so whole words inside it)
+  const int64_t share = (bytes + 128ll * ncol - 1) / (128ll * ncol) * 128, first = id % ncol * share;
+  const int64_t end = first + share < bytes ? first + share : bytes;
+  typedef __attribute__((address_space(3))) void lds_void;
+  typedef __attribute__((address_space(1))) const void global_void;
+  const char* const p = static_cast<const char*>(x) + row0 * row_bytes;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t at = first + threadIdx.x * 128; at < end; at += NT * 128)
+    __builtin_amdgcn_global_load_lds((global_void*)(p + at), (lds_void*)(room + 16 * wave), 4, 0, 0);
+}
+
 // Rows x weights of whole aligned 16-byte pieces: BT false: w is [red][cols] (the forward), BT
 // true: w is [cols][red] (the input gradient).  A workgroup of WR x WC waves takes a tile of BM
 // rows by BN columns, in stages of BK of the reduction through a ring of LDS buffers: all but
@@ -246,6 +272,7 @@ __global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a
   constexpr int kOut = WR * 32 * WC * 32 / 4, NP0 = kOut > NP ? kOut : NP;
   __shared__ u32x4_t s_buf0[NP0 * SPLIT], s_buf1[NP * SPLIT], s_buf2[NP * SPLIT];
   typedef std::conditional_t<X8, uint8_t, T> TX;
+  static_assert(NP >= 16 * (NT / 64), "room for what touch_rows brings");
   const TX* const x = static_cast<const TX*>(a.x);
   const T* const w = static_cast<const T*>(a.w);
   const TileAt t = tile_at<BM, BN>(a.cols);
@@ -341,8 +368,12 @@ __global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a
     if (s + 2 < nk) stage(s_buf2, s_buf1);
   }
   stage_barrier<0>();                              // (no load is on its way to s_buf0)
+  if (a.touch && SPLIT == 1)
+    touch_rows<BM, BN, NT>(a.x, static_cast<int64_t>(a.red) * sizeof(TX), a.n, a.cols,
+                           kResident<BM>, s_buf1);
   finish_tile<TO, X8, BT, BM, BN, WR, WC, NP0 * SPLIT * 16, PAST, SPLIT>(s_buf0, acc, a, t.row0,
                                                                         t.n0);
+  if (a.touch && SPLIT == 1) stage_barrier<0>();
 }
 
 // Rows x weights for any alignment and width: BT false: w is [red][cols] (the forward), BT true:
@@ -983,9 +1014,13 @@ int run_any(const LinearArgs& a) {
   return launched();
 }
 template <typename T, typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC>
-int run_tiles(const LinearArgs& a) {
+int run_tiles(LinearArgs a) {
   constexpr int NT = 64 * WR * WC;
   uint32_t blocks;
+  // (348,208 x 256 -> 1024, its rows in no cache: 531 us, and 468 touched; 1024 -> 256, whose rows the
+  // L2 cannot hold: 261, and 308)
+  const double row = static_cast<double>(a.red) * (X8 ? 1 : sizeof(T));
+  a.touch = BM * row * kResident<BM> / ((a.cols + BN - 1) / BN) <= 4.3e6;
   if (!grid_of<BM, BN>(a, NT, &blocks)) return SPCONV_EINVAL;
   if (linear_past(a.n, a.cols, (a.z ? 2 : 1) * static_cast<int>(sizeof(TO))))
     k_linear<T, TO, X8, BT, BM, BN, WR, WC, true, 1><<<blocks, NT, 0, a.st>>>(a);
