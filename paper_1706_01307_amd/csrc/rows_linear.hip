@@ -253,6 +253,16 @@ __device__ __forceinline__ void touch_rows(const void* x, int64_t row_bytes, int
 // true: w is [cols][red] (the input gradient).  A workgroup of WR x WC waves takes a tile of BM
 // rows by BN columns, in stages of BK of the reduction through a ring of LDS buffers: all but
 // one stage are on their way while that one is multiplied, one barrier a stage.
+// SPLIT: so many groups of WR x WC waves, each with a slice of the reduction and buffers of its own:
+// where there are few tiles the stages of one follow each other in time, and nothing else
+// runs on the card (64 x 2048 -> 512 bf16: 14.1 us, in eight slices 6.5).
+// Of the cycles a compute unit has work, the matrix cores are busy in 45 % and the LDS in 25 (16,384 x
+// 2048 -> 2048 bf16: 145 us, 950 TFLOP/s, a large library product 1,147), or in 17 and 14 (348,208 x
+// 256 -> 1024 with the activation's input, 393 us with its rows in the last-level cache and 461
+// without, 4.1 and 3.5 TB/s): eight stages a tile, whose first ones wait for memory.  (256 x
+// 128 by four waves instead of eight, 128 x 256, 256 x 256: 5 to 10 % slower; a ring of four: an
+// LDS' worth of workgroups fewer, 20 %; the residual asked for a tile ahead: registers for
+// one workgroup a compute unit instead of two, 25 %.)
 template <typename T, typename TO, bool X8, bool BT, int BM, int BN, int WR, int WC, bool PAST,
           int SPLIT>
 __global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a) {
@@ -379,7 +389,8 @@ __global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a
 // Rows x weights for any alignment and width: BT false: w is [red][cols] (the forward), BT true:
 // w is [cols][red] (the input gradient).  Through registers, 128 x 128 or 64 x 64 by four
 // waves in 2 x 2, stages of 128 bytes of the reduction.  X8: rows in 8 bits, widened on their
-// way to LDS.
+// way to LDS.  Bound by the time from a stage's loads to its products, one stage at a time (60,000 x
+// 145 -> 301 bf16: 33 us, 158 TFLOP/s).
 template <typename T, typename TO, bool X8, bool BT, int BM, int BN>
 __global__ __launch_bounds__(kThreads, 2) void k_linear_any(LinearArgs a) {
   constexpr int KB = 128;
@@ -458,6 +469,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_linear_any(LinearArgs a) {
 // there is.  A workgroup of 16 waves takes up to 4 rows and 64 bytes of columns, 4 lanes
 // side by side; its 256 slices of the reduction run down the weights' rows on the vector ALU,
 // 8 loads of a slice in flight, and are added over the lanes, then the waves, in order.
+// (1 row 2048 -> 512: 5.6 us, in sliced tiles on the matrix cores 14.5: they take 64 cycles
+// for 2 of the reduction however few rows there are.)
 constexpr int kFewThreads = 1024, kFewRows = 4;
 template <typename TO>
 __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
@@ -545,7 +558,8 @@ __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
 }
 
 // The same for the input gradient, where a row of weights is the reduction: a wave takes two of
-// them, its lanes side by side along them, and adds the lanes up at the end.
+// them, its lanes side by side along them, and adds the lanes up at the end.  (2048 -> 512: 3.3 us;
+// sliced tiles 5.7.)
 template <typename TO>
 __global__ __launch_bounds__(kThreads) void k_linear_few_back(LinearArgs a) {
   typedef float T;
@@ -661,6 +675,8 @@ __device__ __forceinline__ void store_sums(const f32x16 (&acc)[FN][FC], const Li
 }
 
 // Whole aligned 16-byte pieces: straight to LDS through a ring of three stages of 64 bytes.
+// Bound as k_linear: matrix cores 37 % of the busy cycles, LDS 18 (348,208 x 256 x 1024 bf16: 260 us and
+// 11 for the chunks' sums, 680 TFLOP/s; 902,504 x 64 x 64: 54, 4.3 TB/s).
 template <typename T, int BC, int BN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw_ring(LinearWeight a) {
   constexpr int KB = 64, kRing = 3;
@@ -792,6 +808,9 @@ __device__ __forceinline__ float top_of(u32x4_t u) {
 // when it grows): what is 2^17 below it loses bits, but nothing over 2^-40 of it.  (A dy that is
 // not finite leaves its column NaN.)
 // WHOLE: rows are of whole pieces.
+// 16,384 x 2048 x 2048 of 8 bits: 321 us and 14 for the sums, 860 TFLOP/s of the two products it is:
+// matrix cores 48 % of the busy cycles, vector ALU 44, LDS 28 (eight waves of 64 x 64 instead of
+// four of 128 x 64: 376; stages of 64 rows: 409).
 template <typename T, bool X8, int BC, int BN, int WR, int WC, int KB, bool WHOLE>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
   typedef KTile<T, BC, KB> TX;

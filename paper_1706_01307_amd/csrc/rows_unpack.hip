@@ -2,7 +2,9 @@
 // whose input is at hand in either form.
 //
 // Elementwise and bound by memory.  A group of lanes takes a row at a time, so that its
-// scale is one load and no element asks which row it is in.
+// scale is one load and no element asks which row it is in; as many lanes as a row has
+// pieces, to a power of two (348,208 bf16 rows of 256, half of the lanes idle: 81 us for the
+// GELU of them, 42 so, 6.3 TB/s; its derivative times dy 140, and 80, 5.6).
 #include "rows_act.h"
 
 namespace spc {
