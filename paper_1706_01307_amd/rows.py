@@ -84,9 +84,11 @@ def _on_stream(fn):
 def _given(t, name, dtypes, shape, dims=0):
     """t, contiguous, if it is a cuda tensor on the current device, of one of the
     dtypes and of the shape (or, with shape None, of that many dimensions)."""
-    if (type(t) is not torch.Tensor and not isinstance(t, torch.Tensor)) or not t.is_cuda:
+    if type(t) is not torch.Tensor and not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a cuda tensor")
     if t.get_device() != _device():
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a cuda tensor")
         raise ValueError(f"{name} is on {t.device}, not on the current device")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} has dtype {t.dtype}, needs one of {tuple(dtypes)}")
@@ -101,7 +103,7 @@ def _result(out, shape, dtype, like):
     if out is None:
         if like.dtype == dtype and like.shape == shape:
             return torch.empty_like(like)          # (the quicker of the two)
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     if (not isinstance(out, torch.Tensor) or out.device != like.device or out.dtype != dtype or
             out.shape != shape or not out.is_contiguous()):
         raise ValueError(f"out must be a contiguous {dtype} tensor of shape {tuple(shape)} on "
@@ -131,8 +133,7 @@ def _workspace(name, like, *sizes):
     st = _lib_fn[name](*sizes, ctypes.byref(n))
     if st:
         _lib.check(st, name)
-    return (torch.empty(n.value, dtype=torch.uint8, device=like.device) if n.value else None,
-            n.value)
+    return like.new_empty(n.value, dtype=torch.uint8) if n.value else None, n.value
 
 
 # ---------------------------------------------------------------------------
@@ -438,8 +439,8 @@ def _act(act):
 
 
 def _new8(n, C, like):
-    return Rows8(torch.empty((n, C), dtype=torch.float8_e4m3fn, device=like.device),
-                 torch.empty(n, dtype=torch.float32, device=like.device))
+    return Rows8(like.new_empty((n, C), dtype=torch.float8_e4m3fn),
+                 like.new_empty(n, dtype=torch.float32))
 
 
 @_on_stream
@@ -504,7 +505,7 @@ def rms_norm_forward(x, gamma=None, eps=1e-6, *, residual=None, packed=False, st
     else:
         y = _result(out, (n, C), x.dtype, x)
         yp, ys, code = _ptr(y), None, _CODE[x.dtype]
-    rstd = torch.empty(n, dtype=torch.float32, device=x.device) if stats else None
+    rstd = x.new_empty(n, dtype=torch.float32) if stats else None
     _call("spconv_rms_norm_forward", _CODE[x.dtype], _ptr(x), _ptr(residual), _ptr(gamma),
           float(eps), None if residual is None else _ptr(h), code, yp, ys, _ptr(rstd), n, _i32(C))
     return y, h, rstd
@@ -528,7 +529,7 @@ def rms_norm_backward(dy, h, rstd, gamma=None, *, dh=None, params=None, out=None
     dg = ws = None
     nbytes = 0
     if params:
-        dg = torch.empty(C, dtype=torch.float32, device=dy.device)
+        dg = dy.new_empty(C, dtype=torch.float32)
         ws, nbytes = _workspace("spconv_rms_norm_backward_workspace", dy, n, _i32(C))
     _call("spconv_rms_norm_backward", _CODE[dy.dtype], _ptr(dy), code, _ptr(h), _ptr(scale),
           _ptr(rstd), _ptr(gamma), _ptr(dh), _ptr(dx), _ptr(dg), n, _i32(C), _ptr(ws), nbytes)
@@ -558,7 +559,7 @@ def linear_forward(x, w, bias=None, *, act=None, residual=None, pre=False, out_d
     if residual is not None:
         residual = _given(residual, "residual", (out_dtype,), (n, co))
     y = _result(out, (n, co), out_dtype, x)
-    z = torch.empty((n, co), dtype=out_dtype, device=x.device) if pre else None
+    z = torch.empty_like(y) if pre else None
     _call("spconv_linear_forward", code, _ptr(x), _ptr(scale), _ptr(w), _ptr(bias), _act(act),
           _ptr(residual), _CODE[out_dtype], _ptr(y), _ptr(z), n, _i32(ci), _i32(co))
     return y, z
@@ -595,8 +596,8 @@ def linear_backward_weight(x, dy, *, bias=True):
     if dy.shape[0] != n:
         raise ValueError(f"x has {n} rows, dy {dy.shape[0]}")
     ws, nbytes = _workspace("spconv_linear_backward_weight_workspace", x, code, n, ci, co)
-    dw = torch.empty((ci, co), dtype=torch.float32, device=x.device)
-    db = torch.empty(co, dtype=torch.float32, device=x.device) if bias else None
+    dw = dy.new_empty((ci, co), dtype=torch.float32)
+    db = dy.new_empty(co, dtype=torch.float32) if bias else None
     _call("spconv_linear_backward_weight", code, _ptr(x), _ptr(scale), _ptr(dy), _ptr(dw), _ptr(db),
           n, ci, co, _ptr(ws), nbytes)
     return dw, db
@@ -623,11 +624,12 @@ def route_scores_forward(logits, k, *, score="sigmoid", bias=None, groups=1, top
     n, E = logits.shape
     if bias is not None:
         bias = _given(bias, "bias", _FLOAT, (E,))
-    dev, k = logits.device, int(k)
+    k = int(k)
     ws, nbytes = _workspace("spconv_route_workspace", logits, n, _i32(E), _i32(k))
-    ints = functools.partial(torch.empty, dtype=torch.int32, device=dev)
-    r = Routing(ints((n, k)), torch.empty((n, k), dtype=torch.float32, device=dev), ints(E + 1),
-                ints(n * k), ints((n, k)))
+    ints = functools.partial(logits.new_empty, dtype=torch.int32)
+    experts = ints((n, k))
+    r = Routing(experts, logits.new_empty((n, k), dtype=torch.float32), ints(E + 1), ints(n * k),
+                torch.empty_like(experts))
     _call("spconv_route_scores_forward", _CODE[logits.dtype], _ptr(logits), _ptr(bias), n, E, k,
           _score(score), _i32(int(groups)), _i32(int(top_groups)), 1 if normalize else 0,
           float(scale), _ptr(r.experts), _ptr(r.weights), _ptr(r.offsets), _ptr(r.rows),
