@@ -111,6 +111,7 @@ def test_scores_next_to_one_another(groups, top_groups):
     _check(x, torch.zeros(E), k, groups, top_groups)
     _check(x, torch.randint(0, 3, (E,), generator=g) * 2.0 ** -24, k, groups, top_groups)
     _check(torch.zeros(n, E), None, k, groups, top_groups)
+    _check(torch.zeros(3, 256), None, k, groups, top_groups)
     # scores that 64 bits, but not 32, tell apart; and that neither does
     _check(torch.randn(n, E, generator=g) * 0.5 + 20, torch.zeros(E), k, groups, top_groups)
     _check(torch.randn(n, E, generator=g) + 60, None, k, groups, top_groups, ("sigmoid",))
