@@ -386,6 +386,180 @@ __global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a
   if (a.touch && SPLIT == 1) stage_barrier<0>();
 }
 
+// bf16 rows, a reduction of at most 32 NK, nothing read behind it: a workgroup keeps the weights
+// of its 256 columns in registers (four waves of 64 columns, twice, for 32 rows each) while rows
+// stream past it, 64 at a time through a ring of three LDS buffers.  One barrier a tile is all, and
+// its stores are on their way while the next ones are computed: sums leave rounded, wave by wave,
+// through LDS of the wave's own, in whole lines of 64 columns.  (Waves of 32 columns, whose stores
+// are half lines, take twice the time at 262,144 x 128 -> 272 with the activation's input: 193
+// us, and 89.)  A wave's loads and stores are counted together, in their order: behind the loads of
+// the tile that is needed next lie the next tile's and, where all of a wave's columns are there,
+// the stores of the tile before.  Bound by memory: 348,208 x 256 -> 1024 220 us (4.1 TB/s), with
+// the activation's input 345 (4.6 TB/s), 1024 <- 256 backwards 212 (4.2 TB/s); k_linear 334, 411
+// and 295.
+template <bool BT, int NK, bool PAST>
+__global__ __launch_bounds__(512, NK == 2 ? 4 : 2) void k_linear_short(LinearArgs a, int strips) {
+  typedef bf16_t T;
+  typedef Mma<T> M;
+  typedef RTile<T, 64, 64> TA;                     // 64 rows, 32 of the reduction
+  constexpr int BM = 64, FN = 2, VEC = 8, SUB = TA::PIECES, NP = SUB * NK, PA = NP / 512;
+  static_assert(PA * 512 == NP, "whole pieces a lane");
+  __shared__ u32x4_t s_buf0[NP], s_buf1[NP], s_buf2[NP], s_out[8][32 * 64 / 8];
+  __shared__ __attribute__((aligned(16))) float s_bias[BT ? 4 : 256];
+  const T *const x = static_cast<const T*>(a.x), *const w = static_cast<const T*>(a.w);
+  const int groups = (a.cols + 255) / 256;
+  const int64_t id = die_order(blockIdx.x, gridDim.x);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, h = lane >> 5;
+  const int c0 = static_cast<int>(id % groups) * 256 + wave % 4 * 64, r0 = wave / 4 * 32;
+  const int64_t tiles = (a.n + BM - 1) / BM;
+  const T* const zero = reinterpret_cast<const T*>(&g_zeros);
+
+  // This lane's pieces of a tile: row ra of sub-tiles j0, j0 + 2, ..., the piece whose place in LDS
+  // is the lane's.
+  constexpr int PRA = TA::PR;
+  const int ra = threadIdx.x % SUB / PRA, ka = (TA::at(ra, threadIdx.x % PRA) - ra * PRA) * VEC;
+  const int j0 = threadIdx.x / SUB;
+  auto request = [&](int64_t t, u32x4_t* buf) {
+    const int64_t r = t * BM + ra;
+    const T* const p = x + r * a.red + ka;
+#pragma unroll
+    for (int i = 0; i < PA; ++i) {
+      const int k = (j0 + 2 * i) * 32;
+      load_to_lds(t < tiles && r < a.n && k + ka < a.red ? p + k : zero, buf + 512 * i + 64 * wave);
+    }
+  };
+  int64_t t = id / groups;
+  request(t, s_buf0);
+  request(t + strips, s_buf1);
+
+  // Its weights, 64 of the reduction at a time through s_out.
+  typename M::Frag fw[FN][2 * NK];
+  {
+    typedef RTile<T, 256, 128> TR;                 // BT: rows of weights are columns of y
+    typedef KTile<T, 256, 128> TK;
+    static_assert(TR::PIECES == 2048 && TK::PIECES == 2048 && NK % 2 == 0, "s_out");
+    const int base = c0 - wave % 4 * 64;
+    u32x4_t raw[2 * NK];
+#pragma unroll
+    for (int i = 0; i < 2 * NK; ++i) {
+      const int piece = threadIdx.x + 512 * (i % 4);
+      if constexpr (BT) {
+        const int n = base + piece / 8, k = i / 4 * 64 + piece % 8 * 8;
+        raw[i] = load_left<T, true>(w + static_cast<int64_t>(n) * a.red + k, n < a.cols ? a.red - k : 0);
+      } else {
+        const int k = i / 4 * 64 + piece / 32, n = base + piece % 32 * 8;
+        raw[i] = load_left<T, true>(w + static_cast<int64_t>(k) * a.cols + n, k < a.red ? a.cols - n : 0);
+      }
+    }
+    if (!BT && threadIdx.x < 256) {
+      const int n = base + threadIdx.x;
+      s_bias[threadIdx.x] = a.bias && n < a.cols ? a.bias[n] : 0.0f;
+    }
+    const auto weights_of = [&] {
+      if constexpr (BT) return typename TR::Reader(wave % 4 * 64, lane);
+      else return typename TK::template Reader<32, FN>(wave % 4 * 64, lane);
+    }();
+#pragma unroll
+    for (int part = 0; part < NK / 2; ++part) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int piece = threadIdx.x + 512 * i;
+        s_out[0][BT ? TR::at(piece / 8, piece % 8) : TK::at(piece / 32, piece % 32)] = raw[4 * part + i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int b = 0; b < FN; ++b) fw[b][4 * part + s] = weights_of(s_out[0], b, s);
+    }
+  }
+  // It stores rows lane / 8 + 8 j of a wave's 32, eight columns.  In LDS pieces are permuted by
+  // pairs of rows, their halves exchanged from row 16 on: writes of half a piece by 32 rows and
+  // reads of whole ones meet every bank once.
+  const int col = c0 + lane % 8 * 8, left = a.cols - col;
+  constexpr int kStores = 4;                       // of a tile, twice as many with z
+  const bool whole = c0 + 64 <= a.cols;            // (one for the wave)
+  u32x4_t* const out = s_out[wave];
+  const int put = (lane & 31) * 128 + (h ^ (lane >> 4 & 1)) * 8, turn = lane >> 1 & 7;
+  const typename TA::Reader rows_of(r0, lane);
+
+  auto tile = [&](const u32x4_t* buf, u32x4_t* before) {
+    if (!whole) stage_barrier<PA>();
+    else if (a.z) stage_barrier<PA + 2 * kStores>();
+    else stage_barrier<PA + kStores>();
+    request(t + 2 * strips, before);
+    asm volatile("" ::: "memory");                 // (the tile's stores come behind these loads)
+    f32x16 acc[FN];
+#pragma unroll
+    for (int b = 0; b < FN; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[b][i] = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 2 * NK; ++q) {
+      const typename M::Frag fa = rows_of(buf + q / 2 * SUB, 0, q % 2);
+#pragma unroll
+      for (int b = 0; b < FN; ++b) acc[b] = M::mma(fw[b][q], fa, acc[b]);
+    }
+    auto leave = [&](void* y) {
+#pragma unroll
+      for (int b = 0; b < FN; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = acc[b][4 * q + i];
+          const u32x4_t u = pack(v);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint2 half = {u[2 * i], u[2 * i + 1]};
+            *reinterpret_cast<uint2*>(reinterpret_cast<char*>(out) + put + (4 * b + q + i ^ turn) * 16) = half;
+          }
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int lr = lane / 8 + 8 * j;
+        const int64_t r = t * BM + r0 + lr;
+        if (r >= a.n || left <= 0) continue;
+        u32x4_t u = out[lr * 8 + (lane % 8 ^ (lr >> 1 & 7))];
+        if (j >= 2) u = u32x4_t{u[2], u[3], u[0], u[1]};
+        store_left<T, PAST>(static_cast<T*>(y) + r * a.cols + col, u, left);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    };
+    if constexpr (!BT) {
+      // (a lane's sums are of row lane % 32, columns 32 b + 8 q + 4 h + i)
+#pragma unroll
+      for (int b = 0; b < FN; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float4 v = *reinterpret_cast<const float4*>(s_bias + wave % 4 * 64 + 32 * b + 8 * q + 4 * h);
+          acc[b][4 * q] += v.x, acc[b][4 * q + 1] += v.y, acc[b][4 * q + 2] += v.z, acc[b][4 * q + 3] += v.w;
+        }
+      if (a.z) leave(a.z);
+      by_act(a.act, [&](auto k) {
+#pragma unroll
+        for (int b = 0; b < FN; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[b][i] = activate<decltype(k)::value>(acc[b][i]);
+      });
+    }
+    leave(a.y);
+    t += strips;
+  };
+  // (Before the first tile nothing was stored.)
+  stage_barrier<0>();
+  while (t < tiles) {
+    tile(s_buf0, s_buf2);
+    if (t < tiles) tile(s_buf1, s_buf0);
+    if (t < tiles) tile(s_buf2, s_buf1);
+  }
+  stage_barrier<0>();                              // (no load to LDS outlives the workgroup)
+}
+
 // Rows x weights for any alignment and width: BT false: w is [red][cols] (the forward), BT true:
 // w is [cols][red] (the input gradient).  Through registers, 128 x 128 or 64 x 64 by four
 // waves in 2 x 2, stages of 128 bytes of the reduction.  X8: rows in 8 bits, widened on their
@@ -1053,7 +1227,18 @@ template <typename T, typename TO, bool X8, bool BT> int run_split(const LinearA
   k_linear<T, TO, X8, BT, 32, 32, 1, 1, false, kSplit><<<blocks, 64 * kSplit, 0, a.st>>>(a);
   return launched();
 }
-// The kernel that linear_plan says.
+template <bool BT, int NK> int run_short(const LinearArgs& a) {
+  // as many workgroups as fit
+  const int groups = (a.cols + 255) / 256, slots = (NK == 2 ? 512 : 256) / groups;
+  const int64_t tiles = (a.n + 63) / 64, most = slots > 1 ? slots : 1;
+  const int strips = static_cast<int>(tiles < most ? tiles : most);
+  if (linear_past(a.n, a.cols, a.z ? 4 : 2))
+    k_linear_short<BT, NK, true><<<strips * groups, 512, 0, a.st>>>(a, strips);
+  else
+    k_linear_short<BT, NK, false><<<strips * groups, 512, 0, a.st>>>(a, strips);
+  return launched();
+}
+// The kernel that linear_plan says, or k_linear_short where linear_short has a place for it.
 template <typename T, typename TO, bool X8, bool BT> int by_size(const LinearArgs& a) {
   const bool whole = (X8 ? a.red % 16 == 0 && aligned_to(a.x, 16) : whole_rows<T>(a.x, a.red)) &&
                      whole_rows<T>(a.w, BT ? a.red : a.cols);
@@ -1075,6 +1260,14 @@ template <typename T, typename TO, bool X8, bool BT> int by_size(const LinearArg
   if (p.kernel == LinearKernel::kAny)
     return p.tile == 64 ? run_any<T, TO, X8, BT, 64, 64>(a) : run_any<T, TO, X8, BT, 128, 128>(a);
   if constexpr (sizeof(T) == 2) {
+    if constexpr (!X8 && sizeof(TO) == 2) {
+      switch (whole && !a.side ? linear_short(a.n, a.red, a.cols) : 0) {
+        case 2: return run_short<BT, 2>(a);
+        case 4: return run_short<BT, 4>(a);
+        case 6: return run_short<BT, 6>(a);
+        case 8: return run_short<BT, 8>(a);
+      }
+    }
     if (p.tile == 256) return run_tiles<T, TO, X8, BT, 256, 128, 4, 2>(a);
   }
   if (p.tile == 128) return run_tiles<T, TO, X8, BT, 128, 128, 2, 2>(a);

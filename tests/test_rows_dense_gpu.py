@@ -21,7 +21,7 @@ torch = pytest.importorskip("torch")
 
 import paper_1706_01307_amd as spc  # noqa: E402
 from tests import rows_dense_ref as ref  # noqa: E402
-from tests.linear_variants import PRODUCTS, WEIGHTS  # noqa: E402
+from tests.linear_variants import PRODUCTS, SHORT, WEIGHTS  # noqa: E402
 from tests.rows_ref import BF16, U  # noqa: E402
 from tests.test_rows_gpu import DT, _close, _dev, _f64, _gen, _gpu, _shifted  # noqa: E402,F401
 
@@ -244,6 +244,44 @@ def _operands(dt, n, ci, co, seed):
     x = x * torch.exp(r(n, 1))
     q, s = ref.packed(x)
     return _rows8(q, s), ref.stands_for(q, s), w, b, d
+
+
+@pytest.mark.parametrize("backward,n,red,cols,stages", SHORT)
+def test_products_that_keep_their_weights(backward, n, red, cols, stages):
+    """Sums as in test_products; rows in front of y and behind it stay as they are, a row of infinities
+    and NaN reaches no other."""
+    ci, co = (cols, red) if backward else (red, cols)
+    x, _, w, b, d = _operands("bf16", n, ci, co, n + red)
+    rows = (_gen(n)(n, co, dtype=d) if backward else x.cpu()).clone()
+    bad = n // 2
+    rows[bad, 0], rows[bad, red - 1] = float("inf"), float("nan")
+    good = torch.arange(n) != bad
+    clean = rows.clone()
+    clean[bad] = 0
+    frame = torch.full((n + 16, cols), 7.0, dtype=torch.bfloat16, device="cuda")
+    y = frame[8:n + 8]
+    wt = _f64(w).t() if backward else _f64(w)
+    z, mag = _f64(clean) @ wt, _f64(clean).abs() @ wt.abs()
+    if backward:
+        assert spc.linear_backward_data(rows.cuda(), w.cuda(), out=y) is y
+        _off(y[good], z[good], (red + 34) * U * mag[good], "dx")
+        assert bool(torch.isnan(y[bad]).any())
+    else:
+        for bias in (None, b):
+            v, m = (z, mag) if bias is None else (z + _f64(bias), mag + _f64(bias).abs())
+            ez = (red + 34) * U * m
+            for act in ACTS:
+                for keep in (False, True):
+                    got, pre = spc.linear_forward(rows.cuda(), w.cuda(), None if bias is None else bias.cuda(),
+                                                  act=act, pre=keep, out=y)
+                    a = ref.act(v, act)
+                    assert got is y and (pre is not None) == keep
+                    _off(y[good], a[good], (1.13 * ez + 8 * U * v.abs() + 2 * U * a.abs())[good], ("y", act))
+                    if keep:
+                        _off(pre[good], v[good], ez[good], "z")
+                if n > 40000 and act == "relu":
+                    break
+    assert bool((frame[:8] == 7).all()) and bool((frame[n + 8:] == 7).all())
 
 
 @pytest.mark.parametrize("dt,backward,n,red,cols,want", PRODUCTS)
