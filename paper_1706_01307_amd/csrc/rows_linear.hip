@@ -386,7 +386,7 @@ __global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a
   if (a.touch && SPLIT == 1) stage_barrier<0>();
 }
 
-// bf16 rows, a reduction of at most 32 NK, nothing read behind it: a workgroup keeps the weights
+// bf16 rows, a reduction of at most 32 NK, nothing read behind it but a residual: a workgroup keeps the weights
 // of its 256 columns in registers (four waves of 64 columns, twice, for 32 rows each) while rows
 // stream past it, 64 at a time through a ring of three LDS buffers.  One barrier a tile is all, and
 // its stores are on their way while the next ones are computed: sums leave rounded, wave by wave,
@@ -394,11 +394,13 @@ __global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a
 // are half lines, take twice the time at 262,144 x 128 -> 272 with the activation's input: 193
 // us, and 89.)  A wave's loads and stores are counted together, in their order: behind the loads of
 // the tile that is needed next lie the next tile's and, where all of a wave's columns are there,
-// the stores of the tile before.  Bound by memory: 348,208 x 256 -> 1024 220 us (4.1 TB/s), with
-// the activation's input 345 (4.6 TB/s), 1024 <- 256 backwards 212 (4.2 TB/s); k_linear 334, 411
-// and 295.
-template <bool BT, int NK, bool PAST>
-__global__ __launch_bounds__(512, NK == 2 ? 4 : 2) void k_linear_short(LinearArgs a, int strips) {
+// the stores and the next residual's loads of the tile before.  (An activation's input read in the
+// same way, for the input gradient, takes more registers than there are: 348,208 x 256 -> 1024 616
+// us, k_linear 539.)  Bound by memory: 348,208 x 256 -> 1024 220 us (4.1 TB/s), with
+// the activation's input 345 (4.6 TB/s), a residual 352 (4.6 TB/s), 1024 <- 256 backwards 212
+// (4.2 TB/s); k_linear 334, 411, 488 and 295.
+template <bool BT, int NK, bool PAST, bool RES>
+__global__ __launch_bounds__(512, NK == 2 && !RES ? 4 : 2) void k_linear_short(LinearArgs a, int strips) {
   typedef bf16_t T;
   typedef Mma<T> M;
   typedef RTile<T, 64, 64> TA;                     // 64 rows, 32 of the reduction
@@ -479,15 +481,28 @@ __global__ __launch_bounds__(512, NK == 2 ? 4 : 2) void k_linear_short(LinearArg
   // reads of whole ones meet every bank once.
   const int col = c0 + lane % 8 * 8, left = a.cols - col;
   constexpr int kStores = 4;                       // of a tile, twice as many with z
+  constexpr int kSide = RES ? 4 : 0;               // loads of the residual
   const bool whole = c0 + 64 <= a.cols;            // (one for the wave)
   u32x4_t* const out = s_out[wave];
   const int put = (lane & 31) * 128 + (h ^ (lane >> 4 & 1)) * 8, turn = lane >> 1 & 7;
   const typename TA::Reader rows_of(r0, lane);
 
+  // The next tile's residual, in the places that are stored.
+  u32x4_t res[4];
+  auto res_of = [&](int64_t t) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t r = t * BM + r0 + lane / 8 + 8 * j;
+      const T* const p = static_cast<const T*>(a.side) + r * a.cols + col;
+      res[j] = load_left<T, true>(p, r < a.n ? left : 0);
+    }
+  };
+  if constexpr (RES) res_of(t);
+
   auto tile = [&](const u32x4_t* buf, u32x4_t* before) {
     if (!whole) stage_barrier<PA>();
-    else if (a.z) stage_barrier<PA + 2 * kStores>();
-    else stage_barrier<PA + kStores>();
+    else if (a.z) stage_barrier<PA + 2 * kStores + kSide>();
+    else stage_barrier<PA + kStores + kSide>();
     request(t + 2 * strips, before);
     asm volatile("" ::: "memory");                 // (the tile's stores come behind these loads)
     f32x16 acc[FN];
@@ -513,7 +528,7 @@ __global__ __launch_bounds__(512, NK == 2 ? 4 : 2) void k_linear_short(LinearArg
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const uint2 half = {u[2 * i], u[2 * i + 1]};
-            *reinterpret_cast<uint2*>(reinterpret_cast<char*>(out) + put + (4 * b + q + i ^ turn) * 16) = half;
+            *reinterpret_cast<uint2*>(reinterpret_cast<char*>(out) + put + ((4 * b + q + i) ^ turn) * 16) = half;
           }
         }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -546,6 +561,31 @@ __global__ __launch_bounds__(512, NK == 2 ? 4 : 2) void k_linear_short(LinearArg
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[b][i] = activate<decltype(k)::value>(acc[b][i]);
       });
+    }
+    if constexpr (RES) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int lr = lane / 8 + 8 * j;
+        u32x4_t u = res[j];
+        if (j >= 2) u = u32x4_t{u[2], u[3], u[0], u[1]};
+        out[lr * 8 + (lane % 8 ^ (lr >> 1 & 7))] = u;
+      }
+      res_of(t + strips);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int b = 0; b < FN; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint2 u = *reinterpret_cast<const uint2*>(reinterpret_cast<const char*>(out) + put +
+                                                          ((4 * b + q) ^ turn) * 16);
+          acc[b][4 * q] += __uint_as_float(u.x << 16);
+          acc[b][4 * q + 1] += __uint_as_float(u.x & 0xffff0000u);
+          acc[b][4 * q + 2] += __uint_as_float(u.y << 16);
+          acc[b][4 * q + 3] += __uint_as_float(u.y & 0xffff0000u);
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
     leave(a.y);
     t += strips;
@@ -1227,16 +1267,21 @@ template <typename T, typename TO, bool X8, bool BT> int run_split(const LinearA
   k_linear<T, TO, X8, BT, 32, 32, 1, 1, false, kSplit><<<blocks, 64 * kSplit, 0, a.st>>>(a);
   return launched();
 }
-template <bool BT, int NK> int run_short(const LinearArgs& a) {
+template <bool BT, int NK, bool RES> int run_short_of(const LinearArgs& a) {
   // as many workgroups as fit
-  const int groups = (a.cols + 255) / 256, slots = (NK == 2 ? 512 : 256) / groups;
+  const int groups = (a.cols + 255) / 256, slots = (NK == 2 && !RES ? 512 : 256) / groups;
   const int64_t tiles = (a.n + 63) / 64, most = slots > 1 ? slots : 1;
   const int strips = static_cast<int>(tiles < most ? tiles : most);
   if (linear_past(a.n, a.cols, a.z ? 4 : 2))
-    k_linear_short<BT, NK, true><<<strips * groups, 512, 0, a.st>>>(a, strips);
+    k_linear_short<BT, NK, true, RES><<<strips * groups, 512, 0, a.st>>>(a, strips);
   else
-    k_linear_short<BT, NK, false><<<strips * groups, 512, 0, a.st>>>(a, strips);
+    k_linear_short<BT, NK, false, RES><<<strips * groups, 512, 0, a.st>>>(a, strips);
   return launched();
+}
+template <bool BT, int NK> int run_short(const LinearArgs& a) {
+  if constexpr (!BT)
+    if (a.side) return run_short_of<BT, NK, true>(a);
+  return run_short_of<BT, NK, false>(a);
 }
 // The kernel that linear_plan says, or k_linear_short where linear_short has a place for it.
 template <typename T, typename TO, bool X8, bool BT> int by_size(const LinearArgs& a) {
@@ -1261,7 +1306,7 @@ template <typename T, typename TO, bool X8, bool BT> int by_size(const LinearArg
     return p.tile == 64 ? run_any<T, TO, X8, BT, 64, 64>(a) : run_any<T, TO, X8, BT, 128, 128>(a);
   if constexpr (sizeof(T) == 2) {
     if constexpr (!X8 && sizeof(TO) == 2) {
-      switch (whole && !a.side ? linear_short(a.n, a.red, a.cols) : 0) {
+      switch (whole && !(BT && a.side) ? linear_short(a.n, a.red, a.cols, a.side) : 0) {
         case 2: return run_short<BT, 2>(a);
         case 4: return run_short<BT, 4>(a);
         case 6: return run_short<BT, 6>(a);

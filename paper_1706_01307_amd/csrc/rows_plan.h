@@ -195,13 +195,15 @@ inline LinearPlan linear_plan(int in_dt, bool backward, int64_t n, int red, int 
   return {LinearKernel::kTiles, 64};
 }
 // Stages of 32 of the reduction that k_linear_short keeps weights of (bf16 rows of whole pieces in
-// and out, nothing read behind the product), or 0: from one tile of 64 rows a compute unit on,
-// for more columns than a tile of k_linear has.  (us in tiles and so, 348,208 x 256 -> 1024 334
-// and 220, with the activation's input 411 and 345; 16,384 x 256 -> 256 8.7 and 8.5; 65,536 x
-// 96 -> 512 24 and 16; 262,144 x 160 -> 136 64 and 35; 900,000 x 64 -> 128 with the
-// activation's input 98 and 124.)
-inline int linear_short(int64_t n, int red, int cols) {
-  if (red > 256 || cols <= 128 || (n + 63) / 64 * ((cols + 255) / 256) < 256) return 0;
+// and out, nothing read behind the product but a residual), or 0: from one tile of 64 rows a
+// compute unit on, eight with a residual, for more columns than a tile of k_linear has.  (us in
+// tiles and so, 348,208 x 256 -> 1024 334 and 220, with the activation's input 411 and 345;
+// 16,384 x 256 -> 256 8.7 and 8.5; 65,536 x 96 -> 512 24 and 16; 262,144 x 160 -> 136 64 and 35;
+// 900,000 x 64 -> 128 with the activation's input 98 and 124; with a residual 65,536 x 256 -> 256
+// 21.6 and 22.4, 65,536 x 256 -> 328 48 and 36.)
+inline int linear_short(int64_t n, int red, int cols, bool residual) {
+  const int64_t tiles = (n + 63) / 64 * ((cols + 255) / 256);
+  if (red > 256 || cols <= 128 || tiles < (residual ? 2048 : 256)) return 0;
   return (red + 63) / 64 * 2;
 }
 // Whether finished rows are stored past the caches: 32 MB of them are in no L2 anyway when

@@ -10,7 +10,9 @@ void plan_linear(int in_dt, int backward, int64_t n, int red, int cols, int whol
   out[1] = p.tile;
 }
 
-int plan_linear_short(int64_t n, int red, int cols) { return spc::linear_short(n, red, cols); }
+int plan_linear_short(int64_t n, int red, int cols, int residual) {
+  return spc::linear_short(n, red, cols, residual);
+}
 
 void plan_linear_weight(int dt, int64_t n, int C_in, int C_out, int64_t* out) {
   const spc::DwPlan p = spc::linear_dw_plan(dt, n, C_in, C_out);

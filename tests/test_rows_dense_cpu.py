@@ -137,7 +137,7 @@ def plans(tmp_path_factory):
     lib = ctypes.CDLL(so)
     i, i64, p = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p
     lib.plan_linear.argtypes = [i, i, i64, i, i, i, p]
-    lib.plan_linear_short.argtypes = [i64, i, i]
+    lib.plan_linear_short.argtypes = [i64, i, i, i]
     lib.plan_linear_weight.argtypes = [i, i64, i, i, p]
     return lib
 
@@ -167,13 +167,15 @@ def test_products_reach_every_kernel(plans):
 def test_products_that_keep_their_weights(plans):
     """The sizes of SHORT reach every number of stages both ways; small, wide and long ones stay out."""
     from tests.linear_variants import SHORT
-    for backward, n, red, cols, stages in SHORT:
-        assert plans.plan_linear_short(n, red, cols) == stages, (n, red, cols)
+    for backward, n, red, cols, stages, residual in SHORT:
+        assert plans.plan_linear_short(n, red, cols, 0) == stages, (n, red, cols)
+        assert plans.plan_linear_short(n, red, cols, 1) == (stages if residual else 0), (n, red, cols)
         assert (stages - 2) * 32 < red <= stages * 32
-    assert {s[::4] for s in SHORT} == {(b, k) for b in (0, 1) for k in (2, 4, 6, 8)}
+    assert {(s[0], s[4]) for s in SHORT} == {(b, k) for b in (0, 1) for k in (2, 4, 6, 8)}
+    assert {s[4] for s in SHORT if not s[0] and s[5]} == {2, 4, 6, 8}
     for n, red, cols in ((16320, 64, 256), (70000, 257, 256), (70000, 64, 128), (1, 8, 256), (0, 8, 256)):
-        assert plans.plan_linear_short(n, red, cols) == 0
-    assert plans.plan_linear_short(2 ** 31 - 1, 256, 2 ** 23) == 8
+        assert plans.plan_linear_short(n, red, cols, 0) == 0
+    assert plans.plan_linear_short(2 ** 31 - 1, 256, 2 ** 23, 1) == 8
 
 
 def test_weight_gradient_chunks_cover_the_rows(plans):

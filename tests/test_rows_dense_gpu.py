@@ -246,8 +246,8 @@ def _operands(dt, n, ci, co, seed):
     return _rows8(q, s), ref.stands_for(q, s), w, b, d
 
 
-@pytest.mark.parametrize("backward,n,red,cols,stages", SHORT)
-def test_products_that_keep_their_weights(backward, n, red, cols, stages):
+@pytest.mark.parametrize("backward,n,red,cols,stages,residual", SHORT)
+def test_products_that_keep_their_weights(backward, n, red, cols, stages, residual):
     """Sums as in test_products; rows in front of y and behind it stay as they are, a row of infinities
     and NaN reaches no other."""
     ci, co = (cols, red) if backward else (red, cols)
@@ -258,29 +258,32 @@ def test_products_that_keep_their_weights(backward, n, red, cols, stages):
     good = torch.arange(n) != bad
     clean = rows.clone()
     clean[bad] = 0
+    rows, w_, b_ = rows.cuda(), w.cuda(), b.cuda()
     frame = torch.full((n + 16, cols), 7.0, dtype=torch.bfloat16, device="cuda")
     y = frame[8:n + 8]
     wt = _f64(w).t() if backward else _f64(w)
     z, mag = _f64(clean) @ wt, _f64(clean).abs() @ wt.abs()
     if backward:
-        assert spc.linear_backward_data(rows.cuda(), w.cuda(), out=y) is y
+        assert spc.linear_backward_data(rows, w_, out=y) is y
         _off(y[good], z[good], (red + 34) * U * mag[good], "dx")
         assert bool(torch.isnan(y[bad]).any())
     else:
-        for bias in (None, b):
+        big = n * cols > 3e6
+        res = _gen(n + 1)(n, cols, dtype=d) if residual else None
+        calls = [(a, keep, bias) for a in ACTS for keep in (False, True) for bias in (None, b)]
+        for act, keep, bias in [(None, False, b), ("gelu", True, b), ("silu", False, None)] if big else calls:
             v, m = (z, mag) if bias is None else (z + _f64(bias), mag + _f64(bias).abs())
-            ez = (red + 34) * U * m
-            for act in ACTS:
-                for keep in (False, True):
-                    got, pre = spc.linear_forward(rows.cuda(), w.cuda(), None if bias is None else bias.cuda(),
-                                                  act=act, pre=keep, out=y)
-                    a = ref.act(v, act)
-                    assert got is y and (pre is not None) == keep
-                    _off(y[good], a[good], (1.13 * ez + 8 * U * v.abs() + 2 * U * a.abs())[good], ("y", act))
-                    if keep:
-                        _off(pre[good], v[good], ez[good], "z")
-                if n > 40000 and act == "relu":
-                    break
+            ez, a = (red + 34) * U * m, ref.act(v, act)
+            for r in (None, res) if residual else (None,):
+                s = a if r is None else a + _f64(r)
+                if r is not None and keep:               # in place of the residual
+                    y.copy_(r)
+                got, pre = spc.linear_forward(rows, w_, None if bias is None else b_, act=act, pre=keep,
+                                              residual=None if r is None else y if keep else r.cuda(), out=y)
+                assert got is y and (pre is not None) == keep
+                _off(y[good], s[good], (1.13 * ez + 8 * U * v.abs() + 2 * U * s.abs())[good], ("y", act))
+                if keep:
+                    _off(pre[good], v[good], ez[good], "z")
     assert bool((frame[:8] == 7).all()) and bool((frame[n + 8:] == 7).all())
 
 
