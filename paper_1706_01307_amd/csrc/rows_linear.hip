@@ -86,7 +86,8 @@ __device__ __forceinline__ void finish_tile(u32x4_t* lds,
   constexpr int PART = RW * CW / 4;                // pieces of a slice's part
   static_assert(PART * SPLIT * 16 <= BYTES, "a part of the finished tile fits");
   static_assert(NT % PR == 0 && NPC * NT >= RW * PR, "a lane's pieces lie in the same columns");
-  const int slice = threadIdx.x / (64 * WR * WC), wave = (threadIdx.x >> 6) % (WR * WC), lane = threadIdx.x & 63, h = lane >> 5;
+  const int slice = threadIdx.x / (64 * WR * WC), wave = (threadIdx.x >> 6) % (WR * WC);
+  const int lane = threadIdx.x & 63, h = lane >> 5;
   const int wrow = wave / WC, wcol = wave % WC, piece = threadIdx.x % PR;
   const bool side8 = BT && a.side_scale;
 #pragma unroll
@@ -257,9 +258,10 @@ __device__ __forceinline__ void touch_rows(const void* x, int64_t row_bytes, int
 // where there are few tiles the stages of one follow each other in time, and nothing else
 // runs on the card (64 x 2048 -> 512 bf16: 14.1 us, in eight slices 6.5).
 // Of the cycles a compute unit has work, the matrix cores are busy in 45 % and the LDS in 25 (16,384 x
-// 2048 -> 2048 bf16: 145 us, 950 TFLOP/s, a large library product 1,147), or in 17 and 14 (348,208 x
-// 256 -> 1024 with the activation's input, 393 us with its rows in the last-level cache and 461
-// without, 4.1 and 3.5 TB/s): eight stages a tile, whose first ones wait for memory.  (256 x
+// 2048 -> 2048 bf16: 145 us, 950 TFLOP/s, a large library product 1,147), or in 19 and 17 (348,208 x
+// 256 -> 1024 with the activation's input, 411 us with its rows in the last-level cache and 461
+// without, 3.9 and 3.5 TB/s: eight stages a tile, whose first ones wait for memory; what
+// k_linear_short does not take, 8-bit and fp32 rows or sums, runs so).  (256 x
 // 128 by four waves instead of eight, 128 x 256, 256 x 256: 5 to 10 % slower; a ring of four: an
 // LDS' worth of workgroups fewer, 20 %; the residual asked for a tile ahead: registers for
 // one workgroup a compute unit instead of two, 25 %.)
@@ -398,7 +400,8 @@ __global__ __launch_bounds__(64 * WR * WC * SPLIT, 2) void k_linear(LinearArgs a
 // same way, for the input gradient, takes more registers than there are: 348,208 x 256 -> 1024 616
 // us, k_linear 539.)  Bound by memory: 348,208 x 256 -> 1024 220 us (4.1 TB/s), with
 // the activation's input 345 (4.6 TB/s), a residual 352 (4.6 TB/s), 1024 <- 256 backwards 212
-// (4.2 TB/s); k_linear 334, 411, 488 and 295.
+// (4.2 TB/s); k_linear 334, 411, 488 and 295.  Matrix cores and LDS are busy in 23 % of the cycles
+// each, the vector ALU (activating) in 40.
 template <bool BT, int NK, bool PAST, bool RES>
 __global__ __launch_bounds__(512, NK == 2 && !RES ? 4 : 2) void k_linear_short(LinearArgs a, int strips) {
   typedef bf16_t T;

@@ -9,7 +9,7 @@
 // the errors of both sides, that row is chosen again from 64-bit scores.
 //
 // 348,208 fp32 rows to 8 of 64 experts from 4 of 8 groups: 96 us, and 17 + 5 for the pairs'
-// order, where the bytes alone would take 27; k_scores is bound by the vector ALU (77 % of the
+// order, where the bytes alone would take 27; k_scores is bound by the vector ALU (75 % of the
 // cycles it has work): nine searches of 16 scores a lane, then the groups, the scores and the
 // rows' weights.  The gradient takes 43 us.
 #include <cmath>
