@@ -1323,36 +1323,34 @@ template <typename T, typename TO, bool X8, bool BT> int by_size(const LinearArg
   return run_tiles<T, TO, X8, BT, 64, 64, 2, 2>(a);
 }
 
-template <typename T, bool X8> void run_dw(const LinearWeight& a, const DwPlan& p) {
+// The kernel of exactly the plan's tile (its workgroups are counted for that one): the ring for
+// whole aligned pieces of bf16 and fp32, else k_linear_dw.  (bf16 in cut pieces, us in tiles of up
+// to 256 and of up to 128: 100,000 x 1001 x 1001 651 and 923, 348,208 x 255 x 1023 696 and 1,030,
+// 100,000 x 131 x 300 72 and 77, 485,480 x 174 x 96 133 and 124, 60,000 x 203 x 201 58 and 45.)
+template <typename T, bool X8, int BC, int BN, int WR, int KB>
+void run_dw_tile(const LinearWeight& a, const DwPlan& p) {
   const uint32_t blocks = static_cast<uint32_t>(p.jobs * p.tiles);
   const bool wx = X8 ? a.C_in % 8 == 0 : whole_rows<T>(a.x, a.C_in);
   const bool whole = wx && whole_rows<T>(a.dy, a.C_out);
-  if constexpr (X8) {
-    if (p.tile == 256) {
-      if (whole) k_linear_dw<T, X8, 256, 128, 2, 2, 64, true><<<blocks, 256, 0, a.st>>>(a);
-      else k_linear_dw<T, X8, 256, 128, 2, 2, 64, false><<<blocks, 256, 0, a.st>>>(a);
-    } else if (p.tile == 128) {
-      if (whole) k_linear_dw<T, X8, 128, 128, 2, 2, 128, true><<<blocks, 256, 0, a.st>>>(a);
-      else k_linear_dw<T, X8, 128, 128, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
-    } else {
-      if (whole) k_linear_dw<T, X8, 64, 64, 2, 2, 128, true><<<blocks, 256, 0, a.st>>>(a);
-      else k_linear_dw<T, X8, 64, 64, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
-    }
-  } else {
-    if constexpr (sizeof(T) == 2) {
-      if (whole && p.tile == 256) {
-        k_linear_dw_ring<T, 256, 128, 4, 2><<<blocks, 512, 0, a.st>>>(a);
-        return;
+  if (!whole)
+    k_linear_dw<T, X8, BC, BN, 2, 2, KB, false><<<blocks, 256, 0, a.st>>>(a);
+  else if constexpr (X8)
+    k_linear_dw<T, X8, BC, BN, 2, 2, KB, true><<<blocks, 256, 0, a.st>>>(a);
+  else
+    k_linear_dw_ring<T, BC, BN, WR, 2><<<blocks, 128 * WR, 0, a.st>>>(a);
+}
+template <typename T, bool X8> int run_dw(const LinearWeight& a, const DwPlan& p) {
+  switch (p.tile) {
+    case 64: run_dw_tile<T, X8, 64, 64, 2, 128>(a, p); break;
+    case 128: run_dw_tile<T, X8, 128, 128, 2, 128>(a, p); break;
+    case 256:
+      if constexpr (sizeof(T) == 2) {
+        run_dw_tile<T, X8, 256, 128, 4, 64>(a, p);
+        break;
       }
-    }
-    if (p.tile == 128) {
-      if (whole) k_linear_dw_ring<T, 128, 128, 2, 2><<<blocks, 256, 0, a.st>>>(a);
-      else k_linear_dw<T, false, 128, 128, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
-    } else {
-      if (whole) k_linear_dw_ring<T, 64, 64, 2, 2><<<blocks, 256, 0, a.st>>>(a);
-      else k_linear_dw<T, false, 64, 64, 2, 2, 128, false><<<blocks, 256, 0, a.st>>>(a);
-    }
+    default: return SPCONV_EINVAL;
   }
+  return launched();
 }
 
 bool linear_sizes_ok(int64_t n, int C_in, int C_out) {
@@ -1439,9 +1437,10 @@ extern "C" int spconv_linear_backward_weight(int x_dt, const void* x, const floa
     a.dw = static_cast<float*>(workspace);
     a.db = db ? a.dw + plan.jobs * per : nullptr;
   }
-  if (x_dt == SPCONV_E4M3) run_dw<bf16_t, true>(a, plan);
-  else if (x_dt == SPCONV_BF16) run_dw<bf16_t, false>(a, plan);
-  else run_dw<float, false>(a, plan);
+  const int status = x_dt == SPCONV_E4M3   ? run_dw<bf16_t, true>(a, plan)
+                     : x_dt == SPCONV_BF16 ? run_dw<bf16_t, false>(a, plan)
+                                           : run_dw<float, false>(a, plan);
+  if (status != SPCONV_OK) return status;
   if (plan.jobs > 1) {
     const int64_t values = (per + 3) / 4 * 4 + (db ? C_out : 0);
     if (dw_sum_runs(plan, 1, values) == 8)
