@@ -127,10 +127,17 @@ __device__ __forceinline__ float worth_of(uint32_t o1, uint32_t o2) {
   const float w = value_of(o1 > kNone ? o1 : kNone);
   return o2 > kNone ? w + value_of(o2) : w;
 }
+// What a worth's roundings go with: the magnitudes of its terms, which may cancel in the sum.
+__device__ __forceinline__ float size_of(uint32_t o1, uint32_t o2) {
+  const float w = o1 > kNone ? fabsf(value_of(o1)) : 0.0f;
+  return o2 > kNone ? w + fabsf(value_of(o2)) : w;
+}
 
 // The groups of a row that stay, by fp32 scores: o, the orders of a lane's NV * VEC biased scores,
 // become 0 where their group goes.  Returns whether the gap between the last group that stays and
-// the best that goes is within `near` and the roundings of the sums.  s_v: E words.
+// the best that goes is within `near` and the roundings of the worths (half a unit of each biased
+// score and of their sum: kUnit of their magnitudes is twice that), or a sum is beyond fp32.  s_v: E
+// words.
 // Where a group is of whole pieces of 2^i lanes, its two best are found in registers, piece by
 // piece and then over those lanes; else by reading its scores from s_v.
 template <int LPR, int NV, int VEC>
@@ -140,11 +147,13 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
   const auto col = [&](int i) { return (lane + LPR * (i / VEC)) * VEC + i % VEC; };
   const auto either = [](uint32_t p, uint32_t q) { return p | q; };
   float low = INFINITY, high = -INFINITY;
-  bool odd = false;                                // (NaN among them)
-  auto note = [&](float worth, bool in) {
-    odd |= worth != worth;
-    if (in) low = worth < low ? worth : low;
-    else high = worth > high ? worth : high;
+  bool odd = false;                                // (NaN, infinities and sums past fp32)
+  // (the least that a group that stays can be worth, the most that one that goes can)
+  auto note = [&](float worth, float size, bool in) {
+    odd |= !(size < INFINITY);
+    const float least = worth - kUnit * size, most = worth + kUnit * size;
+    if (in) low = least < low ? least : low;
+    else high = most > high ? most : high;
   };
   if (per % VEC == 0 && (span & (span - 1)) == 0 && span <= LPR) {
     uint32_t o1[NV], o2[NV];
@@ -186,7 +195,7 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const bool in = rank[j] < a.top_groups && ow[j] > kNone;
-      if (g[j] < a.groups) note(worth[j], in);
+      if (g[j] < a.groups) note(worth[j], size_of(o1[j], o2[j]), in);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) o[j * VEC + i] = in ? o[j * VEC + i] : 0u;
     }
@@ -199,7 +208,9 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
     for (int g = lane; g < a.groups; g += LPR) {
       uint32_t o1 = 0, o2 = 0;
       for (int i = 0; i < per; ++i) merge_two(o1, o2, __float_as_uint(s_v[g * per + i]), 0u);
-      s_v[g * per] = worth_of(o1, o2);             // (in the place of its first score)
+      // (in the places of its first scores; the size of one score alone is its magnitude)
+      s_v[g * per] = worth_of(o1, o2);
+      if (per > 1) s_v[g * per + 1] = size_of(o1, o2);
     }
     row_fence();
     uint32_t stay = 0;                             // (of this lane's groups)
@@ -214,7 +225,7 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
         rank += oq > ow || (oq == ow && q < g);
       }
       const bool in = rank < a.top_groups && ow > kNone;
-      note(worth, in);
+      note(worth, per > 1 ? s_v[g * per + 1] : ow > kNone ? fabsf(worth) : 0.0f, in);
       stay |= in ? 1u << t : 0u;
     }
     row_fence();
@@ -233,8 +244,7 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
   low = over_row<LPR>(low, [](float p, float q) { return q < p ? q : p; });
   high = over_row<LPR>(high, [](float p, float q) { return q > p ? q : p; });
   if (over_row<LPR>(odd ? 1u : 0u, either)) return true;
-  return a.top_groups < a.groups && high > -INFINITY && low < INFINITY &&
-         !(low - high > 2 * near + 2 * kUnit * (fabsf(low) + fabsf(high)));
+  return a.top_groups < a.groups && high > -INFINITY && low < INFINITY && !(low - high > 2 * near);
 }
 
 // The k largest of a row's fp32 scores, of orders o, and whether a gap that decides is within
