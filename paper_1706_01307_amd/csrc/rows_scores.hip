@@ -380,6 +380,17 @@ __device__ __forceinline__ void choose_slow(const ScoreArgs& a, const T* logits,
   }
 }
 
+// Sigmoid scores below exp(kFar) are on their way out of fp32, their ratios, which renormalised
+// weights are, are not: a row with a chosen one has its scores without the factor exp(m), m the
+// largest chosen logit or 0.  (A row with fewer experts than k is taken so too.)  sigmoid(x) = exp(x) / (1 + exp(x)); what x - m loses when it is
+// rounded, up to 64 units of exp's value, is put back.
+constexpr float kFar = -64.0f;
+__device__ __forceinline__ float far_score(float x, float top) {
+  if (x >= 0.0f) return 1.0f / (1.0f + expf(-x));
+  const float m = top < 0.0f ? top : 0.0f, d = x - m, lost = (x - d) - m, e = expf(d);
+  return fmaf(e, lost, e) / (1.0f + expf(x));
+}
+
 // LPR lanes hold a row of at most LPR * NV * VEC logits, 16 a lane.
 template <typename T, int LPR, int NV, bool TAIL>
 __global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
@@ -497,16 +508,23 @@ __global__ __launch_bounds__(kThreads, 4) void k_scores(ScoreArgs a) {
     float* const wt = s_weight + q * a.k;
     const T* const row = logits + static_cast<int64_t>(q) * E;
     float top = a.softmax ? s_top[q] : 0.0f, sum = 0.0f;
+    bool far = false;
 #pragma unroll 8
-    for (int t = 0; t < a.k; ++t) wt[t] = ex[t] < 0 ? -INFINITY : Row<T>::get(row[ex[t]]);
-    if (a.softmax && a.normalize) {
+    for (int t = 0; t < a.k; ++t) {
+      const float x = ex[t] < 0 ? -INFINITY : Row<T>::get(row[ex[t]]);
+      far |= x < kFar;
+      wt[t] = x;
+    }
+    far &= a.normalize && !a.softmax;
+    if (far || (a.softmax && a.normalize)) {
       top = -INFINITY;
       for (int t = 0; t < a.k; ++t) top = wt[t] > top || wt[t] != wt[t] ? wt[t] : top;
     }
     for (int t = 0; t < a.k; ++t) {
       const float x = wt[t];
       float w = 0.0f;
-      if (ex[t] >= 0) w = a.softmax ? expf(x - top) : 1.0f / (1.0f + expf(-x));
+      if (ex[t] >= 0)
+        w = a.softmax ? expf(x - top) : far ? far_score(x, top) : 1.0f / (1.0f + expf(-x));
       wt[t] = w;
       sum += w;
     }
@@ -554,11 +572,11 @@ __global__ __launch_bounds__(kThreads) void k_scores_bwd(ScoreGrad a) {
 #pragma unroll
     for (int i = 0; i < VEC; i += 4)
       *reinterpret_cast<float4*>(row + (lane + LPR * j) * VEC + i) = make_float4(0, 0, 0, 0);
-  // this lane's slots (the whole row's dot product and sum of scores)
+  // this lane's slots (the whole row's dot product)
   constexpr int S = (kMaxK + LPR - 1) / LPR;
   int32_t e[S];
   float w[S], dw[S], p[S];
-  float dot = 0.0f, sum = 0.0f;
+  float dot = 0.0f;
 #pragma unroll
   for (int t = 0; t < S; ++t) {
     const int s = lane + LPR * t;
@@ -572,13 +590,10 @@ __global__ __launch_bounds__(kThreads) void k_scores_bwd(ScoreGrad a) {
     if (!a.softmax && e[t] >= 0) p[t] = 1.0f / (1.0f + expf(-Row<T>::get(logits[e[t]])));
   }
 #pragma unroll
-  for (int t = 0; t < S; ++t) {
+  for (int t = 0; t < S; ++t)
     if (e[t] >= 0) dot += w[t] * dw[t];
-    sum += p[t];
-  }
   const auto add = [](float u, float v) { return u + v; };
   dot = over_row<LPR>(dot, add);
-  sum = over_row<LPR>(sum, add);
   float g[NV][VEC];
 #pragma unroll
   for (int j = 0; j < NV; ++j)
@@ -613,17 +628,15 @@ __global__ __launch_bounds__(kThreads) void k_scores_bwd(ScoreGrad a) {
       for (int i = 0; i < VEC; ++i) g[j][i] *= f;
   }
   row_fence();
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
   for (int t = 0; t < S; ++t) {
     if (LPR * t >= k || e[t] < 0) continue;
+    // (of renormalised weights alike: a weight is scale * score / sum, which fp32 can hold where
+    // the scores and their sum are too small for it)
     float d;
-    if (a.softmax) {
-      d = w[t] * (a.normalize ? dw[t] - dot / a.scale : dw[t]);
-    } else {
-      d = a.normalize ? (dw[t] * a.scale - dot) * inv : dw[t] * a.scale;
-      d = d * p[t] * (1.0f - p[t]);
-    }
+    if (a.normalize) d = w[t] * (dw[t] - dot / a.scale);
+    else d = a.softmax ? w[t] * dw[t] : dw[t] * a.scale * p[t];
+    if (!a.softmax) d *= 1.0f - p[t];
     atomicAdd(row + e[t], d);                      // (an expert is chosen once: no order in it)
   }
   row_fence();

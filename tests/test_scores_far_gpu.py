@@ -1,0 +1,66 @@
+"""Routing by sigmoid scores far from 0: renormalised weights and gradients where the scores
+themselves are beyond fp32.
+
+Weights: half a unit each for two arguments and a quotient, a unit for exp, k + 1 for the sum, less
+than (k + 16) U of a weight.  Gradients: a weight, k of them in a sum (k + 1 more), a logistic
+function and four products, less than (3 k + 48) U of the magnitudes."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_1706_01307_amd as spc  # noqa: E402
+from tests.rows_ref import U  # noqa: E402
+from tests.test_rows_gpu import DT, _gen, _gpu  # noqa: E402,F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(x, k, scale, dw):
+    """x [n, E]: against the softmax of the chosen scores' logarithms, which is their ratio to the sum."""
+    r = spc.route_scores_forward(x.cuda(), k, score="sigmoid", scale=scale)
+    e = r.experts.cpu().long()
+    assert bool((e >= 0).all())
+    c = x.double().gather(1, e)
+    share = torch.softmax(torch.nn.functional.logsigmoid(c), 1)
+    w, bf = share * scale, x.dtype == torch.bfloat16
+    off = (r.weights.cpu().double() - w).abs()
+    assert bool((off <= (k + 16) * U * w + 1e-37).all()), float((off / w).max() / U)
+    d = spc.route_scores_backward(dw.cuda(), x.cuda(), r.experts, r.weights, score="sigmoid", scale=scale)
+    d = d.cpu().double()
+    g, back = dw.double() * scale, torch.sigmoid(-c)
+    want = share * back * (g - (share * g).sum(1, keepdim=True))
+    mag = share * back * (g.abs() + (share * g.abs()).sum(1, keepdim=True))
+    got = d.gather(1, e)
+    bound = (3 * k + 48) * U * mag + 1e-36 + (2.0 ** -8 * want.abs() if bf else 0.0)
+    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).max())
+    assert torch.equal(d.scatter(1, e, torch.zeros_like(got)), torch.zeros_like(d))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1.0, 2.5])
+def test_logits_far_below_0(scale, dtype):
+    dt, r = DT[dtype], _gen(4)
+    same = torch.full((1, 8), -100.0).to(dt)
+    w = spc.route_scores_forward(same.cuda(), 2, scale=scale).weights
+    assert w.cpu().tolist() == [[0.5 * scale] * 2]
+    for E, k, lo, hi in ((2, 2, -89, -89), (8, 3, -90, -86), (16, 8, -300, -85), (64, 8, -110, -60),
+                         (5, 5, -100, 5), (8, 8, -104, 0), (300, 16, -700, -90), (4, 4, -2000, -800),
+                         (16, 4, -30, -15)):
+        n = 50
+        x = (lo + (hi - lo) * torch.rand(n, E, generator=torch.Generator().manual_seed(E))).to(dt)
+        _check(x, k, scale, r(n, k))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_what_is_not_finite_beside_far_logits(dtype):
+    x = torch.tensor([[-200.0, math.nan, -201.0], [-200.0, math.inf, -201.0],
+                      [-200.0, -math.inf, -201.0], [-3e38, -200.0, -201.0]]).to(DT[dtype])
+    r = spc.route_scores_forward(x.cuda(), 3, score="sigmoid")
+    w, e = r.weights.cpu(), r.experts.cpu().tolist()
+    assert torch.isnan(w[0]).all() and e[1] == [1, 0, 2] and w[1].tolist() == [1.0, 0.0, 0.0]
+    two = torch.softmax(x[2, ::2].double(), 0)
+    assert e[2] == [0, 2, -1] and bool(((w[2, :2].double() - two).abs() <= 20 * U).all()) and w[2, 2] == 0
+    two = torch.softmax(x[3, 1:].double(), 0)
+    assert e[3] == [1, 2, 0] and bool(((w[3, :2].double() - two).abs() <= 20 * U).all()) and w[3, 2] == 0
