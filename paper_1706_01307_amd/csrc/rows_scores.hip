@@ -575,19 +575,22 @@ __global__ __launch_bounds__(kThreads) void k_scores_bwd(ScoreGrad a) {
   // this lane's slots (the whole row's dot product)
   constexpr int S = (kMaxK + LPR - 1) / LPR;
   int32_t e[S];
-  float w[S], dw[S], p[S];
+  float w[S], dw[S], p[S], q[S];                   // (p, q: a sigmoid and 1 - it, to its own last bit)
   float dot = 0.0f;
 #pragma unroll
   for (int t = 0; t < S; ++t) {
     const int s = lane + LPR * t;
-    e[t] = -1, w[t] = dw[t] = p[t] = 0.0f;
+    e[t] = -1, w[t] = dw[t] = p[t] = q[t] = 0.0f;
     if (LPR * t >= k) continue;                    // (uniform)
     e[t] = s < k ? a.experts[r * k + s] : -1;
     if (e[t] >= E) e[t] = -1;
     w[t] = e[t] < 0 ? 0.0f : a.weights[r * k + s];
     dw[t] = e[t] < 0 ? 0.0f : a.dweights[r * k + s];
-    p[t] = 0.0f;
-    if (!a.softmax && e[t] >= 0) p[t] = 1.0f / (1.0f + expf(-Row<T>::get(logits[e[t]])));
+    if (!a.softmax && e[t] >= 0) {
+      const float x = Row<T>::get(logits[e[t]]), u = expf(-fabsf(x)), r = 1.0f / (1.0f + u);
+      p[t] = x < 0.0f ? u * r : r;
+      q[t] = x < 0.0f ? r : u * r;
+    }
   }
 #pragma unroll
   for (int t = 0; t < S; ++t)
@@ -636,7 +639,7 @@ __global__ __launch_bounds__(kThreads) void k_scores_bwd(ScoreGrad a) {
     float d;
     if (a.normalize) d = w[t] * (dw[t] - dot / a.scale);
     else d = a.softmax ? w[t] * dw[t] : dw[t] * a.scale * p[t];
-    if (!a.softmax) d *= 1.0f - p[t];
+    if (!a.softmax) d *= q[t];
     atomicAdd(row + e[t], d);                      // (an expert is chosen once: no order in it)
   }
   row_fence();

@@ -1,5 +1,5 @@
 """Routing by sigmoid scores far from 0: renormalised weights and gradients where the scores
-themselves are beyond fp32.
+themselves are beyond fp32, and gradients where they are all but 1.
 
 Weights: half a unit each for two arguments and a quotient, a unit for exp, k + 1 for the sum, less
 than (k + 16) U of a weight.  Gradients: a weight, k of them in a sum (k + 1 more), a logistic
@@ -64,3 +64,21 @@ def test_what_is_not_finite_beside_far_logits(dtype):
     assert e[2] == [0, 2, -1] and bool(((w[2, :2].double() - two).abs() <= 20 * U).all()) and w[2, 2] == 0
     two = torch.softmax(x[3, 1:].double(), 0)
     assert e[3] == [1, 2, 0] and bool(((w[3, :2].double() - two).abs() <= 20 * U).all()) and w[3, 2] == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_gradient_of_scores_all_but_1(normalize, dtype):
+    """The slope s (1 - s) of a score next to 1 keeps the bits of 1 - s."""
+    n, E, k, scale = 60, 16, 4, 2.5
+    x = (5 + 75 * torch.rand(n, E, generator=torch.Generator().manual_seed(2))).to(DT[dtype])
+    dw = _gen(3)(n, k)
+    if normalize:
+        return _check(x, k, scale, dw)
+    r = spc.route_scores_forward(x.cuda(), k, scale=scale, normalize=False)
+    d = spc.route_scores_backward(dw.cuda(), x.cuda(), r.experts, r.weights, scale=scale, normalize=False)
+    c = x.double().gather(1, r.experts.cpu().long())
+    want = dw.double() * scale * torch.sigmoid(c) * torch.sigmoid(-c)
+    got = d.cpu().double().gather(1, r.experts.cpu().long())
+    bound = (16 * U + (2.0 ** -8 if dtype == "bf16" else 0.0)) * want.abs() + 1e-36
+    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).max())
