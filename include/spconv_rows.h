@@ -310,7 +310,7 @@ int spconv_linear_backward_weight_workspace(int x_dt, int64_t n, int C_in, int C
  *   x_dt  dtype of x [n][C_in]; that of dy [n][C_out] too, bf16 for rows in 8 bits
  *   dw    fp32 [C_in][C_out];  db fp32 [C_out] or NULL
  * Many rows are summed in chunks of a size fixed by the arguments, the chunks in
- * ascending order. */
+ * ascending order.  The factor x_scale * dy of rows in 8 bits is rounded to fp32. */
 int spconv_linear_backward_weight(int x_dt, const void* x, const float* x_scale, const void* dy,
                                   float* dw, float* db, int64_t n, int C_in, int C_out,
                                   void* workspace, size_t workspace_bytes, void* stream);

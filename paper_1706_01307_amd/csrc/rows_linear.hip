@@ -4,7 +4,7 @@
 // 8-bit rows are multiplied as the bf16 numbers they are (every e4m3 value is one), and the
 // row's scale is taken out of the sum: forwards it is a factor of the finished row, in the
 // weight gradient, where the sum runs over the rows, it goes to the other operand, scale *
-// dy, which enters as the sum of two f16 numbers.
+// dy, which enters as the sum of three bf16 numbers.
 #include <type_traits>
 
 #include "rows_act.h"
@@ -871,7 +871,7 @@ template <int BC, int BN> __device__ __forceinline__ WeightJob weight_job(const 
 // The finished tile, straight from the registers (32 bytes of a row by two lanes).
 template <int FC, int FN>
 __device__ __forceinline__ void store_sums(const f32x16 (&acc)[FN][FC], const LinearWeight& a,
-                                           int64_t job, int r0, int c0, float unit) {
+                                           int64_t job, int r0, int c0) {
   const int lane = threadIdx.x & 63;
   float* out = a.dw + job * a.C_in * a.C_out;
 #pragma unroll
@@ -885,7 +885,7 @@ __device__ __forceinline__ void store_sums(const f32x16 (&acc)[FN][FC], const Li
         const int c = c0 + 32 * n + 8 * q + 4 * (lane >> 5);
         float v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = acc[n][m][4 * q + i] * unit;
+        for (int i = 0; i < 4; ++i) v[i] = acc[n][m][4 * q + i];
         if (c < a.C_out) store_left(out + r * a.C_out + c, pack(v), a.C_out - c);
       }
     }
@@ -975,69 +975,48 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw_ring(LinearWeight
       if (lane < 32 && col < a.C_out) a.db[t.job * a.C_out + col] = v;
     }
   }
-  store_sums<FC, FN>(acc, a, t.job, t.c0 + wr, t.n0 + wc, 1.0f);
+  store_sums<FC, FN>(acc, a, t.job, t.c0 + wr, t.n0 + wc);
 }
 
-// The matrix cores' step for 8-bit rows: both operands in f16.
-struct MmaHalf {
-  typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-  __device__ static f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
-                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  }
-};
-// Eight e4m3 values as f16, exactly.
-__device__ __forceinline__ u32x4_t widen_half(uint32_t lo, uint32_t hi) {
-  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-  u32x4_t v;
-  v[0] = __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
-  v[1] = __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
-  v[2] = __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
-  v[3] = __builtin_bit_cast(uint32_t, (h2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
-  return v;
-}
-
-// The largest finite |dy| of a piece of eight (as bf16, by their bits).
-__device__ __forceinline__ float top_of(u32x4_t u) {
-  typedef uint16_t s2 __attribute__((ext_vector_type(2)));
-  s2 t = {0, 0};
+// Eight fp32 numbers as three bf16 ones each that add up to them, cut off rather than rounded: 8 bits
+// at the top, the 8 behind them, the 8 that are left.  An infinity is its first number, beside
+// zeros.  (A NaN's three are NaN.)
+template <bool INF>
+__device__ __forceinline__ void split_bf16(const float (&v)[8], u32x4_t (&part)[3]) {
+  // (the high halves of b and a)
+  const auto both = [](float a, float b) {
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+  };
+  const auto top = [](float a) { return __uint_as_float(__float_as_uint(a) & 0xffff0000u); };
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const s2 m = __builtin_bit_cast(s2, u[i] & 0x7fff7fffu);
-    t = __builtin_elementwise_max(t, m);
+    float a = v[2 * i], b = v[2 * i + 1];
+    part[0][i] = both(a, b);
+    a = INF && fabsf(a) == INFINITY ? 0.0f : a - top(a);
+    b = INF && fabsf(b) == INFINITY ? 0.0f : b - top(b);
+    part[1][i] = both(a, b);
+    part[2][i] = both(a - top(a), b - top(b));
   }
-  const uint32_t most = t[0] > t[1] ? t[0] : t[1];
-  if (most < 0x7f80u) return __uint_as_float(most << 16);
-  float v[8], top = 0.0f;                          // (an infinity or NaN among them)
-  unpack(u, v);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float m = __uint_as_float(magnitude(v[i]));
-    top = m < INFINITY && m > top ? m : top;
-  }
-  return top;
 }
 
 // The same through registers: cut or unaligned pieces, and rows in 8 bits (X8), whose scale goes
-// to the other operand.  v = scale * dy enters as two f16 numbers, v 2^-e and what it leaves:
-// 22 bits.  e follows the largest finite |v| that the workgroup has met (it is told of a
-// stage's in front of the barrier that the stage waits at anyway; the sums so far are moved
-// when it grows): what is 2^17 below it loses bits, but nothing over 2^-40 of it.  (A dy that is
-// not finite leaves its column NaN.)
+// to the other operand: scale * dy, rounded to fp32, enters as three bf16 numbers that are exactly
+// it, beside the e4m3 values as the bf16 numbers they are, so that every product is exact
+// wherever its factors lie.  (Two f16 numbers under a power of two for the tile: 22 bits of the
+// tile's largest and fewer of what is far below it, at two thirds of the products: 16,384 x 2048 x
+// 2048 300 us, 348,208 x 256 x 1024 421, and 363 and 509 so.)
 // WHOLE: rows are of whole pieces.
-// 16,384 x 2048 x 2048 of 8 bits: 321 us and 14 for the sums, 860 TFLOP/s of the two products it is:
-// matrix cores 48 % of the busy cycles, vector ALU 44, LDS 28 (eight waves of 64 x 64 instead of
-// four of 128 x 64: 376; stages of 64 rows: 409).
+// 16,384 x 2048 x 2048 of 8 bits, with the chunks' sums: 363 us, 1,140 TFLOP/s of the three products it
+// is, as much as a large library product.
 template <typename T, bool X8, int BC, int BN, int WR, int WC, int KB, bool WHOLE>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
   typedef KTile<T, BC, KB> TX;
   typedef KTile<T, BN, KB> TY;
   constexpr int VEC = Row<T>::VEC, BK = kBK<T, KB>, NT = 64 * WR * WC;
   constexpr int FC = BC / WR / 32, FN = BN / WC / 32;
-  constexpr int PX = TX::PIECES / NT, PY = TY::PIECES / NT, NL = X8 ? 2 : 1;
+  constexpr int PX = TX::PIECES / NT, PY = TY::PIECES / NT, NL = X8 ? 3 : 1;
   __shared__ u32x4_t s_x[TX::PIECES], s_y[NL][TY::PIECES];
-  __shared__ float s_db[NT / TY::PR][BN + 1];
-  __shared__ float s_top[2][WR * WC];
+  __shared__ float s_db[NT / TY::PR][BN];
   const T* const dy = static_cast<const T*>(a.dy);
   const WeightJob t = weight_job<BC, BN>(a);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -1083,20 +1062,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
   const int wr = wave / WC * (BC / WR), wc = wave % WC * (BN / WC);
   const typename TX::template Reader<32, FC> x_of(wr, lane);
   const typename TY::template Reader<32, FN> dy_of(wc, lane);
-  int power = -126;                                // e: |v| 2^-e < 2^15
-  int turn = 0;
   if (t.begin < t.end) request(t.begin);
   for (int64_t j0 = t.begin; j0 < t.end; j0 += BK) {
-    if constexpr (X8) {
-      float top = 0.0f;
-#pragma unroll
-      for (int i = 0; i < PY; ++i) {
-        const float m = top_of(ry[i]) * rs[i];
-        top = m < INFINITY && m > top ? m : top;
-      }
-      top = group_reduce<64>(top, [](float p, float q) { return q > p ? q : p; });
-      if (lane == 0) s_top[turn][wave] = top;
-    }
     if (bias) {
 #pragma unroll
       for (int i = 0; i < PY; ++i) {
@@ -1107,52 +1074,25 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
       }
     }
     __syncthreads();
-    float unit = 1.0f;
-    if constexpr (X8) {
-      float top = s_top[turn][0];
-#pragma unroll
-      for (int q = 1; q < WR * WC; ++q) top = s_top[turn][q] > top ? s_top[turn][q] : top;
-      turn ^= 1;
-      // top < 2^(its exponent + 1)
-      int need = static_cast<int>(__float_as_uint(top) >> 23) - 127 + 1 - 15;
-      need = __builtin_amdgcn_readfirstlane(need < -126 ? -126 : need);
-      if (need > power) {
-        const float f = ldexpf(1.0f, power - need);
-        power = need;
-#pragma unroll
-        for (int n = 0; n < FN; ++n)
-#pragma unroll
-          for (int m = 0; m < FC; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[n][m][i] *= f;
-      }
-      unit = __uint_as_float(static_cast<uint32_t>(127 - power) << 23);
-    }
 #pragma unroll
     for (int i = 0; i < PX; ++i)
-      s_x[TX::at(jx + NT / TX::PR * i, px)] = X8 ? widen_half(rx8[i].x, rx8[i].y) : rx[i];
+      s_x[TX::at(jx + NT / TX::PR * i, px)] = X8 ? widen(rx8[i].x, rx8[i].y) : rx[i];
 #pragma unroll
     for (int i = 0; i < PY; ++i) {
       const int to = TY::at(jy + NT / TY::PR * i, py);
       if constexpr (X8) {
-        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-        typedef float f2 __attribute__((ext_vector_type(2)));
-        // (kept finite beside a row of zeros, whose products are too small for `power`)
-        float by = rs[i] * unit;
-        by = by > 0x1p127f && rs[i] < INFINITY ? 0x1p127f : by;
-        float v[VEC];
+        float v[VEC], most = 0.0f;
         unpack(ry[i], v);
-        u32x4_t hi, lo;
 #pragma unroll
-        for (int e = 0; e < VEC; e += 2) {
-          const f2 u = {v[e] * by, v[e + 1] * by};
-          const h2 up = __builtin_convertvector(u, h2);
-          const f2 rest = {u[0] - static_cast<float>(up[0]), u[1] - static_cast<float>(up[1])};
-          hi[e / 2] = __builtin_bit_cast(uint32_t, up);
-          lo[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, h2));
+        for (int e = 0; e < VEC; ++e) {
+          v[e] *= rs[i];
+          most = fmaxf(most, fabsf(v[e]));
         }
-        s_y[0][to] = hi;
-        s_y[NL - 1][to] = lo;
+        u32x4_t part[3];
+        if (most < INFINITY) split_bf16<false>(v, part);
+        else split_bf16<true>(v, part);
+#pragma unroll
+        for (int l = 0; l < NL; ++l) s_y[l][to] = part[l];
       } else {
         s_y[0][to] = ry[i];
       }
@@ -1174,7 +1114,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
 #pragma unroll
           for (int n = 0; n < FN; ++n)
 #pragma unroll
-            for (int m = 0; m < FC; ++m) acc[n][m] = MmaHalf::mma(fy[l][n], fx[m], acc[n][m]);
+            for (int m = 0; m < FC; ++m) acc[n][m] = Mma<T>::mma(fy[l][n], fx[m], acc[n][m]);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
@@ -1194,7 +1134,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
       a.db[t.job * a.C_out + t.n0 + threadIdx.x] = s;
     }
   }
-  store_sums<FC, FN>(acc, a, t.job, t.c0 + wr, t.n0 + wc, X8 ? ldexpf(1.0f, power) : 1.0f);
+  store_sums<FC, FN>(acc, a, t.job, t.c0 + wr, t.n0 + wc);
 }
 
 // The chunks' sums: kThreads / RUNS lanes side by side with four values each, RUNS of them down

@@ -220,12 +220,12 @@ inline bool linear_past(int64_t n, int cols, int bytes) {
 // (us by jobs, bf16 348,208 x 1024 x 256 in tiles of 256: 32 360, 64 271, 128 292; 16,384 x
 // 2048 x 2048: 2 232, 4 162, 8 198, of 128 3 178; 902,504 x 64 x 64 of 64: 256 60, 512 45,
 // 1,024 55; 8,000 x 512 x 512 of 64: 4 26, 8 20, 32 25.  Rows in 8 bits, 16,384 x 2048 x
-// 2048 of 256: 4 335; fp32 65,536 x 1024 x 1024 of 128: 4 1,203, 12 1,066.)
+// 2048 of 256: 2 463, 4 343, 8 354, of 128 2 407, of 64 1 579; fp32 65,536 x 1024 x 1024 of 128: 4 1,203, 12 1,066.)
 inline DwPlan linear_dw_plan(int x_dt, int64_t n, int C_in, int C_out) {
   struct Rate { int tile; double alone, full, slots; };
   static const Rate bf16[3] = {{64, 0.5, 0.62, 1024}, {128, 0.77, 0.9, 768}, {256, 0.82, 1.05, 512}};
   static const Rate f32[2] = {{64, 0.52, 1.15, 1024}, {128, 1.17, 3.05, 768}};
-  static const Rate e4m3[3] = {{64, 0.6, 1.22, 1024}, {128, 1.17, 1.6, 512}, {256, 1.5, 2.45, 512}};
+  static const Rate e4m3[3] = {{64, 0.63, 1.12, 1024}, {128, 1.14, 1.55, 512}, {256, 1.77, 2.55, 512}};
   const Rate* rate = x_dt == SPCONV_F32 ? f32 : x_dt == SPCONV_BF16 ? bf16 : e4m3;
   const int kinds = x_dt == SPCONV_F32 ? 2 : 3, rows = x_dt == SPCONV_F32 ? 16 : 32;
   const double values = static_cast<double>(C_in) * C_out + C_out;

@@ -1,6 +1,7 @@
 """Dense weight gradients against their 64-bit statements, every tile with whole and cut pieces.
 
-Tolerance: (rows + 32) * 2^-24 times the sum of the terms' magnitudes, an fp32 sum in any order."""
+Tolerance: (terms + 32) * 2^-24 times the sum of the terms' magnitudes, an fp32 sum in any order: a
+term a row, of 8-bit rows three, whose factor scale * dy is rounded once (2 units more)."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -29,13 +30,16 @@ def test_every_tile(dt, n, ci, co, tile, whole, several):
     dy = _gen(n + 2)(n, co, dtype=d)
     dv = _f64(dy)
     want, mag = xv.t() @ dv, xv.abs().t() @ dv.abs()
-    views = [(x, dy.cuda())]
-    if whole:
+    terms, views = n, [(x, dy.cuda())]
+    if dt == "e4m3":
+        terms = 3 * n + 2
+        views += [(spc.Rows8(_shifted(x.q.cpu().view(torch.uint8)).view(x.q.dtype), x.scale), _shifted(dy))]
+    elif whole:
         views += [(_shifted(x.cpu()), dy.cuda()), (x, _shifted(dy))]
     for i, (a, b) in enumerate(views):
         _poison()
         dw, db = spc.linear_backward_weight(a, b)
-        _off(dw, want, (n + 32) * U * mag, ("dw", i))
+        _off(dw, want, (terms + 32) * U * mag, ("dw", i))
         _off(db, dv.sum(0), (n + 32) * U * dv.abs().sum(0), ("db", i))
         again, none = spc.linear_backward_weight(a, b, bias=False)
         assert none is None and torch.equal(again, dw), i
