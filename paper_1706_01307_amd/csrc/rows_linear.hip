@@ -694,6 +694,7 @@ __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
   typedef float T;
   constexpr int VEC = Row<T>::VEC, R = kFewRows, CL = 4, NC = CL * VEC, KS = kFewThreads / CL;
   constexpr int KC = 2048, UN = 8;                 // of the reduction in LDS; loads in flight
+  static_assert(KS * UN == KC, "a slice's loads reach to the end of what is in LDS");
   constexpr int NW = kFewThreads / 64;
   __shared__ float s_x[R][KC];
   __shared__ float s_sum[NW][R][NC];
@@ -710,15 +711,13 @@ __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
   for (int k0 = 0; k0 < a.red; k0 += KC) {
     const int kc = a.red - k0 < KC ? a.red - k0 : KC;
     u32x4_t u[UN];
-    auto request = [&](int k1) {
+    // (on their way while the rows are staged)
 #pragma unroll
-      for (int i = 0; i < UN; ++i) {
-        const int k = k1 + KS * i;
-        u[i] = load_piece(k < kc && c < a.cols ? w + static_cast<int64_t>(k0 + k) * a.cols + c
-                                               : reinterpret_cast<const T*>(&g_zeros));
-      }
-    };
-    request(slice);                                // (on their way while the rows are staged)
+    for (int i = 0; i < UN; ++i) {
+      const int k = slice + KS * i;
+      u[i] = load_piece(k < kc && c < a.cols ? w + static_cast<int64_t>(k0 + k) * a.cols + c
+                                             : reinterpret_cast<const T*>(&g_zeros));
+    }
     __syncthreads();
     for (int k = threadIdx.x % (kFewThreads / R); k < kc; k += kFewThreads / R) {
       float v = 0.0f;
@@ -728,19 +727,16 @@ __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
       s_x[sr][k] = v;
     }
     __syncthreads();
-    for (int k1 = slice; k1 < kc; k1 += KS * UN) {
-      if (k1 != slice) request(k1);
 #pragma unroll
-      for (int i = 0; i < UN; ++i) {
-        const int k = k1 + KS * i;
-        if (k >= kc) break;
-        float v[VEC];
-        unpack(u[i], v);
+    for (int i = 0; i < UN; ++i) {
+      const int k = slice + KS * i;
+      if (k >= kc) break;
+      float v[VEC];
+      unpack(u[i], v);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) acc[r][e] = fmaf(s_x[r][k], v[e], acc[r][e]);
-      }
+        for (int e = 0; e < VEC; ++e) acc[r][e] = fmaf(s_x[r][k], v[e], acc[r][e]);
     }
   }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
