@@ -76,7 +76,9 @@ extern "C" {
 #define SPCONV_SCORE_SOFTMAX 1
 
 /* Activations: z; max(z, 0); z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2;
- * z / (1 + exp(-z)). */
+ * z / (1 + exp(-z)).  Before they are rounded to the result's type, values are
+ * within 8 units (2^-24) of |z|, those of the last one in fp32 also within 16 of
+ * their own size down to z = -80; slopes within 32 + 2 |z| units of 1. */
 #define SPCONV_ACT_NONE 0
 #define SPCONV_ACT_RELU 1
 #define SPCONV_ACT_GELU 2
@@ -241,7 +243,7 @@ int spconv_combine_backward(int dt, const void* dout, const void* y, const int32
  *   dt        dtype of x, residual and h
  *   residual  or NULL
  *   gamma     fp32 [C] or NULL (1)
- *   eps       >= 0 and finite
+ *   eps       >= 0 and finite (sum h^2 is in fp32: |h| below 1e19 / sqrt(C))
  *   h         [n][C], or NULL if it is not wanted (NULL without a residual); may
  *             be x or residual itself
  *   out_dt    dt, or SPCONV_E4M3: y is then in 8 bits, packed from fp32, y_scale
@@ -340,7 +342,8 @@ int spconv_route_scores_forward(int dt, const void* logits, const float* bias, i
 
 /* Gradient of those weights with respect to the logits (the choice itself has
  * none), dlogits [n][E] of dtype dt.  experts are a forward's: an expert at most
- * once a row.  dweights of slots without an expert are not read into anything.  logits may be NULL for softmax scores with normalize = 1. */
+ * once a row.  dweights of slots without an expert are not read into anything.
+ * logits may be NULL for softmax scores with normalize = 1. */
 int spconv_route_scores_backward(int dt, const float* dweights, const void* logits,
                                  const int32_t* experts, const float* weights, int64_t n, int E,
                                  int k, int score, int normalize, float scale, void* dlogits,

@@ -83,19 +83,31 @@ __device__ __forceinline__ void store_row8(uint8_t* p, int64_t c, int64_t C, con
 __device__ __forceinline__ float logistic2(float t) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
 }
-constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596303e-8f;
+// The logistic function of z.  Rounding z log2(e) is off by up to |z| units of exp's value, which
+// counts where that is the result, far below 0; FINE (fp32 results: bf16 ones have no place for it)
+// puts it back.  (Both ends are reached long before +-120, and nothing is infinite within.)
+template <bool FINE> __device__ __forceinline__ float logistic(float z) {
+  if constexpr (FINE) {
+    const float c = __builtin_amdgcn_fmed3f(z, -120.0f, 120.0f), t = c * -kLog2e;
+    const float lost = fmaf(c, -kLog2eLow, fmaf(c, -kLog2e, -t));
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(lost, 0.693147181f, 1.0f));
+  } else {
+    return logistic2(z * -kLog2e);
+  }
+}
 // GELU in its tanh form: z (1 + tanh u) / 2 = z / (1 + exp(-2 u)), u = sqrt(2 / pi) (z + 0.044715
 // z^3): -2 u log2(e) = z (G + G3 z^2).
 constexpr float kG = -2.30220819f, kG3 = -0.102943240f;
-template <int ACT> __device__ __forceinline__ float activate(float z) {
+template <int ACT, bool FINE> __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == SPCONV_ACT_RELU) return z < 0.0f ? 0.0f : z;
   if constexpr (ACT == SPCONV_ACT_GELU) return z * logistic2(z * fmaf(kG3, z * z, kG));
-  if constexpr (ACT == SPCONV_ACT_SILU) return z * logistic2(z * -kLog2e);
+  if constexpr (ACT == SPCONV_ACT_SILU) return z * logistic<FINE>(z);
   return z;
 }
 // With s the logistic function's value: s + s (1 - s) z (2 u)', and 1 - s as s - s s (off by
 // half a unit of 1).
-template <int ACT> __device__ __forceinline__ float slope(float z) {
+template <int ACT, bool FINE> __device__ __forceinline__ float slope(float z) {
   if constexpr (ACT == SPCONV_ACT_RELU) return z <= 0.0f ? 0.0f : 1.0f;
   if constexpr (ACT == SPCONV_ACT_GELU) {
     const float z2 = z * z, s = logistic2(z * fmaf(kG3, z2, kG));
@@ -104,7 +116,7 @@ template <int ACT> __device__ __forceinline__ float slope(float z) {
     return fmaf(fmaf(-s, s, s), w, s);
   }
   if constexpr (ACT == SPCONV_ACT_SILU) {
-    const float s = logistic2(z * -kLog2e);
+    const float s = logistic<FINE>(z);
     return fmaf(fmaf(-s, s, s), z, s);
   }
   return 1.0f;

@@ -169,7 +169,7 @@ __device__ __forceinline__ void finish_tile(u32x4_t* lds,
             }
             by_act(a.act, [&](auto k) {
 #pragma unroll
-              for (int e = 0; e < VO; ++e) v[e] *= slope<decltype(k)::value>(s[e]);
+              for (int e = 0; e < VO; ++e) v[e] *= slope<decltype(k)::value, sizeof(TO) == 4>(s[e]);
             });
           }
         } else {
@@ -178,7 +178,7 @@ __device__ __forceinline__ void finish_tile(u32x4_t* lds,
           if (a.z) store_left<TO, PAST>(static_cast<TO*>(a.z) + at[i], pack(v), left);
           by_act(a.act, [&](auto k) {
 #pragma unroll
-            for (int e = 0; e < VO; ++e) v[e] = activate<decltype(k)::value>(v[e]);
+            for (int e = 0; e < VO; ++e) v[e] = activate<decltype(k)::value, sizeof(TO) == 4>(v[e]);
           });
           if (a.side) {
             float s[VO];
@@ -562,7 +562,7 @@ __global__ __launch_bounds__(512, NK == 2 && !RES ? 4 : 2) void k_linear_short(L
 #pragma unroll
         for (int b = 0; b < FN; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[b][i] = activate<decltype(k)::value>(acc[b][i]);
+          for (int i = 0; i < 16; ++i) acc[b][i] = activate<decltype(k)::value, false>(acc[b][i]);
       });
     }
     if constexpr (RES) {
@@ -765,7 +765,7 @@ __global__ __launch_bounds__(kFewThreads) void k_linear_few(LinearArgs a) {
   for (int q = 0; q < NW; ++q) z += s_sum[q][r][threadIdx.x % NC];
   if (a.bias) z += a.bias[col];
   if (a.z) static_cast<TO*>(a.z)[at] = Row<TO>::put(z);
-  by_act(a.act, [&](auto k) { z = activate<decltype(k)::value>(z); });
+  by_act(a.act, [&](auto k) { z = activate<decltype(k)::value, sizeof(TO) == 4>(z); });
   if (a.side) z += Row<TO>::get(static_cast<const TO*>(a.side)[at]);
   static_cast<TO*>(a.y)[at] = Row<TO>::put(z);
 }
@@ -835,7 +835,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_few_back(LinearArgs a) {
           a.side_scale[row];
     else
       z = Row<TO>::get(static_cast<const TO*>(a.side)[at]);
-    by_act(a.act, [&](auto k) { mine *= slope<decltype(k)::value>(z); });
+    by_act(a.act, [&](auto k) { mine *= slope<decltype(k)::value, sizeof(TO) == 4>(z); });
   }
   static_cast<TO*>(a.y)[at] = Row<TO>::put(mine);
 }

@@ -49,7 +49,8 @@ __global__ __launch_bounds__(kThreads) void k_act(ActArgs a) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         const float w = Z8 ? v[u][i] * s[u] : v[u][i];
-        v[u][i] = GRAD ? d[u][i] * slope<ACT>(w) : activate<ACT>(w);
+        v[u][i] = GRAD ? d[u][i] * slope<ACT, sizeof(T) == 4>(w)
+                       : activate<ACT, sizeof(T) == 4>(w);
       }
       store_row<T, TAIL>(out + (first + u) * C, c, C, v[u]);
     }
