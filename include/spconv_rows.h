@@ -330,8 +330,9 @@ int spconv_linear_backward_weight(int x_dt, const void* x, const float* x_scale,
  *               score is -infinity is never chosen (-1 in the slots left over);
  *               NaN ranks above every number.
  *   weights     fp32 [n][k]: the chosen scores without the bias; normalize = 1:
- *               divided by their sum, also where the scores are too small for
- *               fp32; times scale (> 0 and finite).  0 where no expert is chosen.
+ *               divided by their sum, the scores 64-bit numbers here too (0 where
+ *               the sum is 0); times scale (> 0 and finite).  0 where no expert is
+ *               chosen.
  *   offsets, rows, pos and the workspace (spconv_route_workspace) as for
  *               spconv_route_forward */
 int spconv_route_scores_forward(int dt, const void* logits, const float* bias, int64_t n, int E,

@@ -383,9 +383,11 @@ __device__ __forceinline__ void choose_slow(const ScoreArgs& a, const T* logits,
 // Sigmoid scores below exp(kFar) are on their way out of fp32, their ratios, which renormalised
 // weights are, are not: a row with a chosen one has its scores without the factor exp(m), m the
 // largest chosen logit or 0.  (A row with fewer experts than k is taken so too.)  sigmoid(x) = exp(x) / (1 + exp(x)); what x - m loses when it is
-// rounded, up to 64 units of exp's value, is put back.
-constexpr float kFar = -64.0f;
+// rounded, up to hundreds of units of exp's value, is put back.  What 64 bits have as 0, as they
+// do where exp(-x) is past them, is 0: logits of a type's lowest value close a row too.
+constexpr float kFar = -64.0f, kNothing = -709.7827f;
 __device__ __forceinline__ float far_score(float x, float top) {
+  if (x <= kNothing) return 0.0f;
   if (x >= 0.0f) return 1.0f / (1.0f + expf(-x));
   const float m = top < 0.0f ? top : 0.0f, d = x - m, lost = (x - d) - m, e = expf(d);
   return fmaf(e, lost, e) / (1.0f + expf(x));

@@ -18,12 +18,14 @@ pytestmark = pytest.mark.gpu
 
 
 def _check(x, k, scale, dw):
-    """x [n, E]: against the softmax of the chosen scores' logarithms, which is their ratio to the sum."""
+    """x [n, E]: against the chosen scores in 64 bits, 0 from logits of -709.79 on, over their sum."""
     r = spc.route_scores_forward(x.cuda(), k, score="sigmoid", scale=scale)
     e = r.experts.cpu().long()
     assert bool((e >= 0).all())
     c = x.double().gather(1, e)
-    share = torch.softmax(torch.nn.functional.logsigmoid(c), 1)
+    s = 1 / (1 + torch.exp(-c))
+    total = s.sum(1, keepdim=True)
+    share = torch.where(total > 0, s / torch.where(total > 0, total, 1.0), 0.0)
     w, bf = share * scale, x.dtype == torch.bfloat16
     off = (r.weights.cpu().double() - w).abs()
     assert bool((off <= (k + 16) * U * w + 1e-37).all()), float((off / w).max() / U)
@@ -82,3 +84,21 @@ def test_gradient_of_scores_all_but_1(normalize, dtype):
     got = d.cpu().double().gather(1, r.experts.cpu().long())
     bound = (16 * U + (2.0 ** -8 if dtype == "bf16" else 0.0)) * want.abs() + 1e-36
     assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_rows_closed_by_the_lowest_number(normalize, dtype):
+    """A row of the type's lowest value has scores of 0 and weights of 0; beside an open expert such ones
+    weigh nothing; no gradient reaches them."""
+    low = torch.finfo(DT[dtype]).min
+    x = torch.full((3, 8), low).to(DT[dtype])
+    x[1, 5], x[2, 2], x[2, 6] = -95.0, -709.0, -720.0
+    r = spc.route_scores_forward(x.cuda(), 2, normalize=normalize)
+    w = r.weights.cpu()
+    assert r.experts.cpu().tolist() == [[0, 1], [5, 0], [2, 0]]
+    assert w.tolist() == ([[0, 0], [1, 0], [1, 0]] if normalize else [[0, 0], [w[1, 0], 0], [0, 0]])
+    d = spc.route_scores_backward(torch.ones(3, 2, device="cuda"), x.cuda(), r.experts, r.weights,
+                                  normalize=normalize).cpu()
+    d[1, 5] = 0
+    assert not d.any()
