@@ -1002,8 +1002,8 @@ __device__ __forceinline__ void split_bf16(const float (&v)[8], u32x4_t (&part)[
 // tile's largest and fewer of what is far below it, at two thirds of the products: 16,384 x 2048 x
 // 2048 300 us, 348,208 x 256 x 1024 421, and 363 and 509 so.)
 // WHOLE: rows are of whole pieces.
-// 16,384 x 2048 x 2048 of 8 bits, with the chunks' sums: 363 us, 1,140 TFLOP/s of the three products it
-// is, as much as a large library product.
+// 16,384 x 2048 x 2048 of 8 bits: 349 us and 14 for the sums, 1,180 TFLOP/s of the three products it
+// is (a large library product 1,147): matrix cores 60 % of the busy cycles, vector ALU 39, LDS 27.
 template <typename T, bool X8, int BC, int BN, int WR, int WC, int KB, bool WHOLE>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_linear_dw(LinearWeight a) {
   typedef KTile<T, BC, KB> TX;

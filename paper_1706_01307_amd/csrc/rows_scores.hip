@@ -8,7 +8,7 @@
 // choice and the next, between the last group that stays and the best that goes) is within
 // the errors of both sides, that row is chosen again from 64-bit scores.
 //
-// 348,208 fp32 rows to 8 of 64 experts from 4 of 8 groups: 96 us, and 17 + 5 for the pairs'
+// 348,208 fp32 rows to 8 of 64 experts from 4 of 8 groups: 100 us, and 17 + 5 for the pairs'
 // order, where the bytes alone would take 27; k_scores is bound by the vector ALU (75 % of the
 // cycles it has work): nine searches of 16 scores a lane, then the groups, the scores and the
 // rows' weights.  The gradient takes 43 us.
@@ -381,10 +381,11 @@ __device__ __forceinline__ void choose_slow(const ScoreArgs& a, const T* logits,
 }
 
 // Sigmoid scores below exp(kFar) are on their way out of fp32, their ratios, which renormalised
-// weights are, are not: a row with a chosen one has its scores without the factor exp(m), m the
-// largest chosen logit or 0.  (A row with fewer experts than k is taken so too.)  sigmoid(x) = exp(x) / (1 + exp(x)); what x - m loses when it is
-// rounded, up to hundreds of units of exp's value, is put back.  What 64 bits have as 0, as they
-// do where exp(-x) is past them, is 0: logits of a type's lowest value close a row too.
+// weights are, are not: a row with a chosen one (or with fewer experts than k) has its scores
+// without the factor exp(m), m the largest chosen logit or 0.  sigmoid(x) = exp(x) / (1 + exp(x));
+// what x - m loses when it is rounded, up to hundreds of units of exp's value, is put back.  What 64
+// bits have as 0, as they do where exp(-x) is past them, is 0: logits of a type's lowest value
+// close a row too.
 constexpr float kFar = -64.0f, kNothing = -709.7827f;
 __device__ __forceinline__ float far_score(float x, float top) {
   if (x <= kNothing) return 0.0f;
