@@ -123,21 +123,21 @@ __device__ __forceinline__ void merge_two(uint32_t& a1, uint32_t& a2, uint32_t b
   a1 = a1 > b1 ? a1 : b1;
   a2 = low > rest ? low : rest;
 }
+// Half of what a group is worth (so that a sum of two numbers never leaves fp32), and of what its
+// roundings go with: the magnitudes of its terms, which may cancel in the sum.
 __device__ __forceinline__ float worth_of(uint32_t o1, uint32_t o2) {
-  const float w = value_of(o1 > kNone ? o1 : kNone);
-  return o2 > kNone ? w + value_of(o2) : w;
+  const float w = 0.5f * value_of(o1 > kNone ? o1 : kNone);
+  return o2 > kNone ? fmaf(0.5f, value_of(o2), w) : w;
 }
-// What a worth's roundings go with: the magnitudes of its terms, which may cancel in the sum.
 __device__ __forceinline__ float size_of(uint32_t o1, uint32_t o2) {
-  const float w = o1 > kNone ? fabsf(value_of(o1)) : 0.0f;
-  return o2 > kNone ? w + fabsf(value_of(o2)) : w;
+  const float w = o1 > kNone ? 0.5f * fabsf(value_of(o1)) : 0.0f;
+  return o2 > kNone ? fmaf(0.5f, fabsf(value_of(o2)), w) : w;
 }
 
 // The groups of a row that stay, by fp32 scores: o, the orders of a lane's NV * VEC biased scores,
 // become 0 where their group goes.  Returns whether the gap between the last group that stays and
 // the best that goes is within `near` and the roundings of the worths (half a unit of each biased
-// score and of their sum: kUnit of their magnitudes is twice that), or a sum is beyond fp32.  s_v: E
-// words.
+// score and of their sum: kUnit of their magnitudes is twice that).  s_v: E words.
 // Where a group is of whole pieces of 2^i lanes, its two best are found in registers, piece by
 // piece and then over those lanes; else by reading its scores from s_v.
 template <int LPR, int NV, int VEC>
@@ -147,11 +147,12 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
   const auto col = [&](int i) { return (lane + LPR * (i / VEC)) * VEC + i % VEC; };
   const auto either = [](uint32_t p, uint32_t q) { return p | q; };
   float low = INFINITY, high = -INFINITY;
-  bool odd = false;                                // (NaN, infinities and sums past fp32)
+  bool odd = false;                                // (NaN among them)
   // (the least that a group that stays can be worth, the most that one that goes can)
   auto note = [&](float worth, float size, bool in) {
-    odd |= !(size < INFINITY);
-    const float least = worth - kUnit * size, most = worth + kUnit * size;
+    odd |= worth != worth;
+    const float off = size < INFINITY ? kUnit * size : 0.0f;
+    const float least = worth - off, most = worth + off;
     if (in) low = least < low ? least : low;
     else high = most > high ? most : high;
   };
@@ -244,7 +245,7 @@ __device__ __forceinline__ bool keep_groups(uint32_t (&o)[NV * VEC], int lane, c
   low = over_row<LPR>(low, [](float p, float q) { return q < p ? q : p; });
   high = over_row<LPR>(high, [](float p, float q) { return q > p ? q : p; });
   if (over_row<LPR>(odd ? 1u : 0u, either)) return true;
-  return a.top_groups < a.groups && high > -INFINITY && low < INFINITY && !(low - high > 2 * near);
+  return a.top_groups < a.groups && high > -INFINITY && low < INFINITY && !(low - high > near);
 }
 
 // The k largest of a row's fp32 scores, of orders o, and whether a gap that decides is within

@@ -61,3 +61,17 @@ def test_worths_beyond_fp32():
     # a group of which nothing is open goes, however far below the other is
     x = torch.tensor([[-math.inf, -math.inf, 0.0, 0.0]])
     assert _experts(x, torch.tensor([9.0, 9.0, -3e38, -3e38]), 2, 2, 1).tolist() == [[2, 3]]
+
+
+def test_groups_closed_by_the_lowest_number():
+    """Biases of the type's lowest value, of one group's experts or of all but one of every group's,
+    and infinite ones."""
+    r, low = _gen(8), torch.finfo(torch.float32).min
+    x = r(200, 32)
+    for kind in ("sigmoid", "softmax"):
+        for shut in (slice(8, 16), [c for c in range(32) if c % 8 != 3], slice(0, 31), slice(0, 32)):
+            for value in (low, -math.inf, math.inf):
+                bias = r(32, std=0.1)
+                bias[shut] = value
+                want = ref.choose(x, bias, kind, 4, 2, 3)
+                assert torch.equal(_experts(x, bias, 3, 4, 2, kind), want), (kind, shut, value)
